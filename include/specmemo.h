@@ -347,6 +347,63 @@ int specmemo_kv_pad_update(specmemo_dtype dt, const specmemo_trees *t, const spe
                            uint32_t *key_valid, int64_t key_valid_words, int32_t *pos, void *ws, size_t ws_bytes,
                            void *stream);
 
+/* ---- Prompts and shared prefixes ----------------------------------------------
+ *
+ * The pool's committed rows come from prompts (Sec. 3.1: the cache is
+ * preallocated for the conversation's queries), and conversations that open
+ * with the same text need its K/V once.  A prefix is a range of pool rows that
+ * a sequence sees before its own slab rows: rows of their own, or committed rows
+ * of a slab.  Every K/V row that a call walks, masked for some query or not, must
+ * be finite; rows past a sequence's last one are never read. */
+
+/* Per sequence, host arrays [B]: first pool row and rows of its prefix (0 rows:
+ * none).  Sequences that follow one another in the batch with the same base and
+ * length share one: where their query rows are few, its keys are walked once for
+ * all of them. */
+typedef struct {
+  const int64_t *base_h;
+  const int32_t *len_h;
+} specmemo_prefix;
+
+/* Causal attention of prompt tokens (or a chunk of a prompt, or single tokens)
+ * of a ragged batch, packed without padding.  Sequence b brings the T_b =
+ * new_off_h[b+1] - new_off_h[b] >= 0 tokens whose q rows are new_off_h[b] ..;
+ * their K/V rows are slab rows L_b .. L_b + T_b - 1, written by the caller
+ * before the call (L_b = kv->seq_len_h[b]).  For its token i and query head hq,
+ * with KV head kv = hq / (n_q / n_kv):
+ *   keys = prefix rows 0 .. P_b - 1 (if any), slab rows 0 .. L_b + i
+ *   out[new_off[b] + i][hq] = softmax(scale * q . K[kv][key]) . V[kv][key]
+ * new_off_h: host [B+1], new_off_h[0] = 0, non-decreasing, 1 <= B <=
+ * SPECMEMO_MAX_BATCH.  q, out: device [new_off_h[B]][n_q][head_dim] in `dt`;
+ * out may not overlap q (both are ignored where no sequence brings a token).
+ * prefix: NULL for none.  scale, dtypes, head_dim and
+ * slab limits are those of specmemo_tree_attn (a prefix is at most 2^23 rows
+ * too), and L_b + T_b <= seq_cap[b].  The lengths are the caller's to advance
+ * afterwards: the call writes `out` alone.  kv->seq_len is not read.
+ * ws: specmemo_prompt_attn_bytes(...) bytes, 16-byte aligned (the parts of rows
+ * whose keys are walked by several work items, and the descriptors of more than
+ * 48 ranges of rows; may be 0). */
+int specmemo_prompt_attn(specmemo_dtype dt, int32_t B, const int32_t *new_off_h, const specmemo_kv *kv,
+                         const specmemo_prefix *prefix, int32_t n_q, float scale, const void *q, void *out, void *ws,
+                         size_t ws_bytes, void *stream);
+/* Workspace bytes of that call (0 also for invalid arguments, which the call
+ * reports).  Depends on the current device's compute-unit count, as
+ * specmemo_workspace_bytes does. */
+size_t specmemo_prompt_attn_bytes(specmemo_dtype dt, int32_t B, const int32_t *new_off_h, const specmemo_kv *kv,
+                                  const specmemo_prefix *prefix, int32_t n_q);
+
+/* (b'') Tree attention of sequences that see a prefix before their own rows:
+ * specmemo_tree_attn with
+ *   keys = prefix rows 0 .. P_b - 1, slab rows 0 .. L_b - 1, the root path
+ * Same arguments, shapes and limits; prefix must be given (lengths may be 0).
+ * The result is that of specmemo_tree_attn over slabs that hold the prefix's
+ * rows first, up to rounding.  ws: specmemo_tree_attn_prefix_bytes(...) bytes. */
+int specmemo_tree_attn_prefix(specmemo_dtype dt, const specmemo_trees *t, const specmemo_kv *kv,
+                              const specmemo_prefix *prefix, int32_t n_q, float scale, const void *q, void *out,
+                              void *ws, size_t ws_bytes, void *stream);
+size_t specmemo_tree_attn_prefix_bytes(specmemo_dtype dt, const specmemo_trees *t, const specmemo_kv *kv,
+                                       const specmemo_prefix *prefix, int32_t n_q);
+
 /* ---- Memory budget and tree construction (host only) -------------------------
  *
  * SpecMemo's memory model (Sec. 3.1, Eq. 1-6) and its tree construction

@@ -14,8 +14,8 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 OUT = os.path.join(HERE, "_build")
 LIB = os.path.join(OUT, "libspecmemo.so")
-SOURCES = ["api.cpp", "budget.cpp", "medusa_topk.hip", "tree_attn.hip", "accept.hip", "kv_compact.hip",
-           "upload.hip"]
+SOURCES = ["api.cpp", "budget.cpp", "medusa_topk.hip", "tree_attn.hip", "accept.hip", "kv_compact.hip", "range_attn.hip",
+           "upload.hip", "walk_plan.cpp"]
 ARCH = "gfx950"
 
 FLAGS = [
@@ -29,7 +29,7 @@ FLAGS = [
 # (scores of finite inputs, -inf for masked keys), and with NaNs honoured every
 # float maximum of a matrix-core result is preceded by a canonicalising
 # instruction (32 extra vector operations per key tile).
-EXTRA = {"tree_attn.hip": ["-fno-honor-nans"]}
+EXTRA = {"tree_attn.hip": ["-fno-honor-nans"], "range_attn.hip": ["-fno-honor-nans"]}
 
 
 def hipcc() -> str:

@@ -746,6 +746,189 @@ int specmemo_tree_attn_padded(specmemo_dtype dt, const specmemo_trees *t, const 
   return tree_attn_impl(dt, t, kv, key_valid, n_q, scale, q, out, ws, ws_bytes, stream);
 }
 
+}  // extern "C"
+
+// ---- prompts and shared prefixes -----------------------------------------------------
+
+namespace {
+
+// A prefix must lie in the pool, and where it reaches into a slab, in its committed rows.
+int check_prefix(const specmemo_prefix *px, const specmemo_kv *kv, int dt, int B) {
+  if (!px) return SPECMEMO_OK;
+  if (!px->base_h || !px->len_h) return fail(SPECMEMO_E_ARG, "prefix host arrays must be non-NULL");
+  std::vector<int> order(B);
+  std::iota(order.begin(), order.end(), 0);
+  std::sort(order.begin(), order.end(), [&](int x, int y) { return kv->seq_base_h[x] < kv->seq_base_h[y]; });
+  for (int b = 0; b < B; ++b) {
+    const int64_t base = px->base_h[b], len = px->len_h[b];
+    if (len < 0) return fail(SPECMEMO_E_ARG, "sequence %d: prefix of %lld rows", b, (long long)len);
+    if (len == 0) continue;
+    if (base < 0 || base > kv->cap_total - len)
+      return fail(SPECMEMO_E_BUDGET, "sequence %d: prefix of %lld rows at %lld outside the pool of %lld rows", b,
+                  (long long)len, (long long)base, (long long)kv->cap_total);
+    if (dt == SPECMEMO_BF16 && len > kMaxSlabRows)
+      return fail(SPECMEMO_E_BUDGET, "sequence %d: prefix of %lld rows exceeds %d", b, (long long)len, kMaxSlabRows);
+    if (b > 0 && base == px->base_h[b - 1] && len == px->len_h[b - 1]) continue;
+    // the slabs that begin before the prefix ends, from the last one back to the prefix's start
+    auto it = std::lower_bound(order.begin(), order.end(), base + len, [&](int s, int64_t v) { return kv->seq_base_h[s] < v; });
+    while (it != order.begin()) {
+      const int s = *--it;
+      const int64_t sb = kv->seq_base_h[s], se = sb + kv->seq_cap_h[s];
+      if (kv->seq_cap_h[s] == 0) continue;
+      if (se <= base) break;
+      if (std::min(base + len, se) > sb + kv->seq_len_h[s])
+        return fail(SPECMEMO_E_BUDGET, "sequence %d: prefix rows [%lld, %lld) reach past the committed rows of slab %d", b,
+                    (long long)base, (long long)(base + len), s);
+    }
+  }
+  return SPECMEMO_OK;
+}
+
+// Shared checks of the two calls (lengths and trees are checked before).
+int check_walk(int dt, const TreeInfo &ti, const int32_t *off_h, const specmemo_kv *kv, const specmemo_prefix *px, int n_q) {
+  int rc;
+  if ((rc = check_kv(dt, kv, ti, off_h))) return rc;
+  if (n_q < 1 || n_q % kv->n_kv) return fail(SPECMEMO_E_ARG, "n_q=%d must be a positive multiple of n_kv=%d", n_q, kv->n_kv);
+  for (int b = 0; b < ti.B; ++b) {
+    if (dt == SPECMEMO_BF16 && kv->seq_cap_h[b] > kMaxSlabRows)
+      return fail(SPECMEMO_E_BUDGET, "seq_cap[%d]=%d exceeds %d rows", b, kv->seq_cap_h[b], kMaxSlabRows);
+    if ((int64_t)(off_h[b + 1] - off_h[b]) * (n_q / kv->n_kv) > INT32_MAX / 2)
+      return fail(SPECMEMO_E_ARG, "sequence %d: too many query rows", b);
+  }
+  return check_prefix(px, kv, dt, ti.B);
+}
+
+int check_prompt(int dt, int B, const int32_t *off, const specmemo_kv *kv, const specmemo_prefix *px, int n_q, TreeInfo *ti) {
+  int rc;
+  if ((rc = check_dtype(dt))) return rc;
+  if (B < 1 || B > SPECMEMO_MAX_BATCH) return fail(SPECMEMO_E_ARG, "B=%d outside [1, %d]", B, SPECMEMO_MAX_BATCH);
+  if (!off) return fail(SPECMEMO_E_ARG, "new_off_h is NULL");
+  if (off[0] != 0) return fail(SPECMEMO_E_ARG, "new_off[0]=%d, expected 0", off[0]);
+  for (int b = 0; b < B; ++b)
+    if (off[b + 1] < off[b]) return fail(SPECMEMO_E_ARG, "new_off[%d]=%d after %d", b + 1, off[b + 1], off[b]);
+  ti->B = B;
+  ti->total = off[B];
+  return check_walk(dt, *ti, off, kv, px, n_q);
+}
+
+WalkPlan make_walk(int dt, bool causal, const TreeInfo &ti, const int32_t *off_h, const specmemo_kv *kv,
+                   const specmemo_prefix *px, int n_q) {
+  std::vector<WalkSeq> seqs;
+  for (int b = 0; b < ti.B; ++b) {
+    WalkSeq s{};
+    s.T = off_h[b + 1] - off_h[b];
+    if (s.T == 0) continue;
+    s.base = kv->seq_base_h[b];
+    s.L = kv->seq_len_h[b];
+    s.row0 = off_h[b];
+    if (px && px->len_h[b] > 0) {
+      s.pbase = px->base_h[b];
+      s.P = px->len_h[b];
+    }
+    seqs.push_back(s);
+  }
+  WalkPlan p;
+  plan_walk(dt, causal, seqs, kv->n_kv, n_q / kv->n_kv, device_cus(), &p);
+  return p;
+}
+
+size_t walk_table_bytes(const WalkPlan &p) {
+  return p.sets.size() > (size_t)kMaxWalkSets ? align256(p.sets.size() * sizeof(WalkSet)) : 0;
+}
+size_t walk_ws_bytes(const WalkPlan &p, int head_dim) {
+  return walk_table_bytes(p) +
+         (size_t)p.parts * (size_t)(p.rb / 32) * walk_unit_floats((head_dim + 31) / 32) * sizeof(float);
+}
+
+int run_walk(int dt, bool tree, const TreeInfo &ti, const int32_t *off_h, const int32_t *parent, const specmemo_kv *kv,
+             const specmemo_prefix *px, int n_q, float scale, const void *q, void *out, void *ws, size_t ws_bytes,
+             void *stream) {
+  if (!(scale > 0.f)) scale = 1.0f / std::sqrt((float)kv->head_dim);
+  if (!std::isfinite(scale)) return fail(SPECMEMO_E_ARG, "scale is not finite");
+  if (ti.total == 0) return ok();
+  if (!al(q, 16) || !al(out, 16)) return fail(SPECMEMO_E_ARG, "q / out must be non-NULL and 16-byte aligned");
+  const WalkPlan p = make_walk(dt, !tree, ti, off_h, kv, px, n_q);
+  if (p.slots > INT32_MAX / 8 || p.cslots > INT32_MAX / 8 || p.parts > INT32_MAX)
+    return fail(SPECMEMO_E_ARG, "too many work items: %lld", (long long)p.slots);
+  const size_t need = walk_ws_bytes(p, kv->head_dim);
+  if (need && (!al(ws, 16) || ws_bytes < need))
+    return fail(SPECMEMO_E_WORKSPACE, "workspace of %zu bytes needed (16-byte aligned), got %zu", need, ws ? ws_bytes : 0);
+  WalkArgs a{};
+  a.q = q;
+  a.out = out;
+  a.k = kv->k;
+  a.v = kv->v;
+  a.parent = parent;
+  a.cap_total = kv->cap_total;
+  a.n_q = n_q;
+  a.n_kv = kv->n_kv;
+  a.group = n_q / kv->n_kv;
+  a.head_dim = kv->head_dim;
+  a.units = p.units;
+  a.fan = p.fan;
+  a.nset = (int)p.sets.size();
+  a.slots = (int)p.slots;
+  a.cslots = (int)p.cslots;
+  a.rb = p.rb;
+  a.scale_log2 = scale * 1.4426950408889634f;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  uint8_t *w = static_cast<uint8_t *>(ws);
+  const size_t tab = walk_table_bytes(p);
+  if (tab) {
+    hipError_t e = upload_table(p.sets.data(), p.sets.size() * sizeof(WalkSet), w, st);
+    if (e != hipSuccess) return hip_status(e, "descriptor upload");
+    a.tab = reinterpret_cast<const WalkSet *>(w);
+  } else {
+    std::copy(p.sets.begin(), p.sets.end(), a.set);
+  }
+  a.part = reinterpret_cast<float *>(w + tab);
+  return hip_status(launch_walk_attn(dt, tree, a, st), tree ? "tree attention launch" : "prompt attention launch");
+}
+
+int check_tree_prefix(int dt, const specmemo_trees *t, const specmemo_kv *kv, const specmemo_prefix *px, int n_q, TreeInfo *ti) {
+  int rc;
+  if ((rc = check_dtype(dt))) return rc;
+  if ((rc = check_trees(t, ti))) return rc;
+  if (!px) return fail(SPECMEMO_E_ARG, "prefix is NULL");
+  return check_walk(dt, *ti, t->node_off_h, kv, px, n_q);
+}
+
+}  // namespace
+
+extern "C" {
+
+int specmemo_prompt_attn(specmemo_dtype dt, int32_t B, const int32_t *new_off_h, const specmemo_kv *kv,
+                         const specmemo_prefix *prefix, int32_t n_q, float scale, const void *q, void *out, void *ws,
+                         size_t ws_bytes, void *stream) {
+  TreeInfo ti;
+  const int rc = check_prompt(dt, B, new_off_h, kv, prefix, n_q, &ti);
+  if (rc) return rc;
+  return run_walk(dt, false, ti, new_off_h, nullptr, kv, prefix, n_q, scale, q, out, ws, ws_bytes, stream);
+}
+
+size_t specmemo_prompt_attn_bytes(specmemo_dtype dt, int32_t B, const int32_t *new_off_h, const specmemo_kv *kv,
+                                  const specmemo_prefix *prefix, int32_t n_q) {
+  TreeInfo ti;
+  if (check_prompt(dt, B, new_off_h, kv, prefix, n_q, &ti)) return 0;
+  return walk_ws_bytes(make_walk(dt, true, ti, new_off_h, kv, prefix, n_q), kv->head_dim);
+}
+
+int specmemo_tree_attn_prefix(specmemo_dtype dt, const specmemo_trees *t, const specmemo_kv *kv,
+                              const specmemo_prefix *prefix, int32_t n_q, float scale, const void *q, void *out, void *ws,
+                              size_t ws_bytes, void *stream) {
+  TreeInfo ti;
+  const int rc = check_tree_prefix(dt, t, kv, prefix, n_q, &ti);
+  if (rc) return rc;
+  return run_walk(dt, true, ti, t->node_off_h, t->parent, kv, prefix, n_q, scale, q, out, ws, ws_bytes, stream);
+}
+
+size_t specmemo_tree_attn_prefix_bytes(specmemo_dtype dt, const specmemo_trees *t, const specmemo_kv *kv,
+                                       const specmemo_prefix *prefix, int32_t n_q) {
+  TreeInfo ti;
+  if (check_tree_prefix(dt, t, kv, prefix, n_q, &ti)) return 0;
+  return walk_ws_bytes(make_walk(dt, false, ti, t->node_off_h, kv, prefix, n_q), kv->head_dim);
+}
+
 int specmemo_accept(specmemo_dtype dt, const specmemo_trees *t, int32_t vocab, specmemo_accept_mode mode,
                     float temperature, float eps, float delta, const void *base_logits, const int32_t *node_tok,
                     int32_t *accept_len, int32_t *path, int32_t path_stride, int32_t *next_tok, void *ws,

@@ -46,6 +46,10 @@ class _KV(C.Structure):
                 ("seq_cap_h", C.c_void_p), ("seq_len_h", C.c_void_p)]
 
 
+class _Prefix(C.Structure):
+    _fields_ = [("base_h", C.c_void_p), ("len_h", C.c_void_p)]
+
+
 class _Budget(C.Structure):
     _fields_ = [("max_memory", C.c_int64), ("base_model_bytes", C.c_int64), ("head_bytes", C.c_int64),
                 ("layers", C.c_int32), ("n_kv", C.c_int32), ("head_dim", C.c_int32), ("vocab", C.c_int32),
@@ -103,6 +107,15 @@ def load():
         lib.specmemo_tree_attn_padded.restype = C.c_int
         lib.specmemo_kv_pad_update.argtypes = [i32, PT, PK, vp, vp, i32, vp, i64, vp, vp, sz, vp]
         lib.specmemo_kv_pad_update.restype = C.c_int
+        PP = C.POINTER(_Prefix)
+        lib.specmemo_prompt_attn.argtypes = [i32, i32, vp, PK, PP, i32, f32, vp, vp, vp, sz, vp]
+        lib.specmemo_prompt_attn.restype = C.c_int
+        lib.specmemo_prompt_attn_bytes.argtypes = [i32, i32, vp, PK, PP, i32]
+        lib.specmemo_prompt_attn_bytes.restype = sz
+        lib.specmemo_tree_attn_prefix.argtypes = [i32, PT, PK, PP, i32, f32, vp, vp, vp, sz, vp]
+        lib.specmemo_tree_attn_prefix.restype = C.c_int
+        lib.specmemo_tree_attn_prefix_bytes.argtypes = [i32, PT, PK, PP, i32]
+        lib.specmemo_tree_attn_prefix_bytes.restype = sz
         lib.specmemo_mem_kv_bytes.argtypes = [i32, i32, i32, i32, i64, i32]
         lib.specmemo_mem_buffer_bytes.argtypes = [i32, i32, i32, i32, i32, i32]
         lib.specmemo_mem_total_bytes.argtypes = [i64, i64, i32, i64, i64]
@@ -380,6 +393,61 @@ def kv_pad_update(dt: int, trees: Trees, kv: KVPool, accept_len, path, path_stri
     _check(load().specmemo_kv_pad_update(dt, C.byref(ts), C.byref(ks), _ptr(accept_len), _ptr(path), path_stride,
                                          _ptr(key_valid), _words(key_valid, key_valid_words), _ptr(pos), _ptr(ws),
                                          ws_bytes, _stream(stream)))
+
+
+# ---- prompts and shared prefixes ----------------------------------------------------
+
+class Prefix:
+    """Rows of the pool that a sequence sees before its own slab rows: first row and length per sequence (host arrays)."""
+
+    def __init__(self, base, length):
+        self.base_h = np.ascontiguousarray(base, dtype=np.int64)
+        self.len_h = _i32(length)
+        if self.base_h.shape != self.len_h.shape or self.base_h.ndim != 1:
+            raise ValueError("one base and one length per sequence")
+
+    def struct(self) -> _Prefix:
+        return _Prefix(_host_addr(self.base_h), _host_addr(self.len_h))
+
+
+def _prefix_ref(prefix: Optional[Prefix], B: int):
+    if prefix is None:
+        return None
+    if len(prefix.base_h) != B or len(prefix.len_h) != B:
+        raise ValueError(f"prefix of {len(prefix.base_h)} sequences for a batch of {B}")
+    return C.byref(prefix.struct())
+
+
+def _new_off(new_off, kv: KVPool) -> np.ndarray:
+    off = _i32(new_off)
+    if off.ndim != 1 or len(off) < 1 or min(len(kv.seq_base_h), len(kv.seq_cap_h), len(kv.seq_len_h)) < len(off) - 1:
+        raise ValueError(f"new_off of {off.shape} for a pool of {len(kv.seq_base_h)} sequences")
+    return off
+
+
+def prompt_attn_bytes(dt: int, new_off, kv: KVPool, n_q: int, prefix: Optional[Prefix] = None) -> int:
+    off, ks = _new_off(new_off, kv), kv.struct()
+    return int(load().specmemo_prompt_attn_bytes(dt, len(off) - 1, _host_addr(off), C.byref(ks),
+                                                 _prefix_ref(prefix, len(off) - 1), n_q))
+
+
+def prompt_attn(dt: int, new_off, kv: KVPool, n_q: int, q, out, prefix: Optional[Prefix] = None, scale: float = 0.0,
+                ws=None, ws_bytes: int = 0, stream=None):
+    off, ks = _new_off(new_off, kv), kv.struct()
+    _check(load().specmemo_prompt_attn(dt, len(off) - 1, _host_addr(off), C.byref(ks), _prefix_ref(prefix, len(off) - 1),
+                                       n_q, scale, _ptr(q), _ptr(out), _ptr(ws), ws_bytes, _stream(stream)))
+
+
+def tree_attn_prefix_bytes(dt: int, trees: Trees, kv: KVPool, prefix: Prefix, n_q: int) -> int:
+    ts, ks = trees.struct(), kv.struct()
+    return int(load().specmemo_tree_attn_prefix_bytes(dt, C.byref(ts), C.byref(ks), _prefix_ref(prefix, trees.B), n_q))
+
+
+def tree_attn_prefix(dt: int, trees: Trees, kv: KVPool, prefix: Prefix, n_q: int, q, out, scale: float = 0.0, ws=None,
+                     ws_bytes: int = 0, stream=None):
+    ts, ks = trees.struct(), kv.struct()
+    _check(load().specmemo_tree_attn_prefix(dt, C.byref(ts), C.byref(ks), _prefix_ref(prefix, trees.B), n_q, scale,
+                                            _ptr(q), _ptr(out), _ptr(ws), ws_bytes, _stream(stream)))
 
 
 # ---- memory budget and tree construction (host) ------------------------------

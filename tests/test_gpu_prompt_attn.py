@@ -1,0 +1,150 @@
+"""GPU: causal attention of prompt tokens over the pool, against 64 bits."""
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2506_01986_amd import specmemo as sm
+from tests.serving_ref import Batch, causal, check
+
+pytestmark = pytest.mark.gpu
+
+
+def ws_for(x):
+    n = sm.prompt_attn_bytes(x.dt, x.off, x.kv, x.n_q, x.px)
+    return torch.full((max(16, n),), 255, dtype=torch.uint8, device="cuda"), n     # NaN in every unwritten part
+
+
+def run(x, **kw):
+    ws, n = ws_for(x)
+    sm.prompt_attn(x.dt, x.off, x.kv, x.n_q, x.qd, x.out, prefix=x.px, ws=ws, ws_bytes=n, **kw)
+    torch.cuda.synchronize()
+    return x.out
+
+
+def parity(x, **kw):
+    x.upload()
+    ref, tol = x.reference(lambda b: causal(x.n[b]), scale=kw.get("scale"))
+    check(run(x, **kw), ref, tol)
+
+
+def draw(seed, hi, n):
+    return [int(v) for v in np.random.default_rng(seed).integers(0, hi, n)]
+
+
+# query heads, KV heads, new tokens, committed rows, prefix rows, groups of one prefix
+BF16 = {
+    "one_token": (1, 1, [1], [0], None, None),
+    "empty_and_single": (8, 2, [0, 1, 0, 3, 0], [5, 63, 0, 64, 7], None, None),
+    "all_empty": (8, 2, [0, 0], [5, 0], None, None),
+    "tile_edges": (4, 4, [63, 64, 65, 127, 128, 129], [0, 0, 0, 0, 0, 0], None, None),
+    "after_committed": (4, 4, [63, 64, 65, 1, 2], [1, 64, 129, 300, 63], None, None),
+    "one_long": (2, 2, [1000], [0], None, None),                       # split in chunks
+    "one_long_gqa": (16, 2, [700], [333], None, None),
+    "gqa_odd": (15, 3, [37, 150, 5], [20, 0, 400], None, None),        # five heads a KV head: rows end inside tokens
+    "gqa_7": (7, 1, [130, 41], [0, 90], None, None),
+    "mqa": (32, 1, [50, 3], [100, 17], None, None),                    # one KV head over all XCDs
+    "kv_heads_12": (12, 12, [40, 200], [0, 10], None, None),
+    "kv_heads_40": (40, 40, [33], [100], None, None),
+    "decode": (64, 8, [1] * 9, [0, 1, 63, 64, 65, 1000, 3000, 127, 128], None, None),
+    "decode_mha": (8, 8, [1] * 5, [2000, 100, 5, 0, 640], None, None),
+    "few_tokens": (16, 2, [1, 7, 8, 9, 2], [500, 600, 2500, 0, 1], None, None),
+    "prefix_shared": (8, 2, [20, 1, 64, 3], [0, 30, 7, 100], [150] * 4, [0, 0, 0, 0]),
+    "prefix_decode": (32, 4, [1] * 12, draw(1, 90, 12), [700] * 12, [0] * 12),
+    "prefix_mixed": (8, 8, [5, 90, 0, 4, 4, 1], [3, 0, 9, 64, 0, 12], [64, 64, 64, 0, 129, 129], [0, 0, 0, 1, 2, 2]),
+    "prefix_long_prompts": (8, 1, [300, 200], [0, 70], [513, 513], [0, 0]),
+    "many": (4, 2, draw(2, 30, 60), draw(3, 200, 60), None, None),     # more sets than the arguments hold
+    "many_prefixes": (4, 1, draw(4, 9, 70), draw(5, 60, 70), [40] * 70, [i // 2 for i in range(70)]),
+}
+
+
+@pytest.mark.parametrize("name", list(BF16))
+def test_bf16(name):
+    n_q, n_kv, n, L, P, shared = BF16[name]
+    parity(Batch("bf16", n_q, n_kv, 128, n, L, P, shared, seed=len(name)))
+
+
+@pytest.mark.parametrize("d", [4, 20, 32, 36, 64, 96, 100, 128])
+def test_fp32_head_dims(d):
+    parity(Batch("fp32", 6, 2, d, [1, 31, 32, 33, 70, 0], [0, 40, 1, 64, 100, 3], seed=d))
+
+
+@pytest.mark.parametrize("name", ["decode", "one_long", "gqa_odd", "prefix_shared", "prefix_decode", "prefix_mixed", "many",
+                                  "many_prefixes", "kv_heads_12"])
+def test_fp32(name):
+    n_q, n_kv, n, L, P, shared = BF16[name]
+    parity(Batch("fp32", n_q, n_kv, 64, n, L, P, shared, seed=len(name)))
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_scale_and_peaked_scores(dtype):
+    """Scores of several hundred: one key takes almost all of a row, and the running maximum moves often."""
+    parity(Batch(dtype, 4, 2, 128 if dtype == "bf16" else 36, [90, 33], [200, 0], seed=3, std=3.0), scale=1.0)
+
+
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_equal_scores(dtype):
+    """Zero queries: the mean of the visible V rows."""
+    x = Batch(dtype, 2, 2, 128, [130], [70], seed=4)
+    x.q.zero_()
+    parity(x)
+
+
+def test_same_prompt_in_chunks():
+    """A prompt in one call, and token ranges of it on their committed rows, agree within two roundings."""
+    x = Batch("bf16", 8, 2, 128, [333], [0], seed=9).upload()
+    whole = run(x).clone()
+    for i0, i1 in ((0, 1), (1, 100), (100, 300), (300, 333)):
+        kv = sm.KVPool(x.kd, x.vd, x.kv.seq_len, x.base, x.cap, [i0])
+        out = torch.empty_like(x.qd[i0:i1])
+        n = sm.prompt_attn_bytes(x.dt, [0, i1 - i0], kv, 8)
+        ws = torch.empty(max(16, n), dtype=torch.uint8, device="cuda")
+        sm.prompt_attn(x.dt, [0, i1 - i0], kv, 8, x.qd[i0:i1].contiguous(), out, ws=ws, ws_bytes=n)
+        ref, tol = x.reference(lambda b: causal(333))
+        check(out, ref[i0:i1], tol[i0:i1])
+        assert (out.float() - whole[i0:i1].float()).abs().max() <= 2 * tol[i0:i1].max()
+
+
+def test_prefix_in_committed_rows():
+    """A prefix may be another sequence's committed rows."""
+    x = Batch("bf16", 4, 2, 128, [9, 4], [200, 11], seed=5).upload()
+    px = sm.Prefix([0, x.base[0]], [0, 120])
+    n = sm.prompt_attn_bytes(x.dt, x.off, x.kv, 4, px)
+    ws = torch.empty(max(16, n), dtype=torch.uint8, device="cuda")
+    sm.prompt_attn(x.dt, x.off, x.kv, 4, x.qd, x.out, prefix=px, ws=ws, ws_bytes=n)
+    torch.cuda.synchronize()
+    x.pbase, x.plen = [0, x.base[0]], [0, 120]
+    check(x.out, *x.reference(lambda b: causal(x.n[b])))
+
+
+@pytest.mark.parametrize("name", ["prefix_mixed", "one_long_gqa", "many"])
+def test_captured_and_on_another_stream(name):
+    """A captured call, replayed between eager calls on other data, gives the eager result every time."""
+    n_q, n_kv, n, L, P, shared = BF16[name]
+    x = Batch("bf16", n_q, n_kv, 128, n, L, P, shared, seed=7).upload()
+    want = run(x).clone()
+    ws, nb = ws_for(x)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(side):
+        with torch.cuda.graph(graph, stream=side):
+            sm.prompt_attn(x.dt, x.off, x.kv, x.n_q, x.qd, x.out, prefix=x.px, ws=ws, ws_bytes=nb)
+        q0 = x.qd.clone()
+        for i in range(3):
+            x.out.fill_(555.0)
+            x.qd.copy_(q0)
+            graph.replay()
+            side.synchronize()
+            assert torch.equal(x.out.view(torch.int16), want.view(torch.int16)), i
+            x.qd.normal_()                                   # an eager call on other queries in between
+            sm.prompt_attn(x.dt, x.off, x.kv, x.n_q, x.qd, x.out, prefix=x.px, ws=ws, ws_bytes=nb)
+            side.synchronize()
+
+
+def test_repeats_bit_for_bit():
+    n_q, n_kv, n, L, P, shared = BF16["prefix_decode"]
+    x = Batch("bf16", n_q, n_kv, 128, n, L, P, shared, seed=8).upload()
+    first = run(x).clone()
+    for _ in range(3):
+        assert torch.equal(run(x).view(torch.int16), first.view(torch.int16))
