@@ -404,6 +404,57 @@ int specmemo_tree_attn_prefix(specmemo_dtype dt, const specmemo_trees *t, const 
 size_t specmemo_tree_attn_prefix_bytes(specmemo_dtype dt, const specmemo_trees *t, const specmemo_kv *kv,
                                        const specmemo_prefix *prefix, int32_t n_q);
 
+/* ---- Rules on logits ------------------------------------------------------------
+ *
+ * Penalties for tokens that occurred, biases and grammar masks, applied to the
+ * base model's logits of every tree node before specmemo_accept or
+ * specmemo_sample_next reads them.  A node's history is the sequence's committed
+ * tokens (counts) and the tokens on its own root path (App. A.1: a candidate is
+ * verified as the continuation of its path).  1 <= vocab <= 2^30. */
+typedef struct {
+  const int32_t *counts;      /* device [B][vocab]: times each token occurred so far; NULL: none did */
+  const float *repetition;    /* device [B] > 0, or NULL: 1 */
+  const float *presence;      /* device [B] or NULL: 0 */
+  const float *frequency;     /* device [B] or NULL: 0 */
+  const int32_t *bias_off;    /* device [B+1]: entries bias_off[b] .. bias_off[b+1] - 1 are sequence b's */
+  const int32_t *bias_id;     /* device [n_bias]: token ids; ids outside [0, vocab) are ignored, of equal ids the last counts */
+  const float *bias_val;      /* device [n_bias] */
+  int32_t n_bias;             /* all sequences' entries; 0: no biases (the three arrays may be NULL) */
+  const uint32_t *mask;       /* device [n_masks][mask_words]: bit v % 32 of word v / 32 set = token v is allowed */
+  const int32_t *mask_idx;    /* device [sum N_b]: mask of each node's row; outside [0, n_masks): every token is allowed */
+  int32_t n_masks;            /* 0: no masks (the two arrays may be NULL) */
+  int32_t mask_words;         /* words of a mask, >= ceil(vocab / 32) */
+} specmemo_rules;
+
+/* For node u of sequence b and token v, with z = logits[u][v]:
+ *   c = counts[b][v] + how often v occurs among the tokens root .. u (node_tok)
+ *   x = z;  if c > 0: x = (x > 0 ? x / repetition[b] : x * repetition[b])
+ *                         - frequency[b] * c - presence[b]
+ *   out[u][v] = x + bias[b][v], or -inf where u's mask does not allow v
+ * in fp32, rounded once to `dt`.  logits, out: device [sum N_b][vocab] in `dt`,
+ * 16-byte aligned, the same buffer or not overlapping.  node_tok: device int32
+ * [sum N_b], read only with one of the three penalties (else it may be NULL);
+ * tokens outside [0, vocab) count for nothing.  A row whose mask allows no token
+ * is all -inf: greedy acceptance then takes token 0, and typical acceptance and
+ * sampling are not defined for it. */
+int specmemo_logit_rules(specmemo_dtype dt, const specmemo_trees *t, int32_t vocab, const specmemo_rules *rules,
+                         const int32_t *node_tok, const void *logits, void *out, void *stream);
+
+/* counts[b][v] = how often v occurs in tokens[tok_off[b]] .. tokens[tok_off[b+1] - 1]
+ * (added to what counts holds where accumulate is nonzero); tokens outside
+ * [0, vocab) are ignored.  tok_off: device int32 [B+1] with host mirror tok_off_h,
+ * tok_off[0] = 0, non-decreasing; tokens: device int32 [tok_off[B]]; counts:
+ * device int32 [B][vocab].  1 <= B <= SPECMEMO_MAX_BATCH. */
+int specmemo_token_counts(int32_t B, int32_t vocab, const int32_t *tok_off_h, const int32_t *tok_off,
+                          const int32_t *tokens, int32_t *counts, int32_t accumulate, void *stream);
+
+/* After acceptance: counts[b][node_tok of path[b][j]] += 1, j = 0..accept_len[b],
+ * the tokens the step committed.  accept_len, path: as written by specmemo_accept;
+ * a sequence whose accept_len or path entries are out of range (negative, past
+ * its tree, or not increasing) adds nothing. */
+int specmemo_count_accepted(const specmemo_trees *t, int32_t vocab, const int32_t *node_tok, const int32_t *accept_len,
+                            const int32_t *path, int32_t path_stride, int32_t *counts, void *stream);
+
 /* ---- Memory budget and tree construction (host only) -------------------------
  *
  * SpecMemo's memory model (Sec. 3.1, Eq. 1-6) and its tree construction

@@ -14,7 +14,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 OUT = os.path.join(HERE, "_build")
 LIB = os.path.join(OUT, "libspecmemo.so")
-SOURCES = ["api.cpp", "budget.cpp", "medusa_topk.hip", "tree_attn.hip", "accept.hip", "kv_compact.hip", "range_attn.hip",
+SOURCES = ["api.cpp", "budget.cpp", "medusa_topk.hip", "tree_attn.hip", "accept.hip", "kv_compact.hip", "range_attn.hip", "logit_rules.hip",
            "upload.hip", "walk_plan.cpp"]
 ARCH = "gfx950"
 

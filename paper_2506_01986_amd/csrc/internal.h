@@ -237,6 +237,35 @@ struct SampleArgs {
 int sample_segments(int vocab);
 hipError_t launch_sample_next(int dt, const SampleArgs &a, int B, uint64_t *words, hipStream_t st);
 
+// ---- rules on logits -------------------------------------------------------------
+struct RulesArgs {
+  const void *logits;
+  void *out;
+  const int32_t *node_off, *parent, *node_tok;
+  const int32_t *counts;                             // [B][vocab] or null
+  const float *repetition, *presence, *frequency;    // [B] or null (1, 0, 0)
+  const int32_t *bias_off, *bias_id;
+  const float *bias_val;
+  const uint32_t *mask;
+  const int32_t *mask_idx;
+  int32_t n_bias, n_masks, mask_words, vocab;
+  int32_t penalties;         // any of the three is given
+  int32_t groups;            // row groups of the largest tree
+};
+hipError_t launch_logit_rules(int dt, const RulesArgs &a, int B, int max_nodes, hipStream_t st);
+struct CountArgs {
+  const int32_t *tok_off, *tokens;
+  int32_t *counts;
+  int32_t vocab, total, accumulate;
+};
+hipError_t launch_token_counts(const CountArgs &a, int B, hipStream_t st);
+struct AcceptedArgs {
+  const int32_t *node_off, *node_tok, *accept_len, *path;
+  int32_t *counts;
+  int32_t vocab, path_stride;
+};
+hipError_t launch_count_accepted(const AcceptedArgs &a, int B, hipStream_t st);
+
 // ---- compaction ------------------------------------------------------------------
 struct CompactSeq {
   int64_t base;

@@ -50,6 +50,12 @@ class _Prefix(C.Structure):
     _fields_ = [("base_h", C.c_void_p), ("len_h", C.c_void_p)]
 
 
+class _Rules(C.Structure):
+    _fields_ = [("counts", C.c_void_p), ("repetition", C.c_void_p), ("presence", C.c_void_p), ("frequency", C.c_void_p),
+                ("bias_off", C.c_void_p), ("bias_id", C.c_void_p), ("bias_val", C.c_void_p), ("n_bias", C.c_int32),
+                ("mask", C.c_void_p), ("mask_idx", C.c_void_p), ("n_masks", C.c_int32), ("mask_words", C.c_int32)]
+
+
 class _Budget(C.Structure):
     _fields_ = [("max_memory", C.c_int64), ("base_model_bytes", C.c_int64), ("head_bytes", C.c_int64),
                 ("layers", C.c_int32), ("n_kv", C.c_int32), ("head_dim", C.c_int32), ("vocab", C.c_int32),
@@ -116,6 +122,11 @@ def load():
         lib.specmemo_tree_attn_prefix.restype = C.c_int
         lib.specmemo_tree_attn_prefix_bytes.argtypes = [i32, PT, PK, PP, i32]
         lib.specmemo_tree_attn_prefix_bytes.restype = sz
+        lib.specmemo_logit_rules.argtypes = [i32, PT, i32, C.POINTER(_Rules), vp, vp, vp, vp]
+        lib.specmemo_token_counts.argtypes = [i32, i32, vp, vp, vp, vp, i32, vp]
+        lib.specmemo_count_accepted.argtypes = [PT, i32, vp, vp, vp, i32, vp, vp]
+        for f in ("specmemo_logit_rules", "specmemo_token_counts", "specmemo_count_accepted"):
+            getattr(lib, f).restype = C.c_int
         lib.specmemo_mem_kv_bytes.argtypes = [i32, i32, i32, i32, i64, i32]
         lib.specmemo_mem_buffer_bytes.argtypes = [i32, i32, i32, i32, i32, i32]
         lib.specmemo_mem_total_bytes.argtypes = [i64, i64, i32, i64, i64]
@@ -448,6 +459,52 @@ def tree_attn_prefix(dt: int, trees: Trees, kv: KVPool, prefix: Prefix, n_q: int
     ts, ks = trees.struct(), kv.struct()
     _check(load().specmemo_tree_attn_prefix(dt, C.byref(ts), C.byref(ks), _prefix_ref(prefix, trees.B), n_q, scale,
                                             _ptr(q), _ptr(out), _ptr(ws), ws_bytes, _stream(stream)))
+
+
+# ---- rules on logits ----------------------------------------------------------------
+
+class LogitRules:
+    """Device arrays of the penalties, biases and masks (include/specmemo.h, specmemo_rules); None leaves a rule out."""
+
+    def __init__(self, counts=None, repetition=None, presence=None, frequency=None):
+        self.counts, self.repetition, self.presence, self.frequency = counts, repetition, presence, frequency
+        self.bias_off = self.bias_id = self.bias_val = self.mask = self.mask_idx = None
+        self.n_bias = self.n_masks = self.mask_words = 0
+
+    def set_bias(self, off, ids, values):
+        """Sequence b's biases are entries off[b] .. off[b+1] - 1 of ids and values."""
+        if ids.numel() != values.numel():
+            raise ValueError(f"{ids.numel()} bias ids, {values.numel()} values")
+        self.bias_off, self.bias_id, self.bias_val, self.n_bias = off, ids, values, int(ids.numel())
+
+    def set_mask(self, mask, idx):
+        """mask: [masks][words] 32-bit words (bit v % 32 of word v / 32: token v is allowed); idx: mask of each node, -1 for none."""
+        self.mask, self.mask_idx = mask, idx
+        self.n_masks, self.mask_words = (int(s) for s in mask.shape)
+
+    def struct(self) -> _Rules:
+        return _Rules(_ptr(self.counts), _ptr(self.repetition), _ptr(self.presence), _ptr(self.frequency),
+                      _ptr(self.bias_off), _ptr(self.bias_id), _ptr(self.bias_val), self.n_bias, _ptr(self.mask),
+                      _ptr(self.mask_idx), self.n_masks, self.mask_words)
+
+
+def logit_rules(dt: int, trees: Trees, vocab: int, logits, node_tok, rules: LogitRules, out, stream=None):
+    ts, rs = trees.struct(), rules.struct()
+    _check(load().specmemo_logit_rules(dt, C.byref(ts), vocab, C.byref(rs), _ptr(node_tok), _ptr(logits), _ptr(out),
+                                       _stream(stream)))
+
+
+def token_counts(vocab: int, tok_off_h, tok_off, tokens, counts, accumulate: bool = False, stream=None):
+    """tok_off_h: host offsets [B+1]; tok_off: the same on the device."""
+    off = _i32(tok_off_h)
+    _check(load().specmemo_token_counts(len(off) - 1, vocab, _host_addr(off), _ptr(tok_off), _ptr(tokens), _ptr(counts),
+                                        int(accumulate), _stream(stream)))
+
+
+def count_accepted(trees: Trees, vocab: int, node_tok, accept_len, path, path_stride: int, counts, stream=None):
+    ts = trees.struct()
+    _check(load().specmemo_count_accepted(C.byref(ts), vocab, _ptr(node_tok), _ptr(accept_len), _ptr(path), path_stride,
+                                          _ptr(counts), _stream(stream)))
 
 
 # ---- memory budget and tree construction (host) ------------------------------

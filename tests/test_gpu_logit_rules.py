@@ -1,0 +1,231 @@
+"""GPU: penalties, biases and masks on the tree's logits, and the token counts, against numpy in 64 bits."""
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2506_01986_amd import specmemo as sm
+from paper_2506_01986_amd import synth
+
+pytestmark = pytest.mark.gpu
+
+
+class Case:
+    def __init__(self, dtype, vocab, trees, seed=0, hist=40, bias=0, masks=0, penalties=("repetition", "presence", "frequency")):
+        r = np.random.default_rng(seed)
+        self.dtype, self.vocab, self.ts, self.B = dtype, vocab, trees, len(trees)
+        self.dt = sm.FP32 if dtype == "fp32" else sm.BF16
+        self.off = np.concatenate([[0], np.cumsum([t.n for t in trees])]).astype(np.int32)
+        self.par, dep, rank = (np.concatenate([getattr(t, f) for t in trees]) for f in ("parent", "depth", "rank"))
+        self.trees = sm.Trees(self.off, self.par, dep, rank, device="cuda")
+        n = int(self.off[-1])
+        self.z = torch.from_numpy(r.normal(0, 2, (n, vocab)).astype(np.float32)).to(torch.float32 if dtype == "fp32" else torch.bfloat16)
+        self.tok = r.integers(0, vocab, n).astype(np.int32)
+        lens = r.integers(0, hist + 1, self.B)
+        self.hist_off = np.concatenate([[0], np.cumsum(lens)]).astype(np.int32)
+        self.hist = (vocab * r.random(int(lens.sum())) ** 2).astype(np.int32)
+        self.counts = np.stack([np.bincount(self.hist[a:e], minlength=vocab) for a, e in zip(self.hist_off, self.hist_off[1:])]).astype(np.int32)
+        self.pen = {p: r.uniform(*lim, self.B).astype(np.float32) for p, lim in
+                    (("repetition", (0.7, 1.6)), ("presence", (-0.5, 1)), ("frequency", (-0.2, 0.5))) if p in penalties}
+        nb = r.integers(0, bias + 1, self.B)
+        self.bias_off = np.concatenate([[0], np.cumsum(nb)]).astype(np.int32)
+        # ids repeat, and some lie outside the vocabulary
+        self.bias_id = r.integers(-2, vocab + 2, int(nb.sum())).astype(np.int32)
+        self.bias_val = r.uniform(-4, 4, int(nb.sum())).astype(np.float32)
+        words = (vocab + 31) // 32 + 1
+        self.allowed = r.random((masks, words * 32)) < np.linspace(0, 1, masks)[:, None] if masks else np.zeros((0, words * 32), bool)
+        self.mask_idx = r.integers(-1, masks + 1, n).astype(np.int32)          # -1 and `masks`: unrestricted
+
+    def rules(self):
+        dev = lambda a: torch.from_numpy(np.ascontiguousarray(a)).cuda()
+        rules = sm.LogitRules(counts=dev(self.counts), **{p: dev(v) for p, v in self.pen.items()})
+        if len(self.bias_id):
+            rules.set_bias(dev(self.bias_off), dev(self.bias_id), dev(self.bias_val))
+        if len(self.allowed):
+            rules.set_mask(dev(np.packbits(self.allowed, axis=1, bitorder="little").view("<i4").reshape(len(self.allowed), -1)), dev(self.mask_idx))
+        return rules
+
+    def run(self, out=None, z=None):
+        zd = self.z.cuda() if z is None else z
+        out = torch.full_like(zd, 99.0) if out is None else out
+        sm.logit_rules(self.dt, self.trees, self.vocab, zd, torch.from_numpy(self.tok).cuda(), self.rules(), out)
+        torch.cuda.synchronize()
+        return out
+
+    def reference(self):
+        """(result, tolerance): the steps in fp32 round at most five times at the size of their largest term, the
+        result once in its type."""
+        x = self.z.double().numpy().copy()
+        size = np.abs(x)
+        for b in range(self.B):
+            rep, pres, freq = (float(self.pen[p][b]) if p in self.pen else d for p, d in
+                               (("repetition", 1.0), ("presence", 0.0), ("frequency", 0.0)))
+            bias = np.zeros(self.vocab)
+            for j in range(self.bias_off[b], self.bias_off[b + 1]):
+                if 0 <= self.bias_id[j] < self.vocab:
+                    bias[self.bias_id[j]] = self.bias_val[j]
+            for u in range(self.ts[b].n):
+                row = int(self.off[b]) + u
+                if self.pen:
+                    c = self.counts[b].astype(np.float64)
+                    a = u
+                    while a >= 0:
+                        c[self.tok[int(self.off[b]) + a]] += 1
+                        a = int(self.par[int(self.off[b]) + a])
+                    y = x[row]
+                    scaled = np.where(y > 0, y / rep, y * rep)
+                    size[row] = np.where(c > 0, np.abs(scaled) + abs(pres) + abs(freq) * c, size[row])
+                    x[row] = np.where(c > 0, scaled - freq * c - pres, y)
+                x[row] += bias
+                size[row] += np.abs(bias)
+                if 0 <= self.mask_idx[row] < len(self.allowed):
+                    x[row] = np.where(self.allowed[self.mask_idx[row], :self.vocab], x[row], -np.inf)
+        half = 2.0 ** -24 if self.dtype == "fp32" else 2.0 ** -8
+        with np.errstate(invalid="ignore"):
+            return x, 5 * 2.0 ** -24 * size + half * np.abs(x)
+
+    def check(self, out):
+        ref, tol = self.reference()
+        got = out.double().cpu().numpy()
+        hidden = np.isneginf(ref)
+        assert np.array_equal(np.isneginf(got), hidden)
+        err = np.abs(np.where(hidden, 0, got) - np.where(hidden, 0, ref))
+        bad = ~(err <= np.where(hidden, 0, tol))
+        assert not bad.any(), (int(bad.sum()), np.argwhere(bad)[:4].tolist(), float(err.max()))
+
+
+def trees(kind, seed=0):
+    r = np.random.default_rng(seed)
+    return {"single": [synth.chain_tree(1)], "t64x2": [synth.t64()] * 2, "chain": [synth.chain_tree(16)] * 3,
+            "random": [synth.random_tree(r, int(n)) for n in (128, 1, 17, 40)]}[kind]
+
+
+# both types, vocabularies on and off the 16-byte grid, on both sides of a block's segment (2048 bf16, 1024 fp32)
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("vocab", [1, 3, 7, 8, 50, 1000, 1023, 1024, 1029, 2047, 2048, 2055, 4099])
+@pytest.mark.parametrize("kind", ["single", "random"])
+def test_all_rules(dtype, vocab, kind):
+    x = Case(dtype, vocab, trees(kind, vocab), seed=vocab, bias=30, masks=5)
+    x.check(x.run())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_whole_vocabulary(dtype):
+    x = Case(dtype, 32000, trees("t64x2"), seed=2, hist=3000, bias=300, masks=7)
+    x.check(x.run())
+
+
+@pytest.mark.parametrize("use", ["none", "repetition", "presence", "frequency", "bias", "masks", "no_counts"])
+def test_single_rules(use):
+    x = Case("bf16", 777, trees("chain"), seed=5, bias=20 if use == "bias" else 0, masks=4 if use == "masks" else 0,
+             penalties=(use,) if use in ("repetition", "presence", "frequency") else ("repetition",) if use == "no_counts" else ())
+    if use == "no_counts":
+        x.counts[:] = 0
+        rules = x.rules()
+        rules.counts = None
+        out = torch.empty_like(x.z.cuda())
+        sm.logit_rules(x.dt, x.trees, x.vocab, x.z.cuda(), torch.from_numpy(x.tok).cuda(), rules, out)
+        x.check(out)
+        return
+    out = x.run()
+    x.check(out)
+    if use == "none":
+        assert torch.equal(out.cpu().view(torch.int16), x.z.view(torch.int16))
+
+
+def test_same_token_along_a_path():
+    """A chain whose nodes all carry one token: its count grows by one a level."""
+    x = Case("fp32", 64, [synth.chain_tree(16)], seed=6)
+    x.tok[:] = 5
+    x.check(x.run())
+
+
+def test_tokens_outside_the_vocabulary():
+    x = Case("fp32", 64, [synth.chain_tree(4)], seed=7)
+    good = x.run().clone()
+    tok = x.tok.copy()
+    x.tok[1] = -1
+    bad = x.run()
+    assert torch.equal(bad[0], good[0])
+    x.tok[1] = 64
+    assert torch.equal(x.run(), bad)
+    x.tok = tok
+
+
+@pytest.mark.parametrize("vocab", [1000, 1003])
+def test_in_place(vocab):
+    x = Case("bf16", vocab, trees("random"), seed=8, bias=20, masks=3)
+    want = x.run()
+    z = x.z.cuda()
+    assert torch.equal(x.run(out=z, z=z).view(torch.int16), want.view(torch.int16))
+
+
+def test_infinities_and_nan_pass_through():
+    x = Case("bf16", 200, [synth.chain_tree(2)], seed=9, masks=2)
+    x.mask_idx[:] = [-1, 0]               # row 1: nothing allowed
+    x.pen = {}
+    x.z[0, 3], x.z[0, 4], x.z[1, 3] = float("inf"), float("nan"), float("nan")
+    out = x.run().cpu()
+    assert torch.isneginf(out[1]).all()
+    assert out[0, 3] == float("inf") and torch.isnan(out[0, 4])
+    keep = torch.ones(200, dtype=torch.bool)
+    keep[4] = False
+    assert torch.equal(out[0][keep], x.z[0][keep])
+
+
+@pytest.mark.parametrize("vocab", [1, 5, 4096, 4097, 32000])
+@pytest.mark.parametrize("lens", [[0], [1], [5, 0, 3000], [16384, 1, 700, 0, 4095]])
+def test_counts(vocab, lens):
+    r = np.random.default_rng(vocab + len(lens))
+    off = np.concatenate([[0], np.cumsum(lens)]).astype(np.int32)
+    tok = r.integers(-3, vocab + 3, int(off[-1])).astype(np.int32)
+    tok[: len(tok) // 2] = min(2, vocab - 1)                         # one token again and again
+    want = np.stack([np.bincount(t[(t >= 0) & (t < vocab)], minlength=vocab) for t in np.split(tok, off[1:-1])])
+    counts = torch.full((len(lens), vocab), 9, dtype=torch.int32, device="cuda")
+    args = off, torch.from_numpy(off).cuda(), torch.from_numpy(tok).cuda(), counts
+    sm.token_counts(vocab, *args)
+    assert np.array_equal(counts.cpu().numpy(), want)
+    sm.token_counts(vocab, *args, accumulate=True)
+    assert np.array_equal(counts.cpu().numpy(), 2 * want)
+
+
+def test_count_accepted():
+    ts = [synth.t16(), synth.chain_tree(16), synth.chain_tree(1), synth.t16(), synth.t16()]
+    x = Case("fp32", 40, ts, seed=3)
+    acc = torch.tensor([2, 15, 0, 1, 3], dtype=torch.int32)
+    path = torch.full((5, 16), -1, dtype=torch.int32)
+    path[0, :3] = torch.tensor([0, 1, 5])
+    path[1] = torch.arange(16)
+    path[2, 0] = 0
+    path[3, :2] = torch.tensor([0, 16])                              # past the tree: adds nothing
+    path[4, :4] = torch.tensor([0, 3, 2, 9])                         # not increasing
+    x.tok[17:20] = 7                                                 # the same token three times on a path
+    want = x.counts.copy()
+    for b in range(3):
+        for j in range(int(acc[b]) + 1):
+            want[b, x.tok[int(x.off[b]) + int(path[b, j])]] += 1
+    counts = torch.from_numpy(x.counts).cuda()
+    sm.count_accepted(x.trees, 40, torch.from_numpy(x.tok).cuda(), acc.cuda(), path.cuda(), 16, counts)
+    assert np.array_equal(counts.cpu().numpy(), want)
+
+
+def test_captured():
+    x = Case("bf16", 1003, trees("random"), seed=4, bias=20, masks=3)
+    want = x.run()
+    z, tok, rules = x.z.cuda(), torch.from_numpy(x.tok).cuda(), x.rules()
+    counts = rules.counts.clone()
+    off, hist = torch.from_numpy(x.hist_off).cuda(), torch.from_numpy(x.hist).cuda()
+    out = torch.empty_like(z)
+    s = torch.cuda.Stream()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(s):
+        with torch.cuda.graph(g, stream=s):
+            sm.token_counts(x.vocab, x.hist_off, off, hist, rules.counts)
+            sm.logit_rules(x.dt, x.trees, x.vocab, z, tok, rules, out)
+        for i in range(3):
+            out.zero_()
+            rules.counts.fill_(100)
+            g.replay()
+            s.synchronize()
+            assert torch.equal(out.view(torch.int16), want.view(torch.int16)), i
+            assert torch.equal(rules.counts, counts)

@@ -111,3 +111,48 @@ def test_null_host_arrays():
     assert lib.specmemo_prompt_attn(1, 1, None, C.byref(kv), None, 4, 0.0, FAKE, FAKE, FAKE, 1 << 30, None) == -1
     assert lib.specmemo_prompt_attn(1, 1, off.ctypes.data, None, None, 4, 0.0, FAKE, FAKE, FAKE, 1 << 30, None) == -1
     assert lib.specmemo_prompt_attn(1, 1, off.ctypes.data, C.byref(kv), C.byref(px), 4, 0.0, FAKE, FAKE, FAKE, 1 << 30, None) == -1
+
+
+@cpu_only
+def test_rules():
+    t = FakeTrees([synth.t16(), synth.t16()])
+
+    def call(rules=None, trees=t, vocab=1000, dt=sm.BF16, z=FAKE, out=FAKE * 2, tok=FAKE):
+        sm.logit_rules(dt, trees, vocab, z, tok, rules or sm.LogitRules(repetition=FAKE), out, stream=0)
+
+    class Rules(sm.LogitRules):
+        def __init__(self, **k):
+            super().__init__()
+            self.__dict__.update(k)
+
+    expect("E_DTYPE", call, dt=9)
+    expect("E_ARG", call, vocab=0)
+    expect("E_ARG", call, vocab=(1 << 30) + 1)
+    expect("E_ARG", call, z=None)
+    expect("E_ARG", call, out=FAKE + 8)
+    assert "overlap" in expect("E_ARG", call, out=FAKE + 64)
+    expect("E_ARG", call, tok=None)
+    expect("E_ARG", call, rules=Rules(counts=FAKE + 2))
+    expect("E_ARG", call, rules=Rules(frequency=FAKE + 1))
+    expect("E_ARG", call, rules=Rules(n_bias=3, bias_off=FAKE, bias_id=FAKE))
+    expect("E_ARG", call, rules=Rules(n_bias=-1))
+    expect("E_ARG", call, rules=Rules(n_masks=2, mask=FAKE, mask_idx=FAKE, mask_words=31))      # 32 needed
+    expect("E_ARG", call, rules=Rules(n_masks=2, mask=FAKE, mask_words=32))
+    bad = synth.t16()
+    bad.parent[5] = 7
+    expect("E_TREE", call, trees=FakeTrees([bad]))
+
+
+@cpu_only
+def test_counts():
+    call = lambda off, vocab=10, dev=FAKE, tok=FAKE, counts=FAKE: sm.token_counts(vocab, off, dev, tok, counts, stream=0)
+    expect("E_ARG", call, [0])
+    expect("E_ARG", call, [1, 2])
+    expect("E_ARG", call, [0, 3, 2])
+    expect("E_ARG", call, [0, 3], vocab=0)
+    expect("E_ARG", call, [0, 3], dev=None)
+    expect("E_ARG", call, [0, 3], tok=None)
+    expect("E_ARG", call, [0, 3], counts=FAKE + 2)
+    t = FakeTrees([synth.t16()])
+    expect("E_ARG", sm.count_accepted, t, 10, FAKE, FAKE, None, 4, FAKE, stream=0)
+    expect("E_ARG", sm.count_accepted, t, 10, FAKE, FAKE, FAKE, 0, FAKE, stream=0)
