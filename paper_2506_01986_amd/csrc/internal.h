@@ -250,7 +250,7 @@ struct RulesArgs {
   const int32_t *mask_idx;
   int32_t n_bias, n_masks, mask_words, vocab;
   int32_t penalties;         // any of the three is given
-  int32_t groups;            // row groups of the largest tree
+  int32_t rows, groups;      // node rows a block, row groups of the largest tree
 };
 hipError_t launch_logit_rules(int dt, const RulesArgs &a, int B, int max_nodes, hipStream_t st);
 struct CountArgs {

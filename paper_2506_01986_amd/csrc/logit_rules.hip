@@ -19,8 +19,8 @@ namespace specmemo {
 namespace {
 
 constexpr int kNT = 256;          // threads of a rules block
-constexpr int kRows = 16;         // node rows a block works through
-constexpr int kInFlight = 4;      // rows whose loads are in flight at once
+static_assert(kNT >= kMaxNodes, "one thread per tree node");
+constexpr int kRows = 8;          // most node rows of a block, all their loads in flight at once
 
 // Chunks of 16 bytes at 16-byte aligned addresses; a row whose length keeps it from
 // starting or ending on one has up to 2 (V - 1) single values, before and after.
@@ -40,135 +40,211 @@ struct Chunk {
   }
 };
 
-// One block: kRows rows of a sequence, one segment of kNT chunks of the vocabulary.
-// The segment's counts and biases are read once for all the rows and kept in LDS
-// (element e of chunk i at e * kStride + i: any alignment of the rows reads them
-// without bank conflicts).
+// One block: up to kRows rows of a sequence, one segment of kNT chunks of the
+// vocabulary.  The rows' loads go first; while they are on their way the segment's
+// counts and biases are put into LDS, once for all the rows (element e of chunk i
+// at e * kStride + i: any alignment of the rows reads them without bank conflicts).
 template <int DT>
 __global__ __launch_bounds__(kNT) void logit_rules_kernel(RulesArgs a) {
   constexpr int V = Chunk<DT>::V, SEG = kNT * V, COLS = SEG + V, kStride = kNT + 2;
   __shared__ int s_cnt[V * kStride];
-  __shared__ int s_bias[V * kStride];              // index + 1 of the token's last bias entry, then its value
+  __shared__ int s_bias[V * kStride];              // index + 1 of the token's last bias entry
+  __shared__ float s_val[V * kStride];             // its value
   __shared__ uint8_t s_any[kNT + 1];               // chunk-sized groups with a count or a bias
   __shared__ int s_par[kMaxNodes], s_loc[kMaxNodes], s_hit[kMaxNodes], s_after[kMaxNodes];
   const int tid = threadIdx.x;
-  const int b = blockIdx.y / a.groups, r0 = blockIdx.y % a.groups * kRows;
+  const int b = blockIdx.y / a.groups, r0 = blockIdx.y % a.groups * a.rows;
   const int n0 = a.node_off[b], N = a.node_off[b + 1] - n0;
   if (r0 >= N) return;
-  const int col0 = blockIdx.x * SEG;
-  auto at = [&](int c) { return c % V * kStride + c / V; };   // column of the segment -> LDS
-
-  for (int c = tid; c < V * kStride; c += kNT) s_bias[c] = 0;
-  for (int c = tid; c < COLS; c += kNT)
-    s_cnt[at(c)] = a.counts && col0 + c < a.vocab ? a.counts[(int64_t)b * a.vocab + col0 + c] : 0;
-  if (a.penalties)
-    for (int n = tid; n < N; n += kNT) {
-      const int t = a.node_tok[n0 + n];
-      s_par[n] = n == 0 ? -1 : a.parent[n0 + n];
-      s_loc[n] = t >= col0 && t < min(col0 + COLS, a.vocab) ? t - col0 : -1;
-    }
-  __syncthreads();
-  // Nearest node at or above n, and strictly above it, whose token lies in the segment.
-  if (a.penalties)
-    for (int n = tid; n < N; n += kNT) {
-      int u = s_par[n];
-      while (u >= 0 && s_loc[u] < 0) u = s_par[u];
-      s_after[n] = u;
-      s_hit[n] = s_loc[n] >= 0 ? n : u;
-    }
-  if (a.n_bias > 0) {
-    const int j1 = min(max(a.bias_off[b + 1], 0), a.n_bias);
-    for (int j = max(a.bias_off[b], 0) + tid; j < j1; j += kNT) {
-      const int c = a.bias_id[j] - col0;
-      if (a.bias_id[j] >= 0 && c >= 0 && c < COLS) atomicMax(&s_bias[at(c)], j + 1);   // the last entry of an id counts
-    }
-    __syncthreads();
-    for (int c = tid; c < V * kStride; c += kNT) s_bias[c] = s_bias[c] ? __float_as_int(a.bias_val[s_bias[c] - 1]) : 0;
-  }
-  __syncthreads();
-  for (int i = tid; i <= kNT; i += kNT) {
-    int any = 0;
-#pragma unroll
-    for (int e = 0; e < V; ++e) any |= (a.penalties ? s_cnt[e * kStride + i] : 0) | s_bias[e * kStride + i];
-    s_any[i] = any != 0;
-  }
-  __syncthreads();
-
+  const int nrow = min(a.rows, N - r0);
   const float rep = a.repetition ? a.repetition[b] : 1.f, inv_rep = 1.f / rep;
   const float pres = a.presence ? a.presence[b] : 0.f, freq = a.frequency ? a.frequency[b] : 0.f;
+  const int j0 = a.n_bias > 0 ? max(a.bias_off[b], 0) : 0, j1 = a.n_bias > 0 ? min(a.bias_off[b + 1], a.n_bias) : 0;
+  const int col0 = blockIdx.x * SEG, chunk = blockIdx.x * kNT + tid;
+  auto at = [&](int c) { return c % V * kStride + c / V; };   // column of the segment -> LDS
+  auto row_at = [&](int f) { return (int64_t)(n0 + r0 + f) * a.vocab; };
+  auto row_head = [&](int f) { return min((int)(-row_at(f) & (V - 1)), a.vocab); };   // values before the first chunk
+  auto row_mask = [&](int f) {
+    const int m = a.mask ? a.mask_idx[n0 + r0 + f] : -1;
+    return m < a.n_masks ? m : -1;
+  };
+
+  // What the segment's tables are made of, before the rows: loads return in order,
+  // and the tables are built while the rows are on their way.
+  int cnt[V], cnt_last = 0;           // counts of chunk tid's columns; of column SEG + tid, past the last chunk
+#pragma unroll
+  for (int e = 0; e < V; ++e) cnt[e] = 0;
+  if (a.counts) {
+    const int *c = a.counts + (int64_t)b * a.vocab + col0;
+    if (((uintptr_t)c & 15) == 0 && chunk * V + V <= a.vocab) {
+#pragma unroll
+      for (int e = 0; e < V; e += 4) *reinterpret_cast<int4 *>(cnt + e) = *reinterpret_cast<const int4 *>(c + V * tid + e);
+    } else {
+#pragma unroll
+      for (int e = 0; e < V; ++e)
+        if (chunk * V + e < a.vocab) cnt[e] = c[V * tid + e];
+    }
+    if (tid < V && col0 + SEG + tid < a.vocab) cnt_last = c[SEG + tid];
+  }
+  int tok = -1, par = -1;
+  if (a.penalties && tid < N) {
+    tok = a.node_tok[n0 + tid];
+    par = a.parent[n0 + tid];         // -1 at the root
+  }
+  // a bias entry's token as a column of the segment, or -1
+  auto bias_col = [&](int j) {
+    const int v = a.bias_id[j];
+    return v >= 0 && v >= col0 && v - col0 < COLS ? v - col0 : -1;
+  };
+  const int my_col = j0 + tid < j1 ? bias_col(j0 + tid) : -1;   // the first entry of each thread, read with its value
+  const float my_val = j0 + tid < j1 ? a.bias_val[j0 + tid] : 0.f;
+
+  uint4 w[kRows];
+  uint32_t bits[kRows];               // bit e: the chunk's column e is allowed
+#pragma unroll
+  for (int f = 0; f < kRows; ++f) {
+    bits[f] = ~0u;
+    if (f < nrow) {
+      const int head = row_head(f), m = row_mask(f);
+      if (chunk < (a.vocab - head) / V) {
+        w[f] = *reinterpret_cast<const uint4 *>(static_cast<const uint8_t *>(a.logits) + (row_at(f) + head + (int64_t)V * chunk) * (16 / V));
+        if (m >= 0) {
+          const uint32_t *mw = a.mask + (int64_t)m * a.mask_words;
+          const int col = head + V * chunk, i = col >> 5;
+          bits[f] = (uint32_t)(((uint64_t)mw[min(i + 1, a.mask_words - 1)] << 32 | mw[i]) >> (col & 31));
+        }
+      }
+    }
+  }
+  {
+    int any = 0;
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      any |= cnt[e];
+      s_cnt[e * kStride + tid] = cnt[e];
+      s_bias[e * kStride + tid] = 0;
+      s_val[e * kStride + tid] = 0.f;
+    }
+    s_any[tid] = any != 0;
+    const uint64_t last = __builtin_amdgcn_ballot_w64(tid < V && cnt_last != 0);
+    if (tid < V) {
+      s_cnt[tid * kStride + kNT] = cnt_last;
+      s_bias[tid * kStride + kNT] = 0;
+      s_val[tid * kStride + kNT] = 0.f;
+    }
+    if (tid == 0) s_any[kNT] = last != 0;
+  }
+  if (tid < N) {
+    s_par[tid] = par;
+    s_loc[tid] = tok >= col0 && tok < min(col0 + COLS, a.vocab) ? tok - col0 : -1;
+  }
+  __syncthreads();
+  // Nearest node at or above n, and strictly above it, whose token lies in the segment.
+  if (a.penalties && tid < N) {
+    int u = par;
+    while (u >= 0 && s_loc[u] < 0) u = s_par[u];
+    s_after[tid] = u;
+    s_hit[tid] = s_loc[tid] >= 0 ? tid : u;
+  }
+  if (j0 < j1) {                      // of equal ids the last entry counts
+    if (my_col >= 0) atomicMax(&s_bias[at(my_col)], j0 + tid + 1);
+    for (int j = j0 + kNT + tid; j < j1; j += kNT) {
+      const int c = bias_col(j);
+      if (c >= 0) atomicMax(&s_bias[at(c)], j + 1);
+    }
+    __syncthreads();
+    const bool mine = my_col >= 0 && s_bias[at(my_col)] == j0 + tid + 1;
+    for (int j = j0 + kNT + tid; j < j1; j += kNT) {
+      const int c = bias_col(j);
+      if (c >= 0 && s_bias[at(c)] == j + 1) {
+        s_val[at(c)] = a.bias_val[j];
+        s_any[c / V] = 1;
+      }
+    }
+    if (mine) {
+      s_val[at(my_col)] = my_val;
+      s_any[my_col / V] = 1;
+    }
+  }
+  __syncthreads();
+
   // (x / repetition as a product with its reciprocal: one rounding of 2^-24 more, far below the logits' own)
   auto apply = [&](float x, int c, float bias, bool allowed) {
     const float y = fmaf(-freq, (float)c, (x > 0.f ? x * inv_rep : x * rep) - pres);
     x = c > 0 ? y : x;
     return allowed ? x + bias : -INFINITY;
   };
-  auto mask_bits = [&](int m, int col) -> uint32_t {   // bit e: column col + e is allowed
-    const uint32_t *w = a.mask + (int64_t)m * a.mask_words;
-    const int i = col >> 5;
-    return (uint32_t)(((uint64_t)w[min(i + 1, a.mask_words - 1)] << 32 | w[i]) >> (col & 31));
-  };
-
-  const int r1 = min(N, r0 + kRows);
-  for (int rr = r0; rr < r1; rr += kInFlight) {
-    uint4 w[kInFlight];
-    uint32_t bits[kInFlight];
-    int head[kInFlight], nch[kInFlight], mi[kInFlight];
-    const int chunk = blockIdx.x * kNT + tid;
+  // What the rules do to this thread's columns in a row whose path adds no count:
+  // x times one of two factors, plus a term.  Kept from row to row while the rows
+  // begin at the same place of a chunk (every row where vocab is a multiple of V):
+  // four instructions a value instead of twenty, which bound the kernel (640 rows
+  // of 32000 bf16 values 30.1 us before).
+  float pos[V], neg[V], add[V];
+  int kept = -1;
+  bool touched = false;
 #pragma unroll
-    for (int f = 0; f < kInFlight; ++f) {
-      const int r = min(rr + f, r1 - 1);
-      const int64_t base = (int64_t)(n0 + r) * a.vocab;
-      head[f] = min((int)(-base & (V - 1)), a.vocab);
-      nch[f] = (a.vocab - head[f]) / V;
-      mi[f] = a.mask ? a.mask_idx[n0 + r] : -1;
-      if (mi[f] >= a.n_masks) mi[f] = -1;
-      if (chunk < nch[f]) {
-        w[f] = *reinterpret_cast<const uint4 *>(static_cast<const uint8_t *>(a.logits) + (base + head[f] + (int64_t)V * chunk) * (16 / V));
-        bits[f] = mi[f] >= 0 ? mask_bits(mi[f], head[f] + V * chunk) : ~0u;
+  for (int f = 0; f < kRows; ++f) {
+    if (f >= nrow) break;
+    const int head = row_head(f), nch = (a.vocab - head) / V;
+    const int first = a.penalties ? s_hit[r0 + f] : -1;
+    if (chunk < nch) {
+      const int l0 = head + V * tid;             // first column in the segment
+      float x[V];
+      if (kept != head) {
+        kept = head;
+        touched = s_any[tid] | (head ? s_any[tid + 1] : 0);
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          const int c = s_cnt[at(l0 + e)];
+          pos[e] = c > 0 ? inv_rep : 1.f;
+          neg[e] = c > 0 ? rep : 1.f;
+          add[e] = s_val[at(l0 + e)] - (c > 0 ? fmaf(freq, (float)c, pres) : 0.f);
+        }
       }
-    }
+      // tokens of this row's path among the thread's columns
+      uint32_t onpath = 0;
+      for (int u = first; u >= 0; u = s_after[u]) onpath |= (unsigned)(s_loc[u] - l0) < V ? 1u << (s_loc[u] - l0) : 0u;
+      const bool masked = (bits[f] & ((1u << V) - 1)) != (1u << V) - 1;
+      if (touched || masked || onpath) {
 #pragma unroll
-    for (int f = 0; f < kInFlight; ++f) {
-      if (rr + f >= r1) break;
-      const int r = rr + f;
-      const int64_t base = (int64_t)(n0 + r) * a.vocab;
-      const int first = a.penalties ? s_hit[r] : -1;
-      if (chunk < nch[f]) {
-        const int l0 = head[f] + V * tid;          // first column in the segment
-        const bool touched = s_any[tid] | (head[f] ? s_any[tid + 1] : 0);
-        if (touched || first >= 0 || (bits[f] & ((1u << V) - 1)) != (1u << V) - 1) {
-          int c[V];
-          float x[V];
-#pragma unroll
-          for (int e = 0; e < V; ++e) c[e] = s_cnt[at(l0 + e)];
-          for (int u = first; u >= 0; u = s_after[u])
-#pragma unroll
-            for (int e = 0; e < V; ++e) c[e] += s_loc[u] == l0 + e;
+        for (int e = 0; e < V; ++e) {
+          const float z = Chunk<DT>::get(w[f], e);
+          x[e] = fmaf(z, z > 0.f ? pos[e] : neg[e], add[e]);
+        }
+        if (onpath) {
 #pragma unroll
           for (int e = 0; e < V; ++e)
-            x[e] = apply(Chunk<DT>::get(w[f], e), a.penalties ? c[e] : 0, __int_as_float(s_bias[at(l0 + e)]), (bits[f] >> e) & 1u);
-          w[f] = Chunk<DT>::pack(x);
+            if ((onpath >> e) & 1u) {
+              int c = s_cnt[at(l0 + e)];
+              for (int u = first; u >= 0; u = s_after[u]) c += s_loc[u] == l0 + e;
+              x[e] = apply(Chunk<DT>::get(w[f], e), c, s_val[at(l0 + e)], true);
+            }
         }
-        *reinterpret_cast<uint4 *>(static_cast<uint8_t *>(a.out) + (base + head[f] + (int64_t)V * chunk) * (16 / V)) = w[f];
+        if (masked) {
+#pragma unroll
+          for (int e = 0; e < V; ++e) x[e] = (bits[f] >> e) & 1u ? x[e] : -INFINITY;
+        }
+        w[f] = Chunk<DT>::pack(x);
       }
-      // single values: those before the first chunk, those after the last
-      int col = -1;
-      if (blockIdx.x == 0 && tid < head[f]) col = tid;
-      else if ((int)blockIdx.x == nch[f] / kNT) {
-        const int t = tid - (blockIdx.x == 0 ? head[f] : 0);
-        if (t >= 0 && head[f] + V * nch[f] + t < a.vocab) col = head[f] + V * nch[f] + t;
-      }
-      if (col >= 0) {
-        const int l = col - col0;
-        int c = s_cnt[at(l)];
-        for (int u = first; u >= 0; u = s_after[u]) c += s_loc[u] == l;
-        const float z = DT == 0 ? static_cast<const float *>(a.logits)[base + col]
-                                : bf16_to_f32(static_cast<const uint16_t *>(a.logits)[base + col]);
-        const float y = apply(z, a.penalties ? c : 0, __int_as_float(s_bias[at(l)]),
-                              mi[f] < 0 || ((a.mask[(int64_t)mi[f] * a.mask_words + (col >> 5)] >> (col & 31)) & 1u));
-        if (DT == 0) static_cast<float *>(a.out)[base + col] = y;
-        else static_cast<uint16_t *>(a.out)[base + col] = (uint16_t)(pack_bf16x2(y, 0.f) & 0xFFFFu);
-      }
+      *reinterpret_cast<uint4 *>(static_cast<uint8_t *>(a.out) + (row_at(f) + head + (int64_t)V * chunk) * (16 / V)) = w[f];
+    }
+    // single values: those before the first chunk, those after the last
+    int col = -1;
+    if (blockIdx.x == 0 && tid < head) col = tid;
+    else if ((int)blockIdx.x == nch / kNT) {
+      const int t = tid - (blockIdx.x == 0 ? head : 0);
+      if (t >= 0 && head + V * nch + t < a.vocab) col = head + V * nch + t;
+    }
+    if (col >= 0) {
+      const int l = col - col0, m = row_mask(f);
+      int c = s_cnt[at(l)];
+      for (int u = first; u >= 0; u = s_after[u]) c += s_loc[u] == l;
+      const float z = DT == 0 ? static_cast<const float *>(a.logits)[row_at(f) + col]
+                              : bf16_to_f32(static_cast<const uint16_t *>(a.logits)[row_at(f) + col]);
+      const float y = apply(z, c, s_val[at(l)],
+                            m < 0 || ((a.mask[(int64_t)m * a.mask_words + (col >> 5)] >> (col & 31)) & 1u));
+      if (DT == 0) static_cast<float *>(a.out)[row_at(f) + col] = y;
+      else static_cast<uint16_t *>(a.out)[row_at(f) + col] = (uint16_t)(pack_bf16x2(y, 0.f) & 0xFFFFu);
     }
   }
 }
@@ -176,7 +252,7 @@ __global__ __launch_bounds__(kNT) void logit_rules_kernel(RulesArgs a) {
 // Counts of a sequence's tokens: one block per segment of the vocabulary, counted
 // in LDS (integers: the order of the additions does not matter) and written out
 // whole, so that the table needs no clearing.
-constexpr int kCountThreads = 512;
+constexpr int kCountThreads = 1024;
 constexpr int kCountSeg = 4096;
 
 __global__ __launch_bounds__(kCountThreads) void token_counts_kernel(CountArgs a) {
@@ -216,9 +292,12 @@ __global__ __launch_bounds__(64) void count_accepted_kernel(AcceptedArgs a) {
 
 hipError_t launch_logit_rules(int dt, const RulesArgs &args, int B, int max_nodes, hipStream_t st) {
   RulesArgs a = args;
-  a.groups = (max_nodes + kRows - 1) / kRows;
-  const int seg = kNT * (dt == 0 ? 4 : 8);
-  const dim3 grid((a.vocab + seg - 1) / seg, B * a.groups);
+  const int seg = kNT * (dt == 0 ? 4 : 8), segs = (a.vocab + seg - 1) / seg;
+  // fewer rows a block where the chip is not full: their work is the block's chain
+  a.rows = kRows;
+  while (a.rows > 1 && (int64_t)segs * B * ((max_nodes + a.rows - 1) / a.rows) < 2 * device_cus()) a.rows /= 2;
+  a.groups = (max_nodes + a.rows - 1) / a.rows;
+  const dim3 grid(segs, B * a.groups);
   if (dt == 0) hipLaunchKernelGGL(logit_rules_kernel<0>, grid, dim3(kNT), 0, st, a);
   else hipLaunchKernelGGL(logit_rules_kernel<1>, grid, dim3(kNT), 0, st, a);
   return hipGetLastError();
