@@ -829,7 +829,7 @@ WalkPlan make_walk(int dt, bool causal, const TreeInfo &ti, const int32_t *off_h
     seqs.push_back(s);
   }
   WalkPlan p;
-  plan_walk(dt, causal, seqs, kv->n_kv, n_q / kv->n_kv, device_cus(), &p);
+  plan_walk(dt, causal, seqs, kv->n_kv, n_q / kv->n_kv, kv->head_dim, device_cus(), &p);
   return p;
 }
 
@@ -838,7 +838,7 @@ size_t walk_table_bytes(const WalkPlan &p) {
 }
 size_t walk_ws_bytes(const WalkPlan &p, int head_dim) {
   return walk_table_bytes(p) +
-         (size_t)p.parts * (size_t)(p.rb / 32) * walk_unit_floats((head_dim + 31) / 32) * sizeof(float);
+         (size_t)p.parts * walk_unit_floats((head_dim + 31) / 32) * sizeof(float);
 }
 
 int run_walk(int dt, bool tree, const TreeInfo &ti, const int32_t *off_h, const int32_t *parent, const specmemo_kv *kv,
@@ -870,7 +870,6 @@ int run_walk(int dt, bool tree, const TreeInfo &ti, const int32_t *off_h, const 
   a.nset = (int)p.sets.size();
   a.slots = (int)p.slots;
   a.cslots = (int)p.cslots;
-  a.rb = p.rb;
   a.scale_log2 = scale * 1.4426950408889634f;
   hipStream_t st = static_cast<hipStream_t>(stream);
   uint8_t *w = static_cast<uint8_t *>(ws);

@@ -142,10 +142,11 @@ struct WalkSet {
   int64_t base, pbase;   // first pool row of the slab and of the prefix
   int32_t L, T, P;       // committed slab rows, nodes, prefix rows walked here
   int32_t row0;          // first node in q
+  int32_t rb;            // query rows of a row block
   int32_t nrb, ct, nch;  // row blocks, tiles per chunk, most chunks of a row block
   int32_t items;         // (row block, chunk) pairs of one KV head
   int32_t cum;           // item slots of an XCD before this set
-  int32_t part0;         // first partial slot, -1: every row block writes its output
+  int32_t part0;         // first 32-row unit of its parts, -1: every row block writes its output
   int32_t ccum, citems;  // slots of an XCD before this set and 32-row units of one KV head, of the merge
   int32_t cunit0;        // first unit that is merged
   int32_t shared;        // set that holds the prefix's parts of these rows, or -1
@@ -166,36 +167,35 @@ struct WalkArgs {
   int32_t n_q, n_kv, group, head_dim;
   int32_t units, fan;      // virtual units of a set on each XCD; shares of a KV head's items
   int32_t nset, slots, cslots;   // item and merge slots of one XCD
-  int32_t rb;              // query rows of a row block
   float scale_log2;        // scale * log2(e)
   WalkSet set[kMaxWalkSets];
 };
 static_assert(sizeof(WalkArgs) <= 4096, "kernel arguments are limited to 4 KB");
 
 // Slab keys that row block rb walks (a causal one stops at its last node).
-__host__ __device__ inline int walk_keys(const WalkSet &s, int rb, int RB, int g) {
+__host__ __device__ inline int walk_keys(const WalkSet &s, int rb, int g) {
   if (!s.slab) return 0;
   if (!s.causal) return s.L + s.T;
-  const int last = (rb * RB + RB - 1) / g + 1;
+  const int last = (rb * s.rb + s.rb - 1) / g + 1;
   return s.L + (last < s.T ? last : s.T);
 }
-__host__ __device__ inline int walk_tiles(const WalkSet &s, int rb, int RB, int g) {
-  return (s.P + kAttnKeyTile - 1) / kAttnKeyTile + (walk_keys(s, rb, RB, g) + kAttnKeyTile - 1) / kAttnKeyTile;
+__host__ __device__ inline int walk_tiles(const WalkSet &s, int rb, int g) {
+  return (s.P + kAttnKeyTile - 1) / kAttnKeyTile + (walk_keys(s, rb, g) + kAttnKeyTile - 1) / kAttnKeyTile;
 }
-__host__ __device__ inline int walk_chunks(const WalkSet &s, int rb, int RB, int g) {
-  return (walk_tiles(s, rb, RB, g) + s.ct - 1) / s.ct;
+__host__ __device__ inline int walk_chunks(const WalkSet &s, int rb, int g) {
+  return (walk_tiles(s, rb, g) + s.ct - 1) / s.ct;
 }
 // First row block of a causal set that reaches chunk c: its last node's key lies
 // past the chunk's first one.
-__host__ __device__ inline int walk_first_rb(const WalkSet &s, int c, int RB, int g) {
+__host__ __device__ inline int walk_first_rb(const WalkSet &s, int c, int g) {
   const int np = (s.P + kAttnKeyTile - 1) / kAttnKeyTile;
   const int x = (c * s.ct - np) * kAttnKeyTile - s.L;   // nodes that end before the chunk
   if (x <= 0) return 0;
-  return x >= s.T ? s.nrb : (int)((int64_t)x * g / RB);
+  return x >= s.T ? s.nrb : (int)((int64_t)x * g / s.rb);
 }
 // Whether the row block writes its output itself.
-__host__ __device__ inline bool walk_direct(const WalkSet &s, int rb, int RB, int g) {
-  return !s.parts && (s.part0 < 0 || walk_chunks(s, rb, RB, g) == 1);
+__host__ __device__ inline bool walk_direct(const WalkSet &s, int rb, int g) {
+  return !s.parts && (s.part0 < 0 || walk_chunks(s, rb, g) == 1);
 }
 // 4-byte words of a part of 32 rows: O in fp32, m and l
 __host__ __device__ constexpr int walk_unit_floats(int dblocks) { return 32 * 32 * dblocks + 64; }
@@ -207,11 +207,13 @@ struct WalkSeq {
   int32_t L, T, P, row0;
 };
 struct WalkPlan {
-  int rb = 0, fan = 1, units = 1;
-  int64_t slots = 0, cslots = 0, parts = 0;   // of one XCD; partial slots (row blocks)
+  int fan = 1, units = 1;
+  int64_t slots = 0, cslots = 0;   // of one XCD
+  int64_t parts = 0;               // 32-row units
   std::vector<WalkSet> sets;
 };
-void plan_walk(int dt, bool causal, const std::vector<WalkSeq> &seqs, int n_kv, int group, int cus, WalkPlan *p);
+void plan_walk(int dt, bool causal, const std::vector<WalkSeq> &seqs, int n_kv, int group, int head_dim, int cus,
+               WalkPlan *p);
 
 // ---- acceptance ------------------------------------------------------------------
 struct AcceptArgs {

@@ -40,22 +40,24 @@ struct WalkItem {
   int kvh, rb, ch;
 };
 
-// The sets of the launch: in the kernel arguments, or where those do not hold them
-// in the workspace.  (The arguments are read where they lie: a pointer chosen
-// between the two would make the compiler copy all of them to scratch memory.)
-__device__ __forceinline__ const WalkSet *walk_sets(const WalkArgs &a) {
-  const auto *args = reinterpret_cast<const WalkArgs *>((uintptr_t)__builtin_amdgcn_kernarg_segment_ptr());
-  return a.tab ? a.tab : args->set;
-}
+// The kernel arguments where they lie, read by scalar loads (an array of the
+// arguments indexed through a pointer that may also point elsewhere would be copied
+// to scratch memory as a whole).
+typedef __attribute__((address_space(4))) const WalkArgs KernArgs;
+__device__ __forceinline__ KernArgs *kern_args() { return (KernArgs *)__builtin_amdgcn_kernarg_segment_ptr(); }
 
 // The set whose slots hold position k: the last one with first slot <= k.
 template <bool COMBINE>
-__device__ __forceinline__ int find_set(const WalkArgs &a, const WalkSet *sets, int k) {
+__device__ __forceinline__ int find_set(const WalkArgs &a, int k) {
   const int lane = threadIdx.x & 63;
   int lo = 0, cnt = a.nset;
   while (cnt > 1) {   // 64 ways a round: two rounds for up to 4096 sets
     const int st = (cnt + 63) >> 6, at = lane * st;
-    const int first = at < cnt ? (COMBINE ? sets[lo + at].ccum : sets[lo + at].cum) : 0;
+    int first = 0;
+    if (at < cnt) {
+      if (a.tab) first = COMBINE ? a.tab[lo + at].ccum : a.tab[lo + at].cum;
+      else first = COMBINE ? a.set[lo + at].ccum : a.set[lo + at].cum;
+    }
     const int p = __builtin_popcountll(__builtin_amdgcn_ballot_w64(at < cnt && first <= k)) - 1;
     lo += p * st;
     cnt = min(st, cnt - p * st);
@@ -63,14 +65,22 @@ __device__ __forceinline__ int find_set(const WalkArgs &a, const WalkSet *sets, 
   return lo;
 }
 
-// Set s, one word a lane and then in SGPRs (the direct loads need their base there).
-__device__ __forceinline__ WalkSet get_set(const WalkSet *sets, int s) {
+// Set s, in SGPRs (the direct loads need their base there): from the arguments by
+// scalar loads, from the workspace table one word a lane.
+__device__ __forceinline__ WalkSet get_set(const WalkArgs &a, int s) {
   constexpr int N = sizeof(WalkSet) / 4;
   static_assert(sizeof(WalkSet) % 4 == 0 && N <= 64, "copied by words");
-  const int v = reinterpret_cast<const int *>(sets + s)[min((int)(threadIdx.x & 63), N - 1)];
+  s = __builtin_amdgcn_readfirstlane(s);
   int w[N];
+  if (a.tab) {
+    const int v = reinterpret_cast<const int *>(a.tab + s)[min((int)(threadIdx.x & 63), N - 1)];
 #pragma unroll
-  for (int i = 0; i < N; ++i) w[i] = __builtin_amdgcn_readlane(v, i);
+    for (int i = 0; i < N; ++i) w[i] = __builtin_amdgcn_readlane(v, i);
+  } else {
+    const auto *p = (__attribute__((address_space(4))) const int *)&kern_args()->set[s];
+#pragma unroll
+    for (int i = 0; i < N; ++i) w[i] = p[i];
+  }
   WalkSet S;
   __builtin_memcpy(&S, w, sizeof(S));
   return S;
@@ -84,8 +94,7 @@ __device__ __forceinline__ WalkSet get_set(const WalkSet *sets, int s) {
 template <bool COMBINE>
 __device__ __forceinline__ bool decode_unit(const WalkArgs &a, int bid, WalkSet &S, int &kvh, int &i) {
   const int x = bid & 7, k = bid >> 3;
-  const WalkSet *sets = walk_sets(a);
-  S = get_set(sets, find_set<COMBINE>(a, sets, k));
+  S = get_set(a, find_set<COMBINE>(a, k));
   const int kk = k - (COMBINE ? S.ccum : S.cum);
   const int u = x + 8 * (kk % a.units);
   kvh = u % a.n_kv;
@@ -93,7 +102,6 @@ __device__ __forceinline__ bool decode_unit(const WalkArgs &a, int bid, WalkSet 
   return i < (COMBINE ? S.citems : S.items);
 }
 
-template <int RB>
 __device__ __forceinline__ bool decode_walk(const WalkArgs &a, int bid, WalkItem &it) {
   int i;
   if (!decode_unit<false>(a, bid, it.S, it.kvh, i)) return false;
@@ -106,7 +114,7 @@ __device__ __forceinline__ bool decode_walk(const WalkArgs &a, int bid, WalkItem
     it.rb = i % S.nrb;
   } else {                       // chunk by chunk, the row blocks that reach it: at most 64 chunks, one a lane
     const int lane = threadIdx.x & 63;
-    const int r0 = lane < S.nch ? walk_first_rb(S, lane, RB, a.group) : S.nrb;
+    const int r0 = lane < S.nch ? walk_first_rb(S, lane, a.group) : S.nrb;
     int before = S.nrb - r0;
 #pragma unroll
     for (int off = 1; off < 64; off <<= 1) {
@@ -122,23 +130,25 @@ __device__ __forceinline__ bool decode_walk(const WalkArgs &a, int bid, WalkItem
   return true;
 }
 
-// Index of (row block, chunk) among the set's items: its partial slot.
-__device__ __forceinline__ int walk_slot(const WalkArgs &a, const WalkSet &S, int kvh, int rb, int ch, int RB) {
-  int i;
+// First 32-row unit of the parts of (row block, chunk).
+__device__ __forceinline__ int walk_part(const WalkArgs &a, const WalkSet &S, int kvh, int rb, int ch) {
+  int i;   // index among the set's items
   if (S.nch == 1) i = S.nrb - 1 - rb;
   else if (!S.causal || S.nrb == 1) i = ch * S.nrb + rb;
   else {
-    i = rb - walk_first_rb(S, ch, RB, a.group);
-    for (int c = 0; c < ch; ++c) i += S.nrb - walk_first_rb(S, c, RB, a.group);
+    i = rb - walk_first_rb(S, ch, a.group);
+    for (int c = 0; c < ch; ++c) i += S.nrb - walk_first_rb(S, c, a.group);
   }
-  return S.part0 + kvh * S.items + i;
+  return S.part0 + (kvh * S.items + i) * (S.rb >> 5);
 }
 
-// A wave's 32 rows of unnormalised O^T (accumulator order, so that every store is
-// a whole 1 KB), m and l.
+// A wave's 32 rows of unnormalised O^T (accumulator order, so that a store of whole
+// rows is 1 KB in one piece), m and l; rows that do not exist are left out (64
+// sequences of 8 rows: a quarter of the traffic).
 template <int DB>
-__device__ __forceinline__ void write_part(float *u, const f32x16 (&O)[DB], float m, float l) {
+__device__ __forceinline__ void write_part(float *u, const f32x16 (&O)[DB], float m, float l, bool row_ok) {
   const int lane = threadIdx.x & 63;
+  if (!row_ok) return;
 #pragma unroll
   for (int i = 0; i < DB; ++i)
 #pragma unroll
@@ -150,31 +160,30 @@ __device__ __forceinline__ void write_part(float *u, const f32x16 (&O)[DB], floa
   }
 }
 
-// WAVES waves per block; K and V each have a two-slot ring of 64-key tiles.
+constexpr int kBf16Waves = 4;
+constexpr int kTileBytes = TK * D * 2;        // one K or V tile (16 KB)
+
+// Four waves per block; K and V each have a two-slot ring of 64-key tiles.
 // KSPLIT = 1: 32 rows a wave, every wave takes whole tiles.  KSPLIT = 2: two
 // groups of waves over the same rows, one for keys 0-31 of every tile and one
 // for keys 32-63, merged through LDS at the end (items of few rows: half the
 // chain per tile, two waves on every SIMD).
-template <int WAVES, int KSPLIT, bool TREE>
-__global__ __launch_bounds__(WAVES * 64, 2) void walk_attn_bf16(WalkArgs a) {
-  constexpr int RW = WAVES / KSPLIT, RB = 32 * RW, NSB = 2 / KSPLIT;
-  constexpr int TILE = TK * D * 2;            // bytes of one K or V tile (16 KB)
+template <int KSPLIT, bool TREE>
+__device__ __forceinline__ void walk_bf16(const WalkArgs &a, const WalkItem &it, uint8_t (*kring)[kTileBytes], uint8_t (*vring)[kTileBytes]) {
+  constexpr int WAVES = kBf16Waves, RW = WAVES / KSPLIT, RB = 32 * RW, NSB = 2 / KSPLIT;
+  constexpr int TILE = kTileBytes;
   constexpr int IPW = TILE / 1024 / WAVES;    // 1 KB direct loads per wave per tile and operand
-  __shared__ __attribute__((aligned(1024))) uint8_t kring[2][TILE];
-  __shared__ __attribute__((aligned(1024))) uint8_t vring[2][TILE];
   int *const par = reinterpret_cast<int *>(vring[1]);   // filled after the first loop barrier
   static_assert(WAVES * 64 >= kMaxNodes && kMaxNodes * 4 <= TILE, "one thread per tree node");
   static_assert(KSPLIT == 1 || RW * 64 * 64 * 4 <= 2 * TILE, "merge buffer fits the K ring");
 
-  WalkItem it;
-  if (!decode_walk<RB>(a, blockIdx.x, it)) return;   // no barrier reached
   const WalkSet &S = it.S;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int rwave = __builtin_amdgcn_readfirstlane(wave % RW), ksb = __builtin_amdgcn_readfirstlane(wave / RW);
   const int h = lane >> 5, g = a.group, L = S.L, P = S.P;
   const int rows = S.T * g;
   const int np = (P + TK - 1) / TK;                               // prefix tiles
-  const int kend = walk_keys(S, it.rb, RB, g);                    // slab keys of this row block
+  const int kend = walk_keys(S, it.rb, g);                    // slab keys of this row block
   const int j0 = it.ch * S.ct, j1 = min(np + (kend + TK - 1) / TK, j0 + S.ct);
 
   const uint8_t *const K0 = static_cast<const uint8_t *>(a.k), *const V0 = static_cast<const uint8_t *>(a.v);
@@ -406,7 +415,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void walk_attn_bf16(WalkArgs a) {
     m = mn;
   }
   if (!wave_rows) return;
-  if (walk_direct(S, it.rb, RB, g)) {
+  if (walk_direct(S, it.rb, g)) {
     if (!row_ok) return;
     // O^T entry r of d-block i is d = 32 i + 8 (r / 4) + 4 h + r % 4 of this lane's row.
     const float inv = 1.f / ltot;
@@ -418,9 +427,18 @@ __global__ __launch_bounds__(WAVES * 64, 2) void walk_attn_bf16(WalkArgs a) {
         *reinterpret_cast<uint2 *>(op + 32 * i + 8 * q4 + 4 * h) =
             uint2{pack_bf16x2(O[i][4 * q4] * inv, O[i][4 * q4 + 1] * inv), pack_bf16x2(O[i][4 * q4 + 2] * inv, O[i][4 * q4 + 3] * inv)};
   } else {
-    const int64_t slot = walk_slot(a, S, it.kvh, it.rb, it.ch, RB);
-    write_part<D / 32>(a.part + (slot * RW + rwave) * walk_unit_floats(D / 32), O, m, ltot);
+    write_part<D / 32>(a.part + (int64_t)(walk_part(a, S, it.kvh, it.rb, it.ch) + rwave) * walk_unit_floats(D / 32), O, m, ltot, row_ok);
   }
+}
+
+template <bool TREE>
+__global__ __launch_bounds__(kBf16Waves * 64, 2) void walk_attn_bf16(WalkArgs a) {
+  __shared__ __attribute__((aligned(1024))) uint8_t kring[2][kTileBytes];
+  __shared__ __attribute__((aligned(1024))) uint8_t vring[2][kTileBytes];
+  WalkItem it;
+  if (!decode_walk(a, blockIdx.x, it)) return;   // no barrier reached
+  if (it.S.rb == 64) walk_bf16<2, TREE>(a, it, kring, vring);
+  else walk_bf16<1, TREE>(a, it, kring, vring);
 }
 
 // fp32: DB 32-column blocks of the head; the block's 32 rows against 32-key tiles,
@@ -437,13 +455,13 @@ __global__ __launch_bounds__(64 * kF32Waves) void walk_attn_f32(WalkArgs a) {
   __shared__ __attribute__((aligned(16))) float merge[kF32Waves][UF];
   __shared__ int par[kMaxNodes];
   WalkItem it;
-  if (!decode_walk<RB>(a, blockIdx.x, it)) return;
+  if (!decode_walk(a, blockIdx.x, it)) return;
   const WalkSet &S = it.S;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int h = lane >> 5, g = a.group, L = S.L, P = S.P, d = a.head_dim;
   const int rows = S.T * g;
   const int np = (P + TK - 1) / TK;
-  const int kend = walk_keys(S, it.rb, RB, g);
+  const int kend = walk_keys(S, it.rb, g);
   const int j0 = it.ch * S.ct, j1 = min(np + (kend + TK - 1) / TK, j0 + S.ct);
   const int64_t head = (int64_t)it.kvh * a.cap_total;
   const float *const K0 = static_cast<const float *>(a.k), *const V0 = static_cast<const float *>(a.v);
@@ -488,16 +506,29 @@ __global__ __launch_bounds__(64 * kF32Waves) void walk_attn_f32(WalkArgs a) {
     if (kt >= end) continue;
     const int64_t base = (head + (pre ? S.pbase : S.base)) * d;
     const float *kp = K0 + base + (int64_t)min(kt + (lane & 31), end - 1) * d + 4 * h * qh;
+    // the whole tile's loads go out first: one memory latency
+    f32x4 kf[4 * DB];
+#pragma unroll
+    for (int t = 0; t < 4 * DB; ++t) {
+      kf[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+      if (t < myq) kf[t] = *reinterpret_cast<const f32x4 *>(kp + 4 * t);
+    }
+    const float *vp = V0 + base;
+    float vf[16][DB];
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const int t = min(kt + 8 * (r >> 2) + 4 * h + (r & 3), end - 1);
+#pragma unroll
+      for (int i = 0; i < DB; ++i) vf[r][i] = vp[(int64_t)t * d + min(32 * i + (lane & 31), d - 1)];   // columns past the head are not written
+    }
     f32x16 Sc;
 #pragma unroll
     for (int r = 0; r < 16; ++r) Sc[r] = 0.f;
 #pragma unroll
     for (int t = 0; t < 4 * DB; ++t)
       if (t < qh) {
-        f32x4 k = *reinterpret_cast<const f32x4 *>(kp + 4 * (t < myq ? t : 0));
-        if (t >= myq) k = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int e = 0; e < 4; ++e) Sc = __builtin_amdgcn_mfma_f32_32x32x2f32(k[e], qf[t][e], Sc, 0, 0, 0);
+        for (int e = 0; e < 4; ++e) Sc = __builtin_amdgcn_mfma_f32_32x32x2f32(kf[t][e], qf[t][e], Sc, 0, 0, 0);
       }
     float tm = -INFINITY;
 #pragma unroll
@@ -527,19 +558,12 @@ __global__ __launch_bounds__(64 * kF32Waves) void walk_attn_f32(WalkArgs a) {
     for (int i = 0; i < DB; ++i)
 #pragma unroll
       for (int r = 0; r < 16; ++r) O[i][r] *= alpha;
-    const float *vp = V0 + base;
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      const int t = min(kt + 8 * (r >> 2) + 4 * h + (r & 3), end - 1);
+    for (int r = 0; r < 16; ++r)
 #pragma unroll
-      for (int i = 0; i < DB; ++i) {
-        const int col = 32 * i + (lane & 31);
-        const float v = vp[(int64_t)t * d + min(col, d - 1)];   // columns past the head are not written
-        O[i] = __builtin_amdgcn_mfma_f32_32x32x2f32(v, Sc[r], O[i], 0, 0, 0);
-      }
-    }
+      for (int i = 0; i < DB; ++i) O[i] = __builtin_amdgcn_mfma_f32_32x32x2f32(vf[r][i], Sc[r], O[i], 0, 0, 0);
   }
-  write_part<DB>(merge[wave], O, m, sum_with_other_half(l));
+  write_part<DB>(merge[wave], O, m, sum_with_other_half(l), true);
   __syncthreads();
   // Wave w merges the d-block entries 4 DB / 4 w ... of all four waves' parts.
   float mw[kF32Waves], M = -INFINITY, lt = 0.f;
@@ -553,8 +577,8 @@ __global__ __launch_bounds__(64 * kF32Waves) void walk_attn_f32(WalkArgs a) {
     mw[w] = mw[w] == -INFINITY ? 0.f : fast_exp2(mw[w] - M);
     lt = fmaf(merge[w][DB * 1024 + 32 + (lane & 31)], mw[w], lt);
   }
-  const bool direct = walk_direct(S, it.rb, RB, g);
-  float *const u = direct ? nullptr : a.part + (int64_t)walk_slot(a, S, it.kvh, it.rb, it.ch, RB) * UF;
+  const bool direct = walk_direct(S, it.rb, g);
+  float *const u = direct ? nullptr : a.part + (int64_t)walk_part(a, S, it.kvh, it.rb, it.ch) * UF;
   const float inv = direct ? 1.f / lt : 1.f;
 #pragma unroll
   for (int n = 0; n < DB; ++n) {
@@ -567,8 +591,9 @@ __global__ __launch_bounds__(64 * kF32Waves) void walk_attn_f32(WalkArgs a) {
       for (int e = 0; e < 4; ++e) o[e] = fmaf(v[e], mw[w], o[e]);
     }
     const int col = 32 * (iq >> 2) + 8 * (iq & 3) + 4 * h;
+    if (!row_ok) continue;
     if (!direct) *reinterpret_cast<f32x4 *>(u + (iq * 64 + lane) * 4) = o;
-    else if (row_ok && col < d)
+    else if (col < d)
       *reinterpret_cast<f32x4 *>(static_cast<float *>(a.out) + ((int64_t)(S.row0 + node) * a.n_q + hq) * d + col) =
           f32x4{o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
   }
@@ -582,43 +607,37 @@ __global__ __launch_bounds__(64 * kF32Waves) void walk_attn_f32(WalkArgs a) {
 // prefix's set, where the rows lie among the packed rows of all its sequences.
 // Wave w takes the column entries w DB .. + DB - 1 of the accumulator order; the
 // maximum over all parts first (their m alone), so that the sums need no rescaling.
-template <int DB, int RB, bool BF16>
+template <int DB, bool BF16>
 __global__ __launch_bounds__(256) void walk_combine(WalkArgs a) {
-  constexpr int UF = walk_unit_floats(DB), UPB = RB / 32;
+  constexpr int UF = walk_unit_floats(DB);
   WalkSet S;
   int kvh, i;
   if (!decode_unit<true>(a, blockIdx.x, S, kvh, i)) return;
   i += S.cunit0;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5, g = a.group;
-  const int rb = __builtin_amdgcn_readfirstlane(i / UPB), un = __builtin_amdgcn_readfirstlane(i % UPB);
+  const int upb = S.rb >> 5, rb = __builtin_amdgcn_readfirstlane(i / upb), un = __builtin_amdgcn_readfirstlane(i % upb);
   const int row = 32 * i + (lane & 31);
   const bool row_ok = row < S.T * g;
-  const int nown = walk_chunks(S, rb, RB, g);
+  const int nown = walk_chunks(S, rb, g);
   WalkSet H{};
-  int hr = 0, parts = nown;
+  int hr = 0, hsh = 5, parts = nown;
   if (S.shared >= 0) {
-    H = get_set(walk_sets(a), S.shared);
+    H = get_set(a, S.shared);
     hr = (S.row0 - H.row0) * g + (row_ok ? row : 0);
+    hsh = __builtin_ctz(H.rb);
     parts += H.nch;
   }
   const int hl = (hr & 31) | (lane & 32);
   // part p: its 32-row unit (own chunks by row block, the prefix's by lane) and this lane's place in it
   auto unit = [&](int p) {
-    if (p < nown) return a.part + ((int64_t)walk_slot(a, S, kvh, rb, p, RB) * UPB + un) * UF;
-    return a.part + ((int64_t)walk_slot(a, H, kvh, hr / RB, p - nown, RB) * UPB + hr % RB / 32) * UF;
+    if (p < nown) return a.part + (int64_t)(walk_part(a, S, kvh, rb, p) + un) * UF;
+    return a.part + (int64_t)(walk_part(a, H, kvh, hr >> hsh, p - nown) + ((hr & (H.rb - 1)) >> 5)) * UF;
   };
-  constexpr int G = 4;   // parts whose loads are in flight at once
-  float M = -INFINITY;
-  for (int p0 = 0; p0 < parts; p0 += G) {
-    float mp[G];
-#pragma unroll
-    for (int e = 0; e < G; ++e) {
-      const int p = min(p0 + e, parts - 1);
-      mp[e] = unit(p)[DB * 1024 + ((p < nown ? lane : hl) & 31)];
-    }
-    M = fmaxf(fmaxf(M, fmaxf(mp[0], mp[1])), fmaxf(mp[2], mp[3]));
-  }
-  float l = 0.f;
+  if (!row_ok) return;
+  // The first G parts are read at once, everything of them; a running maximum takes
+  // in the others G at a time.
+  constexpr int G = 4;
+  float M = -INFINITY, l = 0.f;
   f32x4 o[DB];
 #pragma unroll
   for (int n = 0; n < DB; ++n) o[n] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -627,17 +646,29 @@ __global__ __launch_bounds__(256) void walk_combine(WalkArgs a) {
     float mp[G], lp[G];
 #pragma unroll
     for (int e = 0; e < G; ++e) {
-      const int p = min(p0 + e, parts - 1), ln = p < nown ? lane : hl;
-      const float *u = unit(p);
-      mp[e] = u[DB * 1024 + (ln & 31)];
-      lp[e] = u[DB * 1024 + 32 + (ln & 31)];
+      mp[e] = -INFINITY;
+      lp[e] = 0.f;
 #pragma unroll
-      for (int n = 0; n < DB; ++n) v[e][n] = *reinterpret_cast<const f32x4 *>(u + ((wave * DB + n) * 64 + ln) * 4);
+      for (int n = 0; n < DB; ++n) v[e][n] = f32x4{0.f, 0.f, 0.f, 0.f};
+      if (p0 + e < parts) {
+        const int p = p0 + e, ln = p < nown ? lane : hl;
+        const float *u = unit(p);
+        mp[e] = u[DB * 1024 + (ln & 31)];
+        lp[e] = u[DB * 1024 + 32 + (ln & 31)];
+#pragma unroll
+        for (int n = 0; n < DB; ++n) v[e][n] = *reinterpret_cast<const f32x4 *>(u + ((wave * DB + n) * 64 + ln) * 4);
+      }
     }
+    const float Mn = fmaxf(fmaxf(M, fmaxf(mp[0], mp[1])), fmaxf(mp[2], mp[3]));
+    // a part without a visible key of this row (m = -inf) weighs nothing
+    const float w0 = M == -INFINITY ? 0.f : fast_exp2(M - Mn);
+    M = Mn;
+    l *= w0;
+#pragma unroll
+    for (int n = 0; n < DB; ++n) o[n] *= w0;
 #pragma unroll
     for (int e = 0; e < G; ++e) {
-      // a part without a visible key of this row, or a repeated load past the last part: weight 0
-      const float w = p0 + e >= parts || mp[e] == -INFINITY ? 0.f : fast_exp2(mp[e] - M);
+      const float w = mp[e] == -INFINITY ? 0.f : fast_exp2(mp[e] - M);
       l = fmaf(lp[e], w, l);
 #pragma unroll
       for (int n = 0; n < DB; ++n)
@@ -645,7 +676,6 @@ __global__ __launch_bounds__(256) void walk_combine(WalkArgs a) {
         for (int c = 0; c < 4; ++c) o[n][c] = fmaf(v[e][n][c], w, o[n][c]);
     }
   }
-  if (!row_ok) return;
   const float inv = 1.f / l;
   const int node = row / g, hq = kvh * g + row % g;
   const int64_t at = ((int64_t)(S.row0 + node) * a.n_q + hq) * a.head_dim;
@@ -667,31 +697,26 @@ void launch_f32(const WalkArgs &a, hipStream_t st) {
   switch ((a.head_dim + 31) / 32) {
     case 1:
       hipLaunchKernelGGL((walk_attn_f32<1, TREE>), grid, block, 0, st, a);
-      if (a.cslots) hipLaunchKernelGGL((walk_combine<1, 32, false>), cgrid, dim3(256), 0, st, a);
+      if (a.cslots) hipLaunchKernelGGL((walk_combine<1, false>), cgrid, dim3(256), 0, st, a);
       break;
     case 2:
       hipLaunchKernelGGL((walk_attn_f32<2, TREE>), grid, block, 0, st, a);
-      if (a.cslots) hipLaunchKernelGGL((walk_combine<2, 32, false>), cgrid, dim3(256), 0, st, a);
+      if (a.cslots) hipLaunchKernelGGL((walk_combine<2, false>), cgrid, dim3(256), 0, st, a);
       break;
     case 3:
       hipLaunchKernelGGL((walk_attn_f32<3, TREE>), grid, block, 0, st, a);
-      if (a.cslots) hipLaunchKernelGGL((walk_combine<3, 32, false>), cgrid, dim3(256), 0, st, a);
+      if (a.cslots) hipLaunchKernelGGL((walk_combine<3, false>), cgrid, dim3(256), 0, st, a);
       break;
     default:
       hipLaunchKernelGGL((walk_attn_f32<4, TREE>), grid, block, 0, st, a);
-      if (a.cslots) hipLaunchKernelGGL((walk_combine<4, 32, false>), cgrid, dim3(256), 0, st, a);
+      if (a.cslots) hipLaunchKernelGGL((walk_combine<4, false>), cgrid, dim3(256), 0, st, a);
   }
 }
 
 template <bool TREE>
 void launch_bf16(const WalkArgs &a, hipStream_t st) {
-  if (a.rb == 64) {
-    hipLaunchKernelGGL((walk_attn_bf16<4, 2, TREE>), dim3(8 * a.slots), dim3(256), 0, st, a);
-    if (a.cslots) hipLaunchKernelGGL((walk_combine<D / 32, 64, true>), dim3(8 * a.cslots), dim3(256), 0, st, a);
-  } else {
-    hipLaunchKernelGGL((walk_attn_bf16<4, 1, TREE>), dim3(8 * a.slots), dim3(256), 0, st, a);
-    if (a.cslots) hipLaunchKernelGGL((walk_combine<D / 32, 128, true>), dim3(8 * a.cslots), dim3(256), 0, st, a);
-  }
+  hipLaunchKernelGGL((walk_attn_bf16<TREE>), dim3(8 * a.slots), dim3(64 * kBf16Waves), 0, st, a);
+  if (a.cslots) hipLaunchKernelGGL((walk_combine<D / 32, true>), dim3(8 * a.cslots), dim3(256), 0, st, a);
 }
 
 }  // namespace

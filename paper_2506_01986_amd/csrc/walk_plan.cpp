@@ -1,6 +1,6 @@
 // Launch planning of the attention over key ranges (range_attn.hip): which
-// sequences' rows walk a shared prefix together, how the keys are split over
-// blocks, and where every part goes.
+// sequences' rows walk a shared prefix together, how many rows a block takes, how
+// the keys are split over blocks, and where every part goes.
 #include <algorithm>
 #include <numeric>
 
@@ -10,62 +10,72 @@ namespace specmemo {
 
 namespace {
 
-// Fewest tiles of a chunk.  A chunk costs a start-up of about two tiles' time
-// and its share of the merge.
-constexpr int kMinTilesBf16 = 3, kMinTilesF32 = 2;
 constexpr int kMaxCausalChunks = 64;   // one a lane (decode_walk)
+
+// Rules of the split, in us of a block's time (two blocks share a compute unit): a
+// 64-key tile takes a block of 64 rows kTileSmall and one of 128 rows kTileLarge
+// (fp32, 32 rows: kTileF32 for each 32 columns of the head).
+constexpr double kTileSmall = 1.05, kTileLarge = 2.0, kTileF32 = 0.45;
+// A chunk's start and its share of the merge.  Below about this much work a chunk
+// is mostly that: 8 sequences of 1 to 8 tokens over 500 to 4000 keys, 64 query heads,
+// 19.1 us in chunks of 8 tiles, 26 in chunks of 3, 42 unsplit.
+constexpr double kChunkStart = 5.0;
+// Chunks may exceed a block slot's average share by this much where their row blocks
+// are full: every part of full row blocks is written and read again (16 KB for 32
+// rows).  10 sequences of 512 rows over 2.1k to 3k keys: unsplit (48 tiles) 74.8 us,
+// chunks of 19 tiles 76.8, of 12 81.1; 24 sequences of 16 rows over a prefix of 4096
+// keys (384 packed rows): 22 tiles 51.6 us, 16 tiles 54.4, unsplit 91.
+constexpr double kFullSlack = 0.6;
 
 int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 
-int64_t chunk_items(const WalkSet &s, int ct, int RB, int g) {
-  if (!s.causal || s.nrb == 1) return (int64_t)s.nrb * ceil_div(walk_tiles(s, 0, RB, g), ct);
+// (row block, chunk) pairs of a KV head
+int count_items(const WalkSet &s, int g) {
+  if (!s.causal || s.nrb == 1) return s.nrb * s.nch;
+  int n = 0;
+  for (int c = 0; c < s.nch; ++c) n += s.nrb - walk_first_rb(s, c, g);
+  return n;
+}
+
+// Tiles of all row blocks of a KV head.
+int64_t count_tiles(const WalkSet &s, int g) {
+  if (!s.causal) return (int64_t)s.nrb * walk_tiles(s, 0, g);
   int64_t n = 0;
-  WalkSet t = s;
-  t.ct = ct;
-  for (int c = 0, nch = ceil_div(walk_tiles(s, s.nrb - 1, RB, g), ct); c < nch; ++c) n += s.nrb - walk_first_rb(t, c, RB, g);
+  for (int rb = 0; rb < s.nrb; ++rb) n += walk_tiles(s, rb, g);
   return n;
 }
 
 }  // namespace
 
-void plan_walk(int dt, bool causal, const std::vector<WalkSeq> &seqs, int n_kv, int g, int cus, WalkPlan *p) {
+void plan_walk(int dt, bool causal, const std::vector<WalkSeq> &seqs, int n_kv, int g, int head_dim, int cus, WalkPlan *p) {
   const bool f32 = dt == 0;
   const int nseq = (int)seqs.size();
   auto rows_of = [&](int i) { return (int64_t)seqs[i].T * g; };
-
-  // Row blocks: 128 rows, or 64 rows with the keys of a tile split over two wave
-  // groups where nobody has more (fp32: 32 rows).
-  int64_t most = 0;
-  for (int i = 0; i < nseq; ++i) most = std::max(most, rows_of(i));
-  int RB = f32 ? 32 : most <= 64 ? 64 : 128;
+  // rows that a block's tile costs are paid for: 128 cost about twice 64
+  auto paid = [&](int64_t rows) { return f32 ? ceil_div(rows, 32) * 32 : rows <= 64 ? 64 : ceil_div(rows, 128) * 128; };
 
   // Runs of neighbours over one prefix: their rows are packed for its keys where
-  // that walks them with at most three quarters of the row blocks (the parts of
-  // both sides are then written and merged).
+  // that pays for at most three quarters of the rows (the parts of both sides are
+  // then written and merged).
   struct Run {
     int first, last;
   };
   std::vector<Run> runs;
   std::vector<int> run_of(nseq, -1);
-  int RBp = RB;
   for (int i = 0; i < nseq;) {
     int j = i + 1;
-    int64_t rows = rows_of(i), apart = ceil_div(rows_of(i), RB) * (int64_t)RB;
+    int64_t rows = rows_of(i), apart = paid(rows);
     while (j < nseq && seqs[j].P == seqs[i].P && seqs[j].pbase == seqs[i].pbase && rows + rows_of(j) <= INT32_MAX / 2) {
       rows += rows_of(j);
-      apart += ceil_div(rows_of(j), RB) * (int64_t)RB;
+      apart += paid(rows_of(j));
       ++j;
     }
-    const int rbp = f32 ? 32 : rows <= 64 ? 64 : 128;
-    if (seqs[i].P > 0 && j - i > 1 && 4 * ceil_div(rows, rbp) * (int64_t)rbp <= 3 * apart) {
+    if (seqs[i].P > 0 && j - i > 1 && 4 * (int64_t)paid(rows) <= 3 * apart) {
       for (int k = i; k < j; ++k) run_of[k] = (int)runs.size();
       runs.push_back(Run{i, j});
-      RBp = std::max(RBp, rbp);
     }
     i = j;
   }
-  RB = RBp;
-  p->rb = RB;
 
   std::vector<WalkSet> sets;
   for (const Run &r : runs) {
@@ -96,55 +106,51 @@ void plan_walk(int dt, bool causal, const std::vector<WalkSeq> &seqs, int n_kv, 
     sets.push_back(s);
   }
 
-  // The split: where the unsplit items fit one round of resident blocks, the
-  // shortest chunk that still does; otherwise no item is longer than a block's
-  // average share.
-  const int64_t slots = 2 * (int64_t)cus;
-  const int min_tiles = f32 ? kMinTilesF32 : kMinTilesBf16;
-  int64_t items = 0, work = 0;
-  int longest = 1;
-  for (WalkSet &s : sets) {
-    s.nrb = ceil_div((int64_t)s.T * g, RB);
-    items += (int64_t)s.nrb * n_kv;
-    const int nt = walk_tiles(s, s.nrb - 1, RB, g);
-    longest = std::max(longest, nt);
-    if (!s.causal) {
-      work += (int64_t)nt * s.nrb * n_kv;
-    } else {
-      for (int rb = 0; rb < s.nrb; ++rb) work += (int64_t)walk_tiles(s, rb, RB, g) * n_kv;
-    }
+  // Row blocks of 128 rows, or of 64 with the keys of a tile split over two wave
+  // groups (half the chain per tile, but every tile is loaded for half the rows, and
+  // a block starts twice as often): where nobody has more rows, where 128-row blocks
+  // would not give every compute unit one, and for causal blocks, whose lengths
+  // differ, also up to two a unit if the longest takes eight times its start.
+  // Causal, 32 heads x 1024 rows (256 blocks of 128): 22.0 us in 64, 25.2 in 128; x
+  // 2048 (512, up to 32 tiles) 54.6, 67.3; 8 heads x 8192 rows (512, up to 16 tiles)
+  // 35.8, 32.7; 8 heads x 4 x 2048 rows (512, up to 4) 22.3, 17.6.  Trees, 8 heads x
+  // 5120 rows (320 blocks of 48 tiles): 81.5, 74.8.
+  int64_t large_blocks = 0;
+  int longest = 0;
+  for (const WalkSet &s : sets) {
+    large_blocks += (int64_t)ceil_div((int64_t)s.T * g, 128) * n_kv;
+    longest = std::max(longest, ceil_div(s.P, kAttnKeyTile) + (s.slab ? ceil_div(s.L + s.T, kAttnKeyTile) : 0));
   }
-  int ct = longest;
-  if (items < slots) {
-    int lo = std::min(std::max(min_tiles, ceil_div(longest, slots)), longest), hi = longest;
-    while (lo < hi) {
-      const int mid = (lo + hi) / 2;
-      int64_t n = 0;
-      for (const WalkSet &s : sets) n += chunk_items(s, mid, RB, g) * n_kv;
-      if (n <= slots) hi = mid;
-      else lo = mid + 1;
-    }
-    ct = lo;
-  } else {
-    ct = std::max<int64_t>(min_tiles, (work + slots - 1) / slots);
+  const bool small = large_blocks <= cus || (causal && large_blocks <= 2 * cus && longest * kTileLarge >= 8 * kChunkStart);
+  auto tile_us = [&](const WalkSet &s) { return f32 ? kTileF32 * ceil_div(head_dim, 32) : s.rb > 64 ? kTileLarge : kTileSmall; };
+  double work = 0;
+  for (WalkSet &s : sets) {
+    const int64_t rows = (int64_t)s.T * g;
+    s.rb = f32 ? 32 : rows <= 64 || small ? 64 : 128;
+    s.nrb = ceil_div(rows, s.rb);
+    work += (double)count_tiles(s, g) * tile_us(s) * n_kv;
+  }
+  const double share = work / (2.0 * cus);
+  const size_t n = sets.size();
+  std::vector<double> size(n);             // the longest item of each set
+  for (size_t i = 0; i < n; ++i) {
+    WalkSet &s = sets[i];
+    const int nt = walk_tiles(s, s.nrb - 1, g);
+    const double full = std::min(1.0, (double)s.T * g / s.rb);
+    const double limit = share * (1 + kFullSlack * full) + kChunkStart;
+    int nch = ceil_div(nt, std::max(1, (int)(limit / tile_us(s))));
+    if (s.causal && s.nrb > 1) nch = std::min(nch, kMaxCausalChunks);
+    s.ct = ceil_div(nt, nch);              // equal chunks; the count may drop by rounding
+    s.nch = ceil_div(nt, s.ct);
+    s.items = count_items(s, g);
+    size[i] = s.ct * tile_us(s);
   }
 
-  std::vector<int> size(sets.size());
-  for (size_t i = 0; i < sets.size(); ++i) {
-    WalkSet &s = sets[i];
-    const int nt = walk_tiles(s, s.nrb - 1, RB, g);
-    int nch = std::max(1, ceil_div(nt, ct));
-    if (s.causal && s.nrb > 1) nch = std::min(nch, kMaxCausalChunks);
-    s.ct = ceil_div(nt, nch);            // equal chunks; the count may drop by rounding
-    s.nch = ceil_div(nt, s.ct);
-    s.items = (int)chunk_items(s, s.ct, RB, g);
-    size[i] = s.nch == 1 ? nt : s.ct;
-  }
   // longest items first
-  std::vector<int> order(sets.size()), place(sets.size());
+  std::vector<int> order(n), place(n);
   std::iota(order.begin(), order.end(), 0);
   std::stable_sort(order.begin(), order.end(), [&](int x, int y) { return size[x] > size[y]; });
-  for (size_t i = 0; i < order.size(); ++i) place[order[i]] = (int)i;
+  for (size_t i = 0; i < n; ++i) place[order[i]] = (int)i;
   const int fan = 8 / std::gcd(n_kv, 8), units = n_kv * fan / 8;
   p->fan = fan;
   p->units = units;
@@ -157,11 +163,11 @@ void plan_walk(int dt, bool causal, const std::vector<WalkSeq> &seqs, int n_kv, 
     s.part0 = -1;
     if (s.nch > 1 || s.parts) {
       s.part0 = (int)part;
-      part += (int64_t)s.items * n_kv;
+      part += (int64_t)s.items * n_kv * (s.rb / 32);
     }
     s.ccum = (int)cslot;
     if (s.slab && s.part0 >= 0) {
-      if (!s.parts && s.causal) s.cunit0 = walk_first_rb(s, 1, RB, g) * (RB / 32);
+      if (!s.parts && s.causal) s.cunit0 = walk_first_rb(s, 1, g) * (s.rb / 32);
       s.citems = ceil_div((int64_t)s.T * g, 32) - s.cunit0;
       cslot += (int64_t)ceil_div(s.citems, fan) * units;
     }
