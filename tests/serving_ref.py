@@ -57,7 +57,7 @@ class Batch:
     def rows(self, b):
         return np.concatenate([np.arange(self.plen[b]) + self.pbase[b], np.arange(self.L[b] + self.n[b]) + self.base[b]])
 
-    def reference(self, sees, scale=None):
+    def reference(self, sees, scale=None, device="cpu"):
         """(softmax(q k scale) v, tolerance) in 64 bits; sees(b): bool [n_b][n_b], which of the sequence's own nodes a
         node sees (committed and prefix rows all are)."""
         scale = self.d ** -0.5 if scale is None else scale
@@ -69,15 +69,16 @@ class Batch:
             if n == 0:
                 continue
             rows = torch.from_numpy(self.rows(b))
-            vis = torch.ones(n, before + n, dtype=torch.bool)
-            vis[:, before:] = sees(b)
+            vis = torch.ones(n, before + n, dtype=torch.bool, device=device)
+            vis[:, before:] = sees(b).to(device)
             for h in range(self.n_q):
-                q = self.q[o:o + n, h].double()
-                k, v = self.k[h // g, rows].double(), self.v[h // g, rows].double()
+                q = self.q[o:o + n, h].to(device).double()
+                k, v = (x[h // g, rows].to(device).double() for x in (self.k, self.v))
                 s = (q @ k.t() * scale).masked_fill(~vis, -np.inf)
                 p = torch.softmax(s, 1)
-                out[o:o + n, h] = p @ v
-                tol[o:o + n, h] = self.tolerance(p, v, out[o:o + n, h], q, k, s, scale)
+                exact = p @ v
+                out[o:o + n, h] = exact.cpu()
+                tol[o:o + n, h] = self.tolerance(p, v, exact, q, k, s, scale).cpu()
         return out, tol
 
     def tolerance(self, p, v, out, q, k, s, scale):

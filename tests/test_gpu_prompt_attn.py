@@ -90,6 +90,17 @@ def test_equal_scores(dtype):
     parity(x)
 
 
+@pytest.mark.parametrize("n_q,n_kv,L,P", [(112, 112, 0, 0), (112, 112, 40, 70), (250, 50, 3, 0)])
+def test_many_row_blocks(n_q, n_kv, L, P):
+    """Thousands of row blocks, several rounds of them."""
+    n = [257, 400, 1, 385, 128, 300, 270, 512, 129, 640, 333, 500, 3, 301, 257, 280, 450, 390, 260, 310]
+    x = Batch("bf16", n_q, n_kv, 128, n if n_q == n_kv else n[:14], [L] * (20 if n_q == n_kv else 14),
+              [P] * (20 if n_q == n_kv else 14), seed=P).upload()
+    assert sm.prompt_attn_bytes(x.dt, x.off, x.kv, n_q, x.px) == 0          # nothing is split
+    ref, tol = x.reference(lambda b: causal(x.n[b]), device="cuda")
+    check(run(x), ref, tol)
+
+
 def test_same_prompt_in_chunks():
     """A prompt in one call, and token ranges of it on their committed rows, agree within two roundings."""
     x = Batch("bf16", 8, 2, 128, [333], [0], seed=9).upload()
