@@ -19,7 +19,7 @@
 // bf16: the tile loop of tree_attn_bf16 (K and V tiles in LDS rings filled by
 // direct loads, S^T = K Q^T and O^T = V^T P^T on the 32x32x16 matrix product,
 // 32 query rows a wave, P never leaves its lane).
-// fp32: 32 query rows a block on the 32x32x2 fp32 product, the block's four waves
+// fp32: 32 query rows a block on the 32x32x2 fp32 product, the block's waves
 // taking 32-key tiles in turn straight from memory, merged through LDS.
 #include <type_traits>
 
@@ -442,17 +442,23 @@ __global__ __launch_bounds__(kBf16Waves * 64, 2) void walk_attn_bf16(WalkArgs a)
 }
 
 // fp32: DB 32-column blocks of the head; the block's 32 rows against 32-key tiles,
-// wave w taking tiles w, w + 4, ...  The sum over the columns may run in any order
+// wave w taking tiles w, w + W, ...  The sum over the columns may run in any order
 // as long as both operands use it: lane half h holds the column quads h qh + t, so
 // a lane reads 16 bytes of its key row at a time.  The weights leave the score
 // accumulator as they lie (lane half h, entry r: key 8 (r / 4) + 4 h + r % 4) and
 // meet V rows of the same order.
+// (Eight waves a block, to take short ranges in one turn, cost more to start and
+// merge than they save: 2 x 500 rows x 8 heads of 64 columns 22.4 us, 18.4 with four.)
+// Up to 64 columns a tile's K and V rows are loaded as a whole, one memory latency;
+// past them two waves to a SIMD hide it better than the registers that would take
+// (4 x 1024 rows x 16 heads of 128 columns: 250 us, 271 as a whole).
 constexpr int kF32Waves = 4;
 
 template <int DB, bool TREE>
-__global__ __launch_bounds__(64 * kF32Waves) void walk_attn_f32(WalkArgs a) {
-  constexpr int RB = 32, UF = walk_unit_floats(DB);
-  __shared__ __attribute__((aligned(16))) float merge[kF32Waves][UF];
+__global__ __launch_bounds__(64 * kF32Waves, 2) void walk_attn_f32(WalkArgs a) {
+  constexpr int RB = 32, W = kF32Waves, UF = walk_unit_floats(DB);
+  constexpr int KQ = DB <= 2 ? 4 * DB : 4, VR = DB <= 2 ? 16 : 4;   // column quads and key rows loaded together
+  __shared__ __attribute__((aligned(16))) float merge[W][UF];
   __shared__ int par[kMaxNodes];
   WalkItem it;
   if (!decode_walk(a, blockIdx.x, it)) return;
@@ -485,7 +491,7 @@ __global__ __launch_bounds__(64 * kF32Waves) void walk_attn_f32(WalkArgs a) {
   uint64_t alo = 0, ahi = 0;
   if (TREE) {
     if (tree && tid < S.T) par[tid] = a.parent[S.row0 + tid];
-    __syncthreads();
+    ring_barrier();                                  // (does not wait for the queries)
     if (tree)
       for (int u = node; u >= 0; u = par[u]) {
         alo |= u < 64 ? 1ull << (u & 63) : 0ull;
@@ -500,36 +506,45 @@ __global__ __launch_bounds__(64 * kF32Waves) void walk_attn_f32(WalkArgs a) {
   for (int i = 0; i < DB; ++i)
 #pragma unroll
     for (int r = 0; r < 16; ++r) O[i][r] = 0.f;
-  for (int t2 = 2 * j0 + wave; t2 < 2 * j1; t2 += kF32Waves) {
+  for (int t2 = 2 * j0 + wave; t2 < 2 * j1; t2 += W) {
     const bool pre = (t2 >> 1) < np;
     const int kt = (pre ? t2 : t2 - 2 * np) * 32, end = pre ? P : kend;
     if (kt >= end) continue;
     const int64_t base = (head + (pre ? S.pbase : S.base)) * d;
     const float *kp = K0 + base + (int64_t)min(kt + (lane & 31), end - 1) * d + 4 * h * qh;
-    // the whole tile's loads go out first: one memory latency
-    f32x4 kf[4 * DB];
-#pragma unroll
-    for (int t = 0; t < 4 * DB; ++t) {
-      kf[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-      if (t < myq) kf[t] = *reinterpret_cast<const f32x4 *>(kp + 4 * t);
-    }
     const float *vp = V0 + base;
-    float vf[16][DB];
+    f32x4 kf[KQ];
+    float vf[VR][DB];
+    auto load_k = [&](int t0) __attribute__((always_inline)) {
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      const int t = min(kt + 8 * (r >> 2) + 4 * h + (r & 3), end - 1);
+      for (int t = 0; t < KQ; ++t) {
+        kf[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+        if (t0 + t < myq) kf[t] = *reinterpret_cast<const f32x4 *>(kp + 4 * (t0 + t));
+      }
+    };
+    auto load_v = [&](int r0) __attribute__((always_inline)) {
 #pragma unroll
-      for (int i = 0; i < DB; ++i) vf[r][i] = vp[(int64_t)t * d + min(32 * i + (lane & 31), d - 1)];   // columns past the head are not written
-    }
+      for (int r = 0; r < VR; ++r) {
+        const int t = min(kt + 8 * ((r0 + r) >> 2) + 4 * h + ((r0 + r) & 3), end - 1);
+#pragma unroll
+        for (int i = 0; i < DB; ++i) vf[r][i] = vp[(int64_t)t * d + min(32 * i + (lane & 31), d - 1)];   // columns past the head are not written
+      }
+    };
     f32x16 Sc;
 #pragma unroll
     for (int r = 0; r < 16; ++r) Sc[r] = 0.f;
+    load_k(0);
+    if (VR == 16) load_v(0);
 #pragma unroll
-    for (int t = 0; t < 4 * DB; ++t)
-      if (t < qh) {
+    for (int t0 = 0; t0 < 4 * DB; t0 += KQ) {
+      if (t0 > 0) load_k(t0);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) Sc = __builtin_amdgcn_mfma_f32_32x32x2f32(kf[t][e], qf[t][e], Sc, 0, 0, 0);
-      }
+      for (int t = 0; t < KQ; ++t)
+        if (t0 + t < qh) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) Sc = __builtin_amdgcn_mfma_f32_32x32x2f32(kf[t][e], qf[t0 + t][e], Sc, 0, 0, 0);
+        }
+    }
     float tm = -INFINITY;
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
@@ -559,33 +574,35 @@ __global__ __launch_bounds__(64 * kF32Waves) void walk_attn_f32(WalkArgs a) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) O[i][r] *= alpha;
 #pragma unroll
-    for (int r = 0; r < 16; ++r)
+    for (int r0 = 0; r0 < 16; r0 += VR) {
+      if (VR < 16) load_v(r0);
 #pragma unroll
-      for (int i = 0; i < DB; ++i) O[i] = __builtin_amdgcn_mfma_f32_32x32x2f32(vf[r][i], Sc[r], O[i], 0, 0, 0);
+      for (int r = 0; r < VR; ++r)
+#pragma unroll
+        for (int i = 0; i < DB; ++i) O[i] = __builtin_amdgcn_mfma_f32_32x32x2f32(vf[r][i], Sc[r0 + r], O[i], 0, 0, 0);
+    }
   }
   write_part<DB>(merge[wave], O, m, sum_with_other_half(l), true);
   __syncthreads();
-  // Wave w merges the d-block entries 4 DB / 4 w ... of all four waves' parts.
-  float mw[kF32Waves], M = -INFINITY, lt = 0.f;
+  // Wave w merges entries 4 DB / W w ... of all waves' parts.
+  float mw[W], M = -INFINITY, lt = 0.f;
 #pragma unroll
-  for (int w = 0; w < kF32Waves; ++w) {
+  for (int w = 0; w < W; ++w) {
     mw[w] = merge[w][DB * 1024 + (lane & 31)];
     M = fmaxf(M, mw[w]);
   }
 #pragma unroll
-  for (int w = 0; w < kF32Waves; ++w) {
+  for (int w = 0; w < W; ++w) {
     mw[w] = mw[w] == -INFINITY ? 0.f : fast_exp2(mw[w] - M);
     lt = fmaf(merge[w][DB * 1024 + 32 + (lane & 31)], mw[w], lt);
   }
   const bool direct = walk_direct(S, it.rb, g);
   float *const u = direct ? nullptr : a.part + (int64_t)walk_part(a, S, it.kvh, it.rb, it.ch) * UF;
   const float inv = direct ? 1.f / lt : 1.f;
-#pragma unroll
-  for (int n = 0; n < DB; ++n) {
-    const int iq = wave * DB + n;                    // d-block iq / 4, entries 4 (iq % 4) .. + 3
+  for (int iq = wave; iq < 4 * DB; iq += W) {        // d-block iq / 4, entries 4 (iq % 4) .. + 3
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int w = 0; w < kF32Waves; ++w) {
+    for (int w = 0; w < W; ++w) {
       const f32x4 v = *reinterpret_cast<const f32x4 *>(&merge[w][(iq * 64 + lane) * 4]);
 #pragma unroll
       for (int e = 0; e < 4; ++e) o[e] = fmaf(v[e], mw[w], o[e]);
@@ -691,25 +708,19 @@ __global__ __launch_bounds__(256) void walk_combine(WalkArgs a) {
   }
 }
 
+template <int DB, bool TREE>
+void launch_f32(const WalkArgs &a, hipStream_t st) {
+  hipLaunchKernelGGL((walk_attn_f32<DB, TREE>), dim3(8 * a.slots), dim3(64 * kF32Waves), 0, st, a);
+  if (a.cslots) hipLaunchKernelGGL((walk_combine<DB, false>), dim3(8 * a.cslots), dim3(256), 0, st, a);
+}
+
 template <bool TREE>
 void launch_f32(const WalkArgs &a, hipStream_t st) {
-  const dim3 grid(8 * a.slots), block(64 * kF32Waves), cgrid(8 * a.cslots);
   switch ((a.head_dim + 31) / 32) {
-    case 1:
-      hipLaunchKernelGGL((walk_attn_f32<1, TREE>), grid, block, 0, st, a);
-      if (a.cslots) hipLaunchKernelGGL((walk_combine<1, false>), cgrid, dim3(256), 0, st, a);
-      break;
-    case 2:
-      hipLaunchKernelGGL((walk_attn_f32<2, TREE>), grid, block, 0, st, a);
-      if (a.cslots) hipLaunchKernelGGL((walk_combine<2, false>), cgrid, dim3(256), 0, st, a);
-      break;
-    case 3:
-      hipLaunchKernelGGL((walk_attn_f32<3, TREE>), grid, block, 0, st, a);
-      if (a.cslots) hipLaunchKernelGGL((walk_combine<3, false>), cgrid, dim3(256), 0, st, a);
-      break;
-    default:
-      hipLaunchKernelGGL((walk_attn_f32<4, TREE>), grid, block, 0, st, a);
-      if (a.cslots) hipLaunchKernelGGL((walk_combine<4, false>), cgrid, dim3(256), 0, st, a);
+    case 1: return launch_f32<1, TREE>(a, st);
+    case 2: return launch_f32<2, TREE>(a, st);
+    case 3: return launch_f32<3, TREE>(a, st);
+    default: return launch_f32<4, TREE>(a, st);
   }
 }
 
