@@ -378,11 +378,11 @@ typedef struct {
  * out may not overlap q (both are ignored where no sequence brings a token).
  * prefix: NULL for none.  scale, dtypes, head_dim and
  * slab limits are those of specmemo_tree_attn (a prefix is at most 2^23 rows
- * too), and L_b + T_b <= seq_cap[b].  The lengths are the caller's to advance
+ * too, and cap_total under 2^40), and L_b + T_b <= seq_cap[b].  The lengths are the caller's to advance
  * afterwards: the call writes `out` alone.  kv->seq_len is not read.
  * ws: specmemo_prompt_attn_bytes(...) bytes, 16-byte aligned (the parts of rows
  * whose keys are walked by several work items, and the descriptors of more than
- * 48 ranges of rows; may be 0). */
+ * 76 ranges of rows; may be 0). */
 int specmemo_prompt_attn(specmemo_dtype dt, int32_t B, const int32_t *new_off_h, const specmemo_kv *kv,
                          const specmemo_prefix *prefix, int32_t n_q, float scale, const void *q, void *out, void *ws,
                          size_t ws_bytes, void *stream);

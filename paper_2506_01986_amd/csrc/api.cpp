@@ -790,6 +790,7 @@ int check_walk(int dt, const TreeInfo &ti, const int32_t *off_h, const specmemo_
   int rc;
   if ((rc = check_kv(dt, kv, ti, off_h))) return rc;
   if (n_q < 1 || n_q % kv->n_kv) return fail(SPECMEMO_E_ARG, "n_q=%d must be a positive multiple of n_kv=%d", n_q, kv->n_kv);
+  if (kv->cap_total >= INT64_C(1) << 40) return fail(SPECMEMO_E_ARG, "cap_total=%lld, under 2^40 expected", (long long)kv->cap_total);
   for (int b = 0; b < ti.B; ++b) {
     if (dt == SPECMEMO_BF16 && kv->seq_cap_h[b] > kMaxSlabRows)
       return fail(SPECMEMO_E_BUDGET, "seq_cap[%d]=%d exceeds %d rows", b, kv->seq_cap_h[b], kMaxSlabRows);
@@ -834,7 +835,7 @@ WalkPlan make_walk(int dt, bool causal, const TreeInfo &ti, const int32_t *off_h
 }
 
 size_t walk_table_bytes(const WalkPlan &p) {
-  return p.sets.size() > (size_t)kMaxWalkSets ? align256(p.sets.size() * sizeof(WalkSet)) : 0;
+  return p.sets.size() > (size_t)kMaxWalkSets ? align256(p.sets.size() * sizeof(WalkSetPacked)) : 0;
 }
 size_t walk_ws_bytes(const WalkPlan &p, int head_dim) {
   return walk_table_bytes(p) +
@@ -875,9 +876,9 @@ int run_walk(int dt, bool tree, const TreeInfo &ti, const int32_t *off_h, const 
   uint8_t *w = static_cast<uint8_t *>(ws);
   const size_t tab = walk_table_bytes(p);
   if (tab) {
-    hipError_t e = upload_table(p.sets.data(), p.sets.size() * sizeof(WalkSet), w, st);
+    hipError_t e = upload_table(p.sets.data(), p.sets.size() * sizeof(WalkSetPacked), w, st);
     if (e != hipSuccess) return hip_status(e, "descriptor upload");
-    a.tab = reinterpret_cast<const WalkSet *>(w);
+    a.tab = reinterpret_cast<const WalkSetPacked *>(w);
   } else {
     std::copy(p.sets.begin(), p.sets.end(), a.set);
   }

@@ -154,7 +154,15 @@ struct WalkSet {
   uint8_t slab;          // slab rows are walked (0: the prefix alone, for the packed rows of a run of sequences)
   uint8_t parts;         // every item is merged
 };
-constexpr int kMaxWalkSets = 48;   // sets described in the kernel arguments
+// The same as it travels: what follows from the rest is computed by walk_expand.
+struct WalkSetPacked {
+  uint32_t base_lo, pbase_lo;
+  uint8_t base_hi, pbase_hi;   // a pool has under 2^40 rows
+  uint8_t rb32;                // row block in units of 32 rows
+  uint8_t flags;               // 1 causal, 2 slab, 4 parts
+  int32_t L, T, P, row0, ct, items, cum, part0, ccum, shared;
+};
+constexpr int kMaxWalkSets = 76;   // sets described in the kernel arguments
 
 struct WalkArgs {
   const void *q;
@@ -162,13 +170,13 @@ struct WalkArgs {
   const void *k, *v;
   const int32_t *parent;
   float *part;
-  const WalkSet *tab;      // more than kMaxWalkSets sets: in the workspace
+  const WalkSetPacked *tab;   // more than kMaxWalkSets sets: in the workspace
   int64_t cap_total;
   int32_t n_q, n_kv, group, head_dim;
   int32_t units, fan;      // virtual units of a set on each XCD; shares of a KV head's items
   int32_t nset, slots, cslots;   // item and merge slots of one XCD
   float scale_log2;        // scale * log2(e)
-  WalkSet set[kMaxWalkSets];
+  WalkSetPacked set[kMaxWalkSets];
 };
 static_assert(sizeof(WalkArgs) <= 4096, "kernel arguments are limited to 4 KB");
 
@@ -197,6 +205,30 @@ __host__ __device__ inline int walk_first_rb(const WalkSet &s, int c, int g) {
 __host__ __device__ inline bool walk_direct(const WalkSet &s, int rb, int g) {
   return !s.parts && (s.part0 < 0 || walk_chunks(s, rb, g) == 1);
 }
+__host__ __device__ inline WalkSet walk_expand(const WalkSetPacked &p, int g) {
+  WalkSet s;
+  s.base = (int64_t)((uint64_t)p.base_hi << 32 | p.base_lo);
+  s.pbase = (int64_t)((uint64_t)p.pbase_hi << 32 | p.pbase_lo);
+  s.L = p.L;
+  s.T = p.T;
+  s.P = p.P;
+  s.row0 = p.row0;
+  s.rb = 32 * p.rb32;
+  s.ct = p.ct;
+  s.items = p.items;
+  s.cum = p.cum;
+  s.part0 = p.part0;
+  s.ccum = p.ccum;
+  s.shared = p.shared;
+  s.causal = p.flags & 1;
+  s.slab = p.flags >> 1 & 1;
+  s.parts = p.flags >> 2 & 1;
+  s.nrb = (s.T * g + s.rb - 1) / s.rb;
+  s.nch = walk_chunks(s, s.nrb - 1, g);
+  s.cunit0 = !s.parts && s.causal && s.part0 >= 0 ? walk_first_rb(s, 1, g) * p.rb32 : 0;
+  s.citems = s.slab && s.part0 >= 0 ? (s.T * g + 31) / 32 - s.cunit0 : 0;
+  return s;
+}
 // 4-byte words of a part of 32 rows: O in fp32, m and l
 __host__ __device__ constexpr int walk_unit_floats(int dblocks) { return 32 * 32 * dblocks + 64; }
 hipError_t launch_walk_attn(int dt, bool tree, const WalkArgs &a, hipStream_t st);
@@ -210,7 +242,7 @@ struct WalkPlan {
   int fan = 1, units = 1;
   int64_t slots = 0, cslots = 0;   // of one XCD
   int64_t parts = 0;               // 32-row units
-  std::vector<WalkSet> sets;
+  std::vector<WalkSetPacked> sets;
 };
 void plan_walk(int dt, bool causal, const std::vector<WalkSeq> &seqs, int n_kv, int group, int head_dim, int cus,
                WalkPlan *p);

@@ -68,8 +68,8 @@ __device__ __forceinline__ int find_set(const WalkArgs &a, int k) {
 // Set s, in SGPRs (the direct loads need their base there): from the arguments by
 // scalar loads, from the workspace table one word a lane.
 __device__ __forceinline__ WalkSet get_set(const WalkArgs &a, int s) {
-  constexpr int N = sizeof(WalkSet) / 4;
-  static_assert(sizeof(WalkSet) % 4 == 0 && N <= 64, "copied by words");
+  constexpr int N = sizeof(WalkSetPacked) / 4;
+  static_assert(sizeof(WalkSetPacked) % 4 == 0 && N <= 64, "copied by words");
   s = __builtin_amdgcn_readfirstlane(s);
   int w[N];
   if (a.tab) {
@@ -81,9 +81,9 @@ __device__ __forceinline__ WalkSet get_set(const WalkArgs &a, int s) {
 #pragma unroll
     for (int i = 0; i < N; ++i) w[i] = p[i];
   }
-  WalkSet S;
-  __builtin_memcpy(&S, w, sizeof(S));
-  return S;
+  WalkSetPacked P;
+  __builtin_memcpy(&P, w, sizeof(P));
+  return walk_expand(P, a.group);
 }
 
 // Block 8 k + x is the k-th block of XCD x (blocks reach the eight XCDs

@@ -177,12 +177,25 @@ void plan_walk(int dt, bool causal, const std::vector<WalkSeq> &seqs, int n_kv, 
       part += (int64_t)s.items * n_kv * (s.rb / 32);
     }
     s.ccum = (int)cslot;
-    if (s.slab && s.part0 >= 0) {
-      if (!s.parts && s.causal) s.cunit0 = walk_first_rb(s, 1, g) * (s.rb / 32);
-      s.citems = ceil_div((int64_t)s.T * g, 32) - s.cunit0;
-      cslot += (int64_t)ceil_div(s.citems, fan) * units;
-    }
-    p->sets.push_back(s);
+    WalkSetPacked q{};
+    q.base_lo = (uint32_t)s.base;
+    q.base_hi = (uint8_t)(s.base >> 32);
+    q.pbase_lo = (uint32_t)s.pbase;
+    q.pbase_hi = (uint8_t)(s.pbase >> 32);
+    q.rb32 = (uint8_t)(s.rb / 32);
+    q.flags = (uint8_t)(s.causal | s.slab << 1 | s.parts << 2);
+    q.L = s.L;
+    q.T = s.T;
+    q.P = s.P;
+    q.row0 = s.row0;
+    q.ct = s.ct;
+    q.items = s.items;
+    q.cum = s.cum;
+    q.part0 = s.part0;
+    q.ccum = s.ccum;
+    q.shared = s.shared;
+    p->sets.push_back(q);
+    cslot += (int64_t)ceil_div(walk_expand(q, g).citems, fan) * units;
   }
   p->slots = slot;
   p->cslots = cslot;

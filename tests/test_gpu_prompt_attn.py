@@ -53,8 +53,10 @@ BF16 = {
     "prefix_decode": (32, 4, [1] * 12, draw(1, 90, 12), [700] * 12, [0] * 12),
     "prefix_mixed": (8, 8, [5, 90, 0, 4, 4, 1], [3, 0, 9, 64, 0, 12], [64, 64, 64, 0, 129, 129], [0, 0, 0, 1, 2, 2]),
     "prefix_long_prompts": (8, 1, [300, 200], [0, 70], [513, 513], [0, 0]),
-    "many": (4, 2, draw(2, 30, 60), draw(3, 200, 60), None, None),     # more sets than the arguments hold
-    "many_prefixes": (4, 1, draw(4, 9, 70), draw(5, 60, 70), [40] * 70, [i // 2 for i in range(70)]),
+    "most_in_arguments": (4, 2, draw(2, 30, 70) + [1] * 6, draw(3, 200, 76), None, None),
+    "many": (4, 2, draw(2, 30, 90), draw(3, 200, 90), None, None),     # more sets than the arguments hold
+    "many_prefixes": (4, 1, draw(4, 9, 100), draw(5, 60, 100), [40] * 100, [i // 2 for i in range(100)]),
+    "many_packed": (4, 8 // 4, [1] * 90, draw(6, 60, 90), [800] * 90, [i // 30 for i in range(90)]),
 }
 
 

@@ -51,7 +51,7 @@ CASES = {
     "two_groups": ("t16", 8, 1, [5, 9, 0, 64, 30, 2], [200, 200, 200, 77, 77, 77], [0, 0, 0, 1, 1, 1]),
     "apart": ("t16", 8, 2, [5, 9, 0, 64], [200, 64, 200, 64], [0, 1, 0, 1]),        # neighbours differ: nothing is packed
     "some_without": ("random", 5, 1, [5, 9, 0, 64, 20], [90, 90, 0, 90, 90], [0, 0, 1, 0, 0]),
-    "many": ("t16", 4, 2, [int(v) for v in np.random.default_rng(6).integers(0, 60, 70)], [100] * 70, [i // 7 for i in range(70)]),
+    "many": ("t16", 4, 2, [int(v) for v in np.random.default_rng(6).integers(0, 60, 90)], [600] * 90, [i // 30 for i in range(90)]),
 }
 
 

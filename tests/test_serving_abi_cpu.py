@@ -53,20 +53,21 @@ def test_prompt_workspace():
     assert sm.prompt_attn_bytes(sm.BF16, [0, 1], FakeKV([5], [60], [0]), 4) == 0         # one chunk
     assert sm.prompt_attn_bytes(sm.BF16, [0, 99], FakeKV([5], [60], [0]), 4) == 0        # invalid
     # more sets than the kernel arguments describe: the table is in the workspace
-    many = FakeKV([5] * 60, [10] * 60, [10 * i for i in range(60)])
-    assert sm.prompt_attn_bytes(sm.BF16, list(range(61)), many, 4) >= 60 * 80
+    many = FakeKV([5] * 90, [10] * 90, [10 * i for i in range(90)])
+    assert sm.prompt_attn_bytes(sm.BF16, list(range(91)), many, 4) >= 90 * 52
+    assert sm.prompt_attn_bytes(sm.BF16, list(range(77)), many, 4) == 0
 
 
 @cpu_only
 def test_prefix():
-    kv = FakeKV([10, 0], [40, 40], [100, 150], cap_total=200)
+    kv = FakeKV([10, 0], [40, 40], [9000, 9050], cap_total=9100)
     ok = dict(ws=None, ws_bytes=0)                                      # a valid call would stop at its workspace
     bad = lambda base, n: expect("E_BUDGET", prompt, [0, 3, 5], kv, prefix=sm.Prefix(base, n))
-    expect("E_WORKSPACE", prompt, [0, 1, 2], kv, prefix=sm.Prefix([0, 0], [100, 100]), **ok)
-    expect("E_WORKSPACE", prompt, [0, 1, 2], kv, prefix=sm.Prefix([0, 0], [110, 110]), **ok)   # with committed rows of slab 0
-    bad([0, 0], [111, 111])                                             # its eleventh row is not committed
-    bad([0, 150], [5, 1])                                               # slab 1 has none
-    bad([0, 195], [5, 6])                                               # past the pool
+    expect("E_WORKSPACE", prompt, [0, 1, 2], kv, prefix=sm.Prefix([0, 0], [9000, 9000]), **ok)
+    expect("E_WORKSPACE", prompt, [0, 1, 2], kv, prefix=sm.Prefix([0, 0], [9010, 9010]), **ok)   # with committed rows of slab 0
+    bad([0, 0], [9011, 9011])                                           # its eleventh row is not committed
+    bad([0, 9050], [5, 1])                                              # slab 1 has none
+    bad([0, 9095], [5, 6])                                              # past the pool
     bad([-1, 0], [5, 5])
     bad([2 ** 63 - 5, 0], [5, 5])
     expect("E_ARG", prompt, [0, 3, 5], kv, prefix=sm.Prefix([0, 0], [-1, 5]))
@@ -81,24 +82,24 @@ def test_prefix():
 @cpu_only
 def test_tree_prefix():
     t = FakeTrees([synth.t16(), synth.t16()])
-    kv = FakeKV([10, 0], [40, 40], [100, 150], cap_total=200)
+    kv = FakeKV([10, 0], [40, 40], [9000, 9050], cap_total=9100)
 
-    def call(trees=t, pool=kv, px=sm.Prefix([0, 0], [90, 90]), n_q=4, q=FAKE, ws=FAKE, ws_bytes=1 << 34, dt=sm.BF16):
+    def call(trees=t, pool=kv, px=sm.Prefix([0, 0], [8000, 8000]), n_q=4, q=FAKE, ws=FAKE, ws_bytes=1 << 34, dt=sm.BF16):
         sm.tree_attn_prefix(dt, trees, pool, px, n_q, q, FAKE, ws=ws, ws_bytes=ws_bytes, stream=0)
 
-    need = sm.tree_attn_prefix_bytes(sm.BF16, t, kv, sm.Prefix([0, 0], [90, 90]), 4)
+    need = sm.tree_attn_prefix_bytes(sm.BF16, t, kv, sm.Prefix([0, 0], [8000, 8000]), 4)
     assert need > 0
     expect("E_WORKSPACE", call, ws_bytes=need - 1)
     expect("E_ARG", call, px=None)
     expect("E_ARG", call, q=FAKE + 2)
     expect("E_ARG", call, n_q=5)
     expect("E_DTYPE", call, dt=3)
-    expect("E_BUDGET", call, pool=FakeKV([30, 0], [40, 40], [100, 150], cap_total=200))
-    expect("E_BUDGET", call, px=sm.Prefix([0, 0], [90, 111]))
+    expect("E_BUDGET", call, pool=FakeKV([30, 0], [40, 40], [9000, 9050], cap_total=9100))
+    expect("E_BUDGET", call, px=sm.Prefix([0, 0], [8000, 9011]))
     bad = synth.t16()
     bad.parent[5] = 7
     expect("E_TREE", call, trees=FakeTrees([bad, synth.t16()]))
-    assert sm.tree_attn_prefix_bytes(sm.BF16, t, kv, sm.Prefix([0, 0], [90, 111]), 4) == 0
+    assert sm.tree_attn_prefix_bytes(sm.BF16, t, kv, sm.Prefix([0, 0], [8000, 9011]), 4) == 0
 
 
 def test_null_host_arrays():
