@@ -354,7 +354,9 @@ int specmemo_kv_pad_update(specmemo_dtype dt, const specmemo_trees *t, const spe
  * with the same text need its K/V once.  A prefix is a range of pool rows that
  * a sequence sees before its own slab rows: rows of their own, or committed rows
  * of a slab.  Every K/V row that a call walks, masked for some query or not, must
- * be finite; rows past a sequence's last one are never read. */
+ * be finite; rows past a sequence's last one are never read.  Buffers and stream
+ * belong to the current device.  A workspace is scratch of one call: calls, or
+ * captured graphs, that can overlap need one each. */
 
 /* Per sequence, host arrays [B]: first pool row and rows of its prefix (0 rows:
  * none).  Sequences that follow one another in the batch with the same base and
@@ -377,8 +379,8 @@ typedef struct {
  * SPECMEMO_MAX_BATCH.  q, out: device [new_off_h[B]][n_q][head_dim] in `dt`;
  * out may not overlap q (both are ignored where no sequence brings a token).
  * prefix: NULL for none.  scale, dtypes, head_dim and
- * slab limits are those of specmemo_tree_attn (a prefix is at most 2^23 rows
- * too, and cap_total under 2^40), and L_b + T_b <= seq_cap[b].  The lengths are the caller's to advance
+ * slab limits are those of specmemo_tree_attn (a bf16 prefix is at most 2^23
+ * rows too, and cap_total under 2^40), and L_b + T_b <= seq_cap[b].  The lengths are the caller's to advance
  * afterwards: the call writes `out` alone.  kv->seq_len is not read.
  * ws: specmemo_prompt_attn_bytes(...) bytes, 16-byte aligned (the parts of rows
  * whose keys are walked by several work items, and the descriptors of more than

@@ -12,6 +12,7 @@
 #include <cstdlib>
 #include <numeric>
 #include <string>
+#include <utility>
 #include <vector>
 
 #include "internal.h"
@@ -753,6 +754,16 @@ int specmemo_tree_attn_padded(specmemo_dtype dt, const specmemo_trees *t, const 
 
 namespace {
 
+// The host planning allocates; nothing is thrown through the C entry points.
+template <class F>
+auto guarded(decltype(std::declval<F>()()) on_throw, F f) noexcept -> decltype(f()) {
+  try {
+    return f();
+  } catch (...) {
+    return on_throw;
+  }
+}
+
 // A prefix must lie in the pool, and where it reaches into a slab, in its committed rows.
 int check_prefix(const specmemo_prefix *px, const specmemo_kv *kv, int dt, int B) {
   if (!px) return SPECMEMO_OK;
@@ -767,8 +778,8 @@ int check_prefix(const specmemo_prefix *px, const specmemo_kv *kv, int dt, int B
     if (base < 0 || base > kv->cap_total - len)
       return fail(SPECMEMO_E_BUDGET, "sequence %d: prefix of %lld rows at %lld outside the pool of %lld rows", b,
                   (long long)len, (long long)base, (long long)kv->cap_total);
-    if (dt == SPECMEMO_BF16 && len > kMaxSlabRows)
-      return fail(SPECMEMO_E_BUDGET, "sequence %d: prefix of %lld rows exceeds %d", b, (long long)len, kMaxSlabRows);
+    const int64_t most = dt == SPECMEMO_BF16 ? kMaxSlabRows : INT32_MAX / 2;   // tile numbers and row offsets in 32 bits
+    if (len > most) return fail(SPECMEMO_E_BUDGET, "sequence %d: prefix of %lld rows exceeds %lld", b, (long long)len, (long long)most);
     if (b > 0 && base == px->base_h[b - 1] && len == px->len_h[b - 1]) continue;
     // the slabs that begin before the prefix ends, from the last one back to the prefix's start
     auto it = std::lower_bound(order.begin(), order.end(), base + len, [&](int s, int64_t v) { return kv->seq_base_h[s] < v; });
@@ -849,6 +860,8 @@ int run_walk(int dt, bool tree, const TreeInfo &ti, const int32_t *off_h, const 
   if (!std::isfinite(scale)) return fail(SPECMEMO_E_ARG, "scale is not finite");
   if (ti.total == 0) return ok();
   if (!al(q, 16) || !al(out, 16)) return fail(SPECMEMO_E_ARG, "q / out must be non-NULL and 16-byte aligned");
+  const size_t bytes = (size_t)ti.total * n_q * kv->head_dim * (dt == SPECMEMO_BF16 ? 2 : 4);
+  if ((uintptr_t)q < (uintptr_t)out + bytes && (uintptr_t)out < (uintptr_t)q + bytes) return fail(SPECMEMO_E_ARG, "out overlaps q");
   const WalkPlan p = make_walk(dt, !tree, ti, off_h, kv, px, n_q);
   if (p.slots > INT32_MAX / 8 || p.cslots > INT32_MAX / 8 || p.parts > INT32_MAX)
     return fail(SPECMEMO_E_ARG, "too many work items: %lld", (long long)p.slots);
@@ -901,33 +914,41 @@ extern "C" {
 int specmemo_prompt_attn(specmemo_dtype dt, int32_t B, const int32_t *new_off_h, const specmemo_kv *kv,
                          const specmemo_prefix *prefix, int32_t n_q, float scale, const void *q, void *out, void *ws,
                          size_t ws_bytes, void *stream) {
-  TreeInfo ti;
-  const int rc = check_prompt(dt, B, new_off_h, kv, prefix, n_q, &ti);
-  if (rc) return rc;
-  return run_walk(dt, false, ti, new_off_h, nullptr, kv, prefix, n_q, scale, q, out, ws, ws_bytes, stream);
+  return guarded((int)SPECMEMO_E_ARG, [&] {
+    TreeInfo ti;
+    const int rc = check_prompt(dt, B, new_off_h, kv, prefix, n_q, &ti);
+    if (rc) return rc;
+    return run_walk(dt, false, ti, new_off_h, nullptr, kv, prefix, n_q, scale, q, out, ws, ws_bytes, stream);
+  });
 }
 
 size_t specmemo_prompt_attn_bytes(specmemo_dtype dt, int32_t B, const int32_t *new_off_h, const specmemo_kv *kv,
                                   const specmemo_prefix *prefix, int32_t n_q) {
-  TreeInfo ti;
-  if (check_prompt(dt, B, new_off_h, kv, prefix, n_q, &ti)) return 0;
-  return walk_ws_bytes(make_walk(dt, true, ti, new_off_h, kv, prefix, n_q), kv->head_dim);
+  return guarded((size_t)0, [&] {
+    TreeInfo ti;
+    if (check_prompt(dt, B, new_off_h, kv, prefix, n_q, &ti)) return (size_t)0;
+    return walk_ws_bytes(make_walk(dt, true, ti, new_off_h, kv, prefix, n_q), kv->head_dim);
+  });
 }
 
 int specmemo_tree_attn_prefix(specmemo_dtype dt, const specmemo_trees *t, const specmemo_kv *kv,
                               const specmemo_prefix *prefix, int32_t n_q, float scale, const void *q, void *out, void *ws,
                               size_t ws_bytes, void *stream) {
-  TreeInfo ti;
-  const int rc = check_tree_prefix(dt, t, kv, prefix, n_q, &ti);
-  if (rc) return rc;
-  return run_walk(dt, true, ti, t->node_off_h, t->parent, kv, prefix, n_q, scale, q, out, ws, ws_bytes, stream);
+  return guarded((int)SPECMEMO_E_ARG, [&] {
+    TreeInfo ti;
+    const int rc = check_tree_prefix(dt, t, kv, prefix, n_q, &ti);
+    if (rc) return rc;
+    return run_walk(dt, true, ti, t->node_off_h, t->parent, kv, prefix, n_q, scale, q, out, ws, ws_bytes, stream);
+  });
 }
 
 size_t specmemo_tree_attn_prefix_bytes(specmemo_dtype dt, const specmemo_trees *t, const specmemo_kv *kv,
                                        const specmemo_prefix *prefix, int32_t n_q) {
-  TreeInfo ti;
-  if (check_tree_prefix(dt, t, kv, prefix, n_q, &ti)) return 0;
-  return walk_ws_bytes(make_walk(dt, false, ti, t->node_off_h, kv, prefix, n_q), kv->head_dim);
+  return guarded((size_t)0, [&] {
+    TreeInfo ti;
+    if (check_tree_prefix(dt, t, kv, prefix, n_q, &ti)) return (size_t)0;
+    return walk_ws_bytes(make_walk(dt, false, ti, t->node_off_h, kv, prefix, n_q), kv->head_dim);
+  });
 }
 
 int specmemo_accept(specmemo_dtype dt, const specmemo_trees *t, int32_t vocab, specmemo_accept_mode mode,

@@ -130,6 +130,30 @@ def test_prefix_in_committed_rows():
     check(x.out, *x.reference(lambda b: causal(x.n[b])))
 
 
+def test_nested_prefixes():
+    """Prefixes of one base and different lengths."""
+    x = Batch("bf16", 4, 2, 128, [9, 4, 30], [20, 11, 0], [100] * 3, [0] * 3, seed=6).upload()
+    x.plen = [100, 60, 64]
+    x.px = sm.Prefix(x.pbase, x.plen)
+    check(run(x), *x.reference(lambda b: causal(x.n[b])))
+
+
+@pytest.mark.parametrize("dtype,rows", [("bf16", 9_000_000), ("fp32", 5_000_000)])
+def test_far_slabs(dtype, rows):
+    """Slabs and prefix more than 2^32 bytes into the pool, in every KV head."""
+    x = Batch(dtype, 4, 2, 128, [70, 1], [200, 500], [90, 90], [0, 0], seed=7).upload()
+    small = [x.kd, x.vd]
+    for name, t in (("kd", x.kd), ("vd", x.vd)):
+        big = torch.empty(2, 2 * rows, 128, dtype=t.dtype, device="cuda")
+        big[:, 2 * rows - t.shape[1]:] = t
+        setattr(x, name, big)
+    shift = 2 * rows - small[0].shape[1]
+    assert shift * 128 * x.kd.element_size() > 2 ** 32
+    x.kv = sm.KVPool(x.kd, x.vd, x.kv.seq_len, [b + shift for b in x.base], x.cap, x.L)
+    x.px = sm.Prefix([b + shift for b in x.pbase], x.plen)
+    check(run(x), *x.reference(lambda b: causal(x.n[b])))
+
+
 @pytest.mark.parametrize("name", ["prefix_mixed", "one_long_gqa", "many"])
 def test_captured_and_on_another_stream(name):
     """A captured call, replayed between eager calls on other data, gives the eager result every time."""

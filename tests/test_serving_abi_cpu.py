@@ -9,7 +9,7 @@ from paper_2506_01986_amd import synth
 from tests.test_abi_cpu import FAKE, FakeKV, FakeTrees, cpu_only, expect
 
 
-def prompt(off, kv, n_q=4, dt=sm.BF16, q=FAKE, out=FAKE, ws=FAKE, ws_bytes=1 << 34, prefix=None, scale=0.0):
+def prompt(off, kv, n_q=4, dt=sm.BF16, q=FAKE, out=FAKE * 2, ws=FAKE, ws_bytes=1 << 34, prefix=None, scale=0.0):
     sm.prompt_attn(dt, off, kv, n_q, q, out, prefix=prefix, scale=scale, ws=ws, ws_bytes=ws_bytes, stream=0)
 
 
@@ -25,7 +25,9 @@ def test_prompt_arguments():
     expect("E_ARG", prompt, [0, 3, 5], kv, n_q=3)
     expect("E_ARG", prompt, [0, 3, 5], kv, n_q=0)
     expect("E_ARG", prompt, [0, 3, 5], kv, q=None)
-    expect("E_ARG", prompt, [0, 3, 5], kv, out=FAKE + 8)
+    expect("E_ARG", prompt, [0, 3, 5], kv, out=FAKE * 2 + 8)
+    assert "overlaps" in expect("E_ARG", prompt, [0, 3, 5], kv, out=FAKE + 4096)
+    assert "overlaps" in expect("E_ARG", prompt, [0, 3, 5], kv, out=FAKE)
     expect("E_ARG", prompt, [0, 3, 5], kv, scale=float("inf"))
     expect("E_ARG", prompt, [0] * 4098, FakeKV([0] * 4097, [0] * 4097, [0] * 4097, cap_total=10))
     with pytest.raises(ValueError):
@@ -73,6 +75,9 @@ def test_prefix():
     expect("E_ARG", prompt, [0, 3, 5], kv, prefix=sm.Prefix([0, 0], [-1, 5]))
     big = FakeKV([10, 0], [40, 40], [1 << 24, (1 << 24) + 50])
     expect("E_BUDGET", prompt, [0, 3, 5], big, prefix=sm.Prefix([0, 0], [(1 << 23) + 1] * 2))
+    huge = FakeKV([10], [40], [1 << 31], d=4, cap_total=1 << 32)
+    expect("E_BUDGET", prompt, [0, 3], huge, dt=sm.FP32, prefix=sm.Prefix([0], [2 ** 31 - 1]))
+    expect("E_ARG", prompt, [0, 3], FakeKV([10], [40], [0], cap_total=1 << 40))
     with pytest.raises(ValueError):
         prompt([0, 3, 5], kv, prefix=sm.Prefix([0], [5]))
     with pytest.raises(ValueError):
@@ -85,7 +90,7 @@ def test_tree_prefix():
     kv = FakeKV([10, 0], [40, 40], [9000, 9050], cap_total=9100)
 
     def call(trees=t, pool=kv, px=sm.Prefix([0, 0], [8000, 8000]), n_q=4, q=FAKE, ws=FAKE, ws_bytes=1 << 34, dt=sm.BF16):
-        sm.tree_attn_prefix(dt, trees, pool, px, n_q, q, FAKE, ws=ws, ws_bytes=ws_bytes, stream=0)
+        sm.tree_attn_prefix(dt, trees, pool, px, n_q, q, FAKE * 2, ws=ws, ws_bytes=ws_bytes, stream=0)
 
     need = sm.tree_attn_prefix_bytes(sm.BF16, t, kv, sm.Prefix([0, 0], [8000, 8000]), 4)
     assert need > 0
@@ -109,9 +114,9 @@ def test_null_host_arrays():
     import ctypes as C
     off = np.array([0, 3], np.int32)
     px = sm._Prefix(None, None)
-    assert lib.specmemo_prompt_attn(1, 1, None, C.byref(kv), None, 4, 0.0, FAKE, FAKE, FAKE, 1 << 30, None) == -1
-    assert lib.specmemo_prompt_attn(1, 1, off.ctypes.data, None, None, 4, 0.0, FAKE, FAKE, FAKE, 1 << 30, None) == -1
-    assert lib.specmemo_prompt_attn(1, 1, off.ctypes.data, C.byref(kv), C.byref(px), 4, 0.0, FAKE, FAKE, FAKE, 1 << 30, None) == -1
+    assert lib.specmemo_prompt_attn(1, 1, None, C.byref(kv), None, 4, 0.0, FAKE, FAKE * 2, FAKE, 1 << 30, None) == -1
+    assert lib.specmemo_prompt_attn(1, 1, off.ctypes.data, None, None, 4, 0.0, FAKE, FAKE * 2, FAKE, 1 << 30, None) == -1
+    assert lib.specmemo_prompt_attn(1, 1, off.ctypes.data, C.byref(kv), C.byref(px), 4, 0.0, FAKE, FAKE * 2, FAKE, 1 << 30, None) == -1
 
 
 @cpu_only
