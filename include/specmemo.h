@@ -12,6 +12,10 @@
  *   specmemo_accept        (c) greedy / typical acceptance of the longest path
  *   specmemo_kv_compact    (d) in-place compaction of the accepted K/V
  *
+ * Around a step: specmemo_prompt_attn (the prompt's attention over the pool),
+ * specmemo_tree_attn_prefix ((b) over a prefix that sequences share) and
+ * specmemo_logit_rules (penalties, biases and masks before (c)).
+ *
  * Symbols follow the paper's memory model (Sec. 3.1): b = batch (B),
  * k = KV heads (n_kv), d = head dim (head_dim), x = KV length
  * (seq_len / seq_cap), l = Medusa heads = tree levels (n_heads),
