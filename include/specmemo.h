@@ -450,7 +450,7 @@ int specmemo_logit_rules(specmemo_dtype dt, const specmemo_trees *t, int32_t voc
  * (added to what counts holds where accumulate is nonzero); tokens outside
  * [0, vocab) are ignored.  tok_off: device int32 [B+1] with host mirror tok_off_h,
  * tok_off[0] = 0, non-decreasing; tokens: device int32 [tok_off[B]]; counts:
- * device int32 [B][vocab].  1 <= B <= SPECMEMO_MAX_BATCH. */
+ * device int32 [B][vocab].  1 <= B <= SPECMEMO_MAX_BATCH, tok_off[B] < 2^30. */
 int specmemo_token_counts(int32_t B, int32_t vocab, const int32_t *tok_off_h, const int32_t *tok_off,
                           const int32_t *tokens, int32_t *counts, int32_t accumulate, void *stream);
 

@@ -1054,6 +1054,7 @@ int specmemo_token_counts(int32_t B, int32_t vocab, const int32_t *tok_off_h, co
   if (tok_off_h[0] != 0) return fail(SPECMEMO_E_ARG, "tok_off[0]=%d, expected 0", tok_off_h[0]);
   for (int b = 0; b < B; ++b)
     if (tok_off_h[b + 1] < tok_off_h[b]) return fail(SPECMEMO_E_ARG, "tok_off[%d]=%d after %d", b + 1, tok_off_h[b + 1], tok_off_h[b]);
+  if (tok_off_h[B] > INT32_MAX / 2) return fail(SPECMEMO_E_ARG, "%d tokens, at most %d", tok_off_h[B], INT32_MAX / 2);   // positions in 32 bits
   if (!al(tok_off, 4) || !al(counts, 4) || (tok_off_h[B] > 0 && !al(tokens, 4)))
     return fail(SPECMEMO_E_ARG, "tok_off / tokens / counts must be non-NULL and 4-byte aligned");
   const CountArgs a{tok_off, tokens, counts, vocab, tok_off_h[B], accumulate};

@@ -155,6 +155,7 @@ def test_counts():
     expect("E_ARG", call, [0])
     expect("E_ARG", call, [1, 2])
     expect("E_ARG", call, [0, 3, 2])
+    assert "tokens" in expect("E_ARG", call, [0, 2 ** 30])              # 32-bit positions
     expect("E_ARG", call, [0, 3], vocab=0)
     expect("E_ARG", call, [0, 3], dev=None)
     expect("E_ARG", call, [0, 3], tok=None)
