@@ -863,8 +863,9 @@ int run_walk(int dt, bool tree, const TreeInfo &ti, const int32_t *off_h, const 
   const size_t bytes = (size_t)ti.total * n_q * kv->head_dim * (dt == SPECMEMO_BF16 ? 2 : 4);
   if ((uintptr_t)q < (uintptr_t)out + bytes && (uintptr_t)out < (uintptr_t)q + bytes) return fail(SPECMEMO_E_ARG, "out overlaps q");
   const WalkPlan p = make_walk(dt, !tree, ti, off_h, kv, px, n_q);
-  if (p.slots > INT32_MAX / 8 || p.cslots > INT32_MAX / 8 || p.parts > INT32_MAX)
-    return fail(SPECMEMO_E_ARG, "too many work items: %lld", (long long)p.slots);
+  constexpr int64_t most = UINT32_MAX / 256 / 8;   // on each XCD: a launch has at most 2^32 - 1 threads
+  if (p.slots > most || p.cslots > most || p.parts > INT32_MAX)
+    return fail(SPECMEMO_E_ARG, "too many work items: %lld", 8 * (long long)std::max(p.slots, p.cslots));
   const size_t need = walk_ws_bytes(p, kv->head_dim);
   if (need && (!al(ws, 16) || ws_bytes < need))
     return fail(SPECMEMO_E_WORKSPACE, "workspace of %zu bytes needed (16-byte aligned), got %zu", need, ws ? ws_bytes : 0);

@@ -45,6 +45,13 @@ def test_prompt_budget():
 
 
 @cpu_only
+def test_prompt_launch_size():
+    # 25.6 million work items of 256 threads: more threads than a launch's 32-bit count
+    kv = FakeKV([0], [200000], [0], d=4, cap_total=200000, n_kv=4096)
+    assert "work items" in expect("E_ARG", prompt, [0, 200000], kv, n_q=4096, dt=sm.FP32, out=1 << 45, ws_bytes=1 << 60)
+
+
+@cpu_only
 def test_prompt_workspace():
     kv = FakeKV([5000], [6000], [0])
     need = sm.prompt_attn_bytes(sm.BF16, [0, 1], kv, 4)
