@@ -149,7 +149,7 @@ void plan_walk(int dt, bool causal, const std::vector<WalkSeq> &seqs, int n_kv, 
     const int nt = walk_tiles(s, s.nrb - 1, g);
     const double full = std::min(1.0, (double)s.T * g / s.rb);
     const double limit = share * (1 + kFullSlack * full) + kChunkStart;
-    int nch = ceil_div(nt, std::max(1, (int)(limit / tile_us(s))));
+    int nch = ceil_div(nt, std::max(1, (int)std::min<double>(nt, limit / tile_us(s))));
     if (s.causal && s.nrb > 1) nch = std::min(nch, kMaxCausalChunks);
     s.ct = ceil_div(nt, nch);              // equal chunks; the count may drop by rounding
     s.nch = ceil_div(nt, s.ct);

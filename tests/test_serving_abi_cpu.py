@@ -68,6 +68,13 @@ def test_prompt_workspace():
 
 
 @cpu_only
+def test_plan_of_the_largest_prompt():
+    # more row blocks than block slots by far: nothing to split, whatever the amount of work
+    for n in (1 << 20, 1 << 28):
+        assert sm.prompt_attn_bytes(sm.FP32, [0, n], FakeKV([0], [n], [0], d=4, n_kv=1), 1) == 0
+
+
+@cpu_only
 def test_prefix():
     kv = FakeKV([10, 0], [40, 40], [9000, 9050], cap_total=9100)
     ok = dict(ws=None, ws_bytes=0)                                      # a valid call would stop at its workspace
