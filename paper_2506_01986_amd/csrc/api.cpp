@@ -760,6 +760,7 @@ auto guarded(decltype(std::declval<F>()()) on_throw, F f) noexcept -> decltype(f
   try {
     return f();
   } catch (...) {
+    (void)fail(SPECMEMO_E_ARG, "no host memory");   // 14 characters: a string holds them without allocating
     return on_throw;
   }
 }
@@ -1001,78 +1002,84 @@ int specmemo_sample_next(specmemo_dtype dt, const specmemo_trees *t, int32_t voc
 
 int specmemo_logit_rules(specmemo_dtype dt, const specmemo_trees *t, int32_t vocab, const specmemo_rules *rules,
                          const int32_t *node_tok, const void *logits, void *out, void *stream) {
-  int rc;
-  if ((rc = check_dtype(dt))) return rc;
-  TreeInfo ti;
-  if ((rc = check_trees(t, &ti))) return rc;
-  if (vocab < 1 || vocab > kMaxRulesVocab) return fail(SPECMEMO_E_ARG, "vocab=%d", vocab);
-  if (!rules) return fail(SPECMEMO_E_ARG, "rules is NULL");
-  if (!al(logits, 16) || !al(out, 16)) return fail(SPECMEMO_E_ARG, "logits / out must be non-NULL and 16-byte aligned");
-  const size_t bytes = (size_t)ti.total * vocab * (dt == SPECMEMO_BF16 ? 2 : 4);
-  const uintptr_t l0 = (uintptr_t)logits, o0 = (uintptr_t)out;
-  if (l0 != o0 && l0 < o0 + bytes && o0 < l0 + bytes) return fail(SPECMEMO_E_ARG, "out overlaps logits");
-  RulesArgs a{};
-  a.penalties = rules->repetition || rules->presence || rules->frequency;
-  for (const void *p : {(const void *)rules->counts, (const void *)rules->repetition, (const void *)rules->presence,
-                        (const void *)rules->frequency})
-    if (p && !al(p, 4)) return fail(SPECMEMO_E_ARG, "counts and penalties must be 4-byte aligned");
-  if (a.penalties && !al(node_tok, 4)) return fail(SPECMEMO_E_ARG, "node_tok must be non-NULL and 4-byte aligned");
-  if (rules->n_bias < 0 || rules->n_masks < 0)
-    return fail(SPECMEMO_E_ARG, "n_bias=%d n_masks=%d", rules->n_bias, rules->n_masks);
-  if (rules->n_bias > 0 && (!al(rules->bias_off, 4) || !al(rules->bias_id, 4) || !al(rules->bias_val, 4)))
-    return fail(SPECMEMO_E_ARG, "bias arrays must be non-NULL and 4-byte aligned");
-  if (rules->n_masks > 0) {
-    if (!al(rules->mask, 4) || !al(rules->mask_idx, 4)) return fail(SPECMEMO_E_ARG, "mask arrays must be non-NULL and 4-byte aligned");
-    if (rules->mask_words < (vocab - 1) / 32 + 1)
-      return fail(SPECMEMO_E_ARG, "mask_words=%d, %d needed", rules->mask_words, (vocab - 1) / 32 + 1);
-    a.mask = rules->mask;
-    a.mask_idx = rules->mask_idx;
-    a.n_masks = rules->n_masks;
-    a.mask_words = rules->mask_words;
-  }
-  a.logits = logits;
-  a.out = out;
-  a.node_off = t->node_off;
-  a.parent = t->parent;
-  a.node_tok = node_tok;
-  if (a.penalties) a.counts = rules->counts;
-  a.repetition = rules->repetition;
-  a.presence = rules->presence;
-  a.frequency = rules->frequency;
-  a.bias_off = rules->bias_off;
-  a.bias_id = rules->bias_id;
-  a.bias_val = rules->bias_val;
-  a.n_bias = rules->n_bias;
-  a.vocab = vocab;
-  return hip_status(launch_logit_rules(dt, a, ti.B, ti.max_nodes, static_cast<hipStream_t>(stream)), "logit rules launch");
+  return guarded((int)SPECMEMO_E_ARG, [&] {
+    int rc;
+    if ((rc = check_dtype(dt))) return rc;
+    TreeInfo ti;
+    if ((rc = check_trees(t, &ti))) return rc;
+    if (vocab < 1 || vocab > kMaxRulesVocab) return fail(SPECMEMO_E_ARG, "vocab=%d", vocab);
+    if (!rules) return fail(SPECMEMO_E_ARG, "rules is NULL");
+    if (!al(logits, 16) || !al(out, 16)) return fail(SPECMEMO_E_ARG, "logits / out must be non-NULL and 16-byte aligned");
+    const size_t bytes = (size_t)ti.total * vocab * (dt == SPECMEMO_BF16 ? 2 : 4);
+    const uintptr_t l0 = (uintptr_t)logits, o0 = (uintptr_t)out;
+    if (l0 != o0 && l0 < o0 + bytes && o0 < l0 + bytes) return fail(SPECMEMO_E_ARG, "out overlaps logits");
+    RulesArgs a{};
+    a.penalties = rules->repetition || rules->presence || rules->frequency;
+    for (const void *p : {(const void *)rules->counts, (const void *)rules->repetition, (const void *)rules->presence,
+                          (const void *)rules->frequency})
+      if (p && !al(p, 4)) return fail(SPECMEMO_E_ARG, "counts and penalties must be 4-byte aligned");
+    if (a.penalties && !al(node_tok, 4)) return fail(SPECMEMO_E_ARG, "node_tok must be non-NULL and 4-byte aligned");
+    if (rules->n_bias < 0 || rules->n_masks < 0)
+      return fail(SPECMEMO_E_ARG, "n_bias=%d n_masks=%d", rules->n_bias, rules->n_masks);
+    if (rules->n_bias > 0 && (!al(rules->bias_off, 4) || !al(rules->bias_id, 4) || !al(rules->bias_val, 4)))
+      return fail(SPECMEMO_E_ARG, "bias arrays must be non-NULL and 4-byte aligned");
+    if (rules->n_masks > 0) {
+      if (!al(rules->mask, 4) || !al(rules->mask_idx, 4)) return fail(SPECMEMO_E_ARG, "mask arrays must be non-NULL and 4-byte aligned");
+      if (rules->mask_words < (vocab - 1) / 32 + 1)
+        return fail(SPECMEMO_E_ARG, "mask_words=%d, %d needed", rules->mask_words, (vocab - 1) / 32 + 1);
+      a.mask = rules->mask;
+      a.mask_idx = rules->mask_idx;
+      a.n_masks = rules->n_masks;
+      a.mask_words = rules->mask_words;
+    }
+    a.logits = logits;
+    a.out = out;
+    a.node_off = t->node_off;
+    a.parent = t->parent;
+    a.node_tok = node_tok;
+    if (a.penalties) a.counts = rules->counts;
+    a.repetition = rules->repetition;
+    a.presence = rules->presence;
+    a.frequency = rules->frequency;
+    a.bias_off = rules->bias_off;
+    a.bias_id = rules->bias_id;
+    a.bias_val = rules->bias_val;
+    a.n_bias = rules->n_bias;
+    a.vocab = vocab;
+    return hip_status(launch_logit_rules(dt, a, ti.B, ti.max_nodes, static_cast<hipStream_t>(stream)), "logit rules launch");
+  });
 }
 
 int specmemo_token_counts(int32_t B, int32_t vocab, const int32_t *tok_off_h, const int32_t *tok_off,
                           const int32_t *tokens, int32_t *counts, int32_t accumulate, void *stream) {
-  if (B < 1 || B > SPECMEMO_MAX_BATCH) return fail(SPECMEMO_E_ARG, "B=%d outside [1, %d]", B, SPECMEMO_MAX_BATCH);
-  if (vocab < 1 || vocab > kMaxRulesVocab) return fail(SPECMEMO_E_ARG, "vocab=%d", vocab);
-  if (!tok_off_h) return fail(SPECMEMO_E_ARG, "tok_off_h is NULL");
-  if (tok_off_h[0] != 0) return fail(SPECMEMO_E_ARG, "tok_off[0]=%d, expected 0", tok_off_h[0]);
-  for (int b = 0; b < B; ++b)
-    if (tok_off_h[b + 1] < tok_off_h[b]) return fail(SPECMEMO_E_ARG, "tok_off[%d]=%d after %d", b + 1, tok_off_h[b + 1], tok_off_h[b]);
-  if (tok_off_h[B] > INT32_MAX / 2) return fail(SPECMEMO_E_ARG, "%d tokens, at most %d", tok_off_h[B], INT32_MAX / 2);   // positions in 32 bits
-  if (!al(tok_off, 4) || !al(counts, 4) || (tok_off_h[B] > 0 && !al(tokens, 4)))
-    return fail(SPECMEMO_E_ARG, "tok_off / tokens / counts must be non-NULL and 4-byte aligned");
-  const CountArgs a{tok_off, tokens, counts, vocab, tok_off_h[B], accumulate};
-  return hip_status(launch_token_counts(a, B, static_cast<hipStream_t>(stream)), "token counts launch");
+  return guarded((int)SPECMEMO_E_ARG, [&] {
+    if (B < 1 || B > SPECMEMO_MAX_BATCH) return fail(SPECMEMO_E_ARG, "B=%d outside [1, %d]", B, SPECMEMO_MAX_BATCH);
+    if (vocab < 1 || vocab > kMaxRulesVocab) return fail(SPECMEMO_E_ARG, "vocab=%d", vocab);
+    if (!tok_off_h) return fail(SPECMEMO_E_ARG, "tok_off_h is NULL");
+    if (tok_off_h[0] != 0) return fail(SPECMEMO_E_ARG, "tok_off[0]=%d, expected 0", tok_off_h[0]);
+    for (int b = 0; b < B; ++b)
+      if (tok_off_h[b + 1] < tok_off_h[b]) return fail(SPECMEMO_E_ARG, "tok_off[%d]=%d after %d", b + 1, tok_off_h[b + 1], tok_off_h[b]);
+    if (tok_off_h[B] > INT32_MAX / 2) return fail(SPECMEMO_E_ARG, "%d tokens, at most %d", tok_off_h[B], INT32_MAX / 2);   // positions in 32 bits
+    if (!al(tok_off, 4) || !al(counts, 4) || (tok_off_h[B] > 0 && !al(tokens, 4)))
+      return fail(SPECMEMO_E_ARG, "tok_off / tokens / counts must be non-NULL and 4-byte aligned");
+    const CountArgs a{tok_off, tokens, counts, vocab, tok_off_h[B], accumulate};
+    return hip_status(launch_token_counts(a, B, static_cast<hipStream_t>(stream)), "token counts launch");
+  });
 }
 
 int specmemo_count_accepted(const specmemo_trees *t, int32_t vocab, const int32_t *node_tok, const int32_t *accept_len,
                             const int32_t *path, int32_t path_stride, int32_t *counts, void *stream) {
-  TreeInfo ti;
-  int rc;
-  if ((rc = check_trees(t, &ti))) return rc;
-  if (vocab < 1 || vocab > kMaxRulesVocab) return fail(SPECMEMO_E_ARG, "vocab=%d", vocab);
-  if (path_stride < 1) return fail(SPECMEMO_E_ARG, "path_stride=%d", path_stride);
-  if (!al(node_tok, 4) || !al(accept_len, 4) || !al(path, 4) || !al(counts, 4))
-    return fail(SPECMEMO_E_ARG, "node_tok / accept_len / path / counts must be non-NULL and 4-byte aligned");
-  const AcceptedArgs a{t->node_off, node_tok, accept_len, path, counts, vocab, path_stride};
-  return hip_status(launch_count_accepted(a, ti.B, static_cast<hipStream_t>(stream)), "accepted counts launch");
+  return guarded((int)SPECMEMO_E_ARG, [&] {
+    TreeInfo ti;
+    int rc;
+    if ((rc = check_trees(t, &ti))) return rc;
+    if (vocab < 1 || vocab > kMaxRulesVocab) return fail(SPECMEMO_E_ARG, "vocab=%d", vocab);
+    if (path_stride < 1) return fail(SPECMEMO_E_ARG, "path_stride=%d", path_stride);
+    if (!al(node_tok, 4) || !al(accept_len, 4) || !al(path, 4) || !al(counts, 4))
+      return fail(SPECMEMO_E_ARG, "node_tok / accept_len / path / counts must be non-NULL and 4-byte aligned");
+    const AcceptedArgs a{t->node_off, node_tok, accept_len, path, counts, vocab, path_stride};
+    return hip_status(launch_count_accepted(a, ti.B, static_cast<hipStream_t>(stream)), "accepted counts launch");
+  });
 }
 
 }  // extern "C"
