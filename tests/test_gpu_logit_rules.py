@@ -209,6 +209,24 @@ def test_count_accepted():
     assert np.array_equal(counts.cpu().numpy(), want)
 
 
+def test_largest_batch():
+    """4096 trees of 128 nodes: as many rows as a call can bring."""
+    r = np.random.default_rng(9)
+    tree, B, vocab = synth.random_tree(r, 128), 4096, 21
+    off = np.arange(B + 1, dtype=np.int32) * 128
+    t = sm.Trees(off, *(np.tile(getattr(tree, f), B) for f in ("parent", "depth", "rank")), device="cuda")
+    z = torch.randn(B * 128, vocab, device="cuda")
+    bias = torch.randn(B, device="cuda")
+    ids = torch.arange(B, dtype=torch.int32, device="cuda") % vocab
+    rules = sm.LogitRules()
+    rules.set_bias(torch.arange(B + 1, dtype=torch.int32, device="cuda"), ids, bias)
+    want = z.view(B, 128, vocab).clone()
+    want[torch.arange(B, device="cuda"), :, ids.long()] += bias[:, None]
+    out = torch.empty_like(z)
+    sm.logit_rules(sm.FP32, t, vocab, z, None, rules, out)
+    assert torch.equal(out.view(B, 128, vocab), want)            # one fp32 addition, rounded once on both sides
+
+
 def test_captured():
     x = Case("bf16", 1003, trees("random"), seed=4, bias=20, masks=3)
     want = x.run()

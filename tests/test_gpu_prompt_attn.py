@@ -154,6 +154,34 @@ def test_far_slabs(dtype, rows):
     check(run(x), *x.reference(lambda b: causal(x.n[b])))
 
 
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("fp32", 4)])
+def test_largest_batch(dtype, d):
+    """4096 sequences of one or two tokens and four packed prefixes: three rounds of the search for a block's set."""
+    n = [1 + v for v in draw(11, 2, 4096)]
+    parity(Batch(dtype, 2, 1, d, n, draw(12, 20, 4096), [600] * 4096, [i // 1024 for i in range(4096)], seed=13))
+
+
+def test_two_calls_at_once():
+    """Calls on two streams, each with a workspace of its own, one of them with its table of sets there."""
+    xs = []
+    for name in ("many", "prefix_decode"):
+        n_q, n_kv, n, L, P, shared = BF16[name]
+        xs.append(Batch("bf16", n_q, n_kv, 128, n, L, P, shared, seed=9).upload())
+    want = [run(x).clone() for x in xs]
+    ws = [ws_for(x) for x in xs]
+    streams = [torch.cuda.Stream() for _ in xs]
+    for x in xs:
+        x.out.fill_(555.0)
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for x, (w, nb), s in zip(xs, ws, streams):
+            with torch.cuda.stream(s):
+                sm.prompt_attn(x.dt, x.off, x.kv, x.n_q, x.qd, x.out, prefix=x.px, ws=w, ws_bytes=nb)
+    torch.cuda.synchronize()
+    for x, w in zip(xs, want):
+        assert torch.equal(x.out.view(torch.int16), w.view(torch.int16))
+
+
 @pytest.mark.parametrize("name", ["prefix_mixed", "one_long_gqa", "many"])
 def test_captured_and_on_another_stream(name):
     """A captured call, replayed between eager calls on other data, gives the eager result every time."""
