@@ -864,9 +864,9 @@ int run_walk(int dt, bool tree, const TreeInfo &ti, const int32_t *off_h, const 
   const size_t bytes = (size_t)ti.total * n_q * kv->head_dim * (dt == SPECMEMO_BF16 ? 2 : 4);
   if ((uintptr_t)q < (uintptr_t)out + bytes && (uintptr_t)out < (uintptr_t)q + bytes) return fail(SPECMEMO_E_ARG, "out overlaps q");
   const WalkPlan p = make_walk(dt, !tree, ti, off_h, kv, px, n_q);
-  constexpr int64_t most = UINT32_MAX / 256 / 8;   // on each XCD: a launch has at most 2^32 - 1 threads
-  if (p.slots > most || p.cslots > most || p.parts > INT32_MAX)
-    return fail(SPECMEMO_E_ARG, "too many work items: %lld", 8 * (long long)std::max(p.slots, p.cslots));
+  constexpr int64_t most = UINT32_MAX / 256;   // blocks of 256 threads: a launch has at most 2^32 - 1 threads
+  if (p.blocks > most || p.cblocks > most || p.parts > INT32_MAX)
+    return fail(SPECMEMO_E_ARG, "too many work items: %lld", (long long)std::max(p.blocks, p.cblocks));
   const size_t need = walk_ws_bytes(p, kv->head_dim);
   if (need && (!al(ws, 16) || ws_bytes < need))
     return fail(SPECMEMO_E_WORKSPACE, "workspace of %zu bytes needed (16-byte aligned), got %zu", need, ws ? ws_bytes : 0);
@@ -881,11 +881,9 @@ int run_walk(int dt, bool tree, const TreeInfo &ti, const int32_t *off_h, const 
   a.n_kv = kv->n_kv;
   a.group = n_q / kv->n_kv;
   a.head_dim = kv->head_dim;
-  a.units = p.units;
-  a.fan = p.fan;
   a.nset = (int)p.sets.size();
-  a.slots = (int)p.slots;
-  a.cslots = (int)p.cslots;
+  a.blocks = (uint32_t)p.blocks;
+  a.cblocks = (uint32_t)p.cblocks;
   a.scale_log2 = scale * 1.4426950408889634f;
   hipStream_t st = static_cast<hipStream_t>(stream);
   uint8_t *w = static_cast<uint8_t *>(ws);

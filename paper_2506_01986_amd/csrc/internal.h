@@ -145,9 +145,9 @@ struct WalkSet {
   int32_t rb;            // query rows of a row block
   int32_t nrb, ct, nch;  // row blocks, tiles per chunk, most chunks of a row block
   int32_t items;         // (row block, chunk) pairs of one KV head
-  int32_t cum;           // item slots of an XCD before this set
+  int32_t cum;           // blocks before this set's
   int32_t part0;         // first 32-row unit of its parts, -1: every row block writes its output
-  int32_t ccum, citems;  // slots of an XCD before this set and 32-row units of one KV head, of the merge
+  int32_t ccum, citems;  // blocks before this set's and 32-row units of one KV head, of the merge
   int32_t cunit0;        // first unit that is merged
   int32_t shared;        // set that holds the prefix's parts of these rows, or -1
   uint8_t causal;        // a node sees the slab rows up to its own
@@ -173,8 +173,8 @@ struct WalkArgs {
   const WalkSetPacked *tab;   // more than kMaxWalkSets sets: in the workspace
   int64_t cap_total;
   int32_t n_q, n_kv, group, head_dim;
-  int32_t units, fan;      // virtual units of a set on each XCD; shares of a KV head's items
-  int32_t nset, slots, cslots;   // item and merge slots of one XCD
+  int32_t nset;
+  uint32_t blocks, cblocks;   // of the walk and of the merge
   float scale_log2;        // scale * log2(e)
   WalkSetPacked set[kMaxWalkSets];
 };
@@ -239,9 +239,8 @@ struct WalkSeq {
   int32_t L, T, P, row0;
 };
 struct WalkPlan {
-  int fan = 1, units = 1;
-  int64_t slots = 0, cslots = 0;   // of one XCD
-  int64_t parts = 0;               // 32-row units
+  int64_t blocks = 0, cblocks = 0;   // of the walk and of the merge
+  int64_t parts = 0;                 // 32-row units
   std::vector<WalkSetPacked> sets;
 };
 void plan_walk(int dt, bool causal, const std::vector<WalkSeq> &seqs, int n_kv, int group, int head_dim, int cus,

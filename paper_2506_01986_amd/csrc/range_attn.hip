@@ -46,7 +46,7 @@ struct WalkItem {
 typedef __attribute__((address_space(4))) const WalkArgs KernArgs;
 __device__ __forceinline__ KernArgs *kern_args() { return (KernArgs *)__builtin_amdgcn_kernarg_segment_ptr(); }
 
-// The set whose slots hold position k: the last one with first slot <= k.
+// The set that block k belongs to: the last one with first block <= k.
 template <bool COMBINE>
 __device__ __forceinline__ int find_set(const WalkArgs &a, int k) {
   const int lane = threadIdx.x & 63;
@@ -86,29 +86,24 @@ __device__ __forceinline__ WalkSet get_set(const WalkArgs &a, int s) {
   return walk_expand(P, a.group);
 }
 
-// Block 8 k + x is the k-th block of XCD x (blocks reach the eight XCDs
-// round-robin).  A virtual unit is a KV head, or with KV heads no multiple of
-// eight one of `fan` interleaved shares of its items, so that every XCD runs the
-// same number of units of every set and one prefix count serves all eight.  A
-// unit's items read the same K/V through one L2.  Sets take turns in which share
-// is first, or sets of one item would all run on the first XCDs (one KV head, 256
-// single tokens over 200 to 1000 keys: 67.5 us, 42.7 in turns; 64 over two documents of
-// 4096 keys 23.2, 20.7).  False: a padding slot.
+// A set's blocks are its items times the KV heads, KV head fastest, without gaps.
+// Blocks reach the eight XCDs round-robin and every set begins at a multiple of
+// n_kv, so a KV head's items run on the XCDs that equal it modulo gcd(n_kv, 8), on
+// one where n_kv is a multiple of eight, and read its K/V through those L2s.
+// (Empty blocks that even out the XCDs' counts set by set push two of the others to
+// one compute unit: one KV head, 40 trees of 64 nodes x 4 heads over a prefix of 4096
+// keys 79.4 us, 68.9 without; 256 single tokens over 200 to 1000 keys 42.7, 29.6.)
 template <bool COMBINE>
-__device__ __forceinline__ bool decode_unit(const WalkArgs &a, int bid, WalkSet &S, int &kvh, int &i) {
-  const int x = bid & 7, k = bid >> 3;
-  const int s = find_set<COMBINE>(a, k);
-  S = get_set(a, s);
-  const int kk = k - (COMBINE ? S.ccum : S.cum);
-  const int u = x + 8 * (kk % a.units);
-  kvh = u % a.n_kv;
-  i = kk / a.units * a.fan + ((u / a.n_kv + s) & (a.fan - 1));
-  return i < (COMBINE ? S.citems : S.items);
+__device__ __forceinline__ void decode_unit(const WalkArgs &a, int bid, WalkSet &S, int &kvh, int &i) {
+  S = get_set(a, find_set<COMBINE>(a, bid));
+  const int n = bid - (COMBINE ? S.ccum : S.cum);
+  kvh = n % a.n_kv;
+  i = n / a.n_kv;
 }
 
-__device__ __forceinline__ bool decode_walk(const WalkArgs &a, int bid, WalkItem &it) {
+__device__ __forceinline__ void decode_walk(const WalkArgs &a, int bid, WalkItem &it) {
   int i;
-  if (!decode_unit<false>(a, bid, it.S, it.kvh, i)) return false;
+  decode_unit<false>(a, bid, it.S, it.kvh, i);
   const WalkSet &S = it.S;
   if (S.nch == 1) {              // longest row blocks first
     it.ch = 0;
@@ -131,7 +126,6 @@ __device__ __forceinline__ bool decode_walk(const WalkArgs &a, int bid, WalkItem
   }
   it.rb = __builtin_amdgcn_readfirstlane(it.rb);
   it.ch = __builtin_amdgcn_readfirstlane(it.ch);
-  return true;
 }
 
 // First 32-row unit of the parts of (row block, chunk).
@@ -447,7 +441,7 @@ __global__ __launch_bounds__(kBf16Waves * 64, 2) void walk_attn_bf16(WalkArgs a)
   __shared__ __attribute__((aligned(1024))) uint8_t kring[2][kTileBytes];
   __shared__ __attribute__((aligned(1024))) uint8_t vring[2][kTileBytes];
   WalkItem it;
-  if (!decode_walk(a, blockIdx.x, it)) return;   // no barrier reached
+  decode_walk(a, blockIdx.x, it);
   if (it.S.rb == 64) walk_bf16<2, TREE>(a, it, kring, vring);
   else walk_bf16<1, TREE>(a, it, kring, vring);
 }
@@ -472,7 +466,7 @@ __global__ __launch_bounds__(64 * kF32Waves, 2) void walk_attn_f32(WalkArgs a) {
   __shared__ __attribute__((aligned(16))) float merge[W][UF];
   __shared__ int par[kMaxNodes];
   WalkItem it;
-  if (!decode_walk(a, blockIdx.x, it)) return;
+  decode_walk(a, blockIdx.x, it);
   const WalkSet &S = it.S;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int h = lane >> 5, g = a.group, L = S.L, P = S.P, d = a.head_dim;
@@ -640,7 +634,7 @@ __global__ __launch_bounds__(256) void walk_combine(WalkArgs a) {
   constexpr int UF = walk_unit_floats(DB);
   WalkSet S;
   int kvh, i;
-  if (!decode_unit<true>(a, blockIdx.x, S, kvh, i)) return;
+  decode_unit<true>(a, blockIdx.x, S, kvh, i);
   i += S.cunit0;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), h = lane >> 5, g = a.group;
   const int upb = S.rb >> 5, rb = __builtin_amdgcn_readfirstlane(i / upb), un = __builtin_amdgcn_readfirstlane(i % upb);
@@ -721,8 +715,8 @@ __global__ __launch_bounds__(256) void walk_combine(WalkArgs a) {
 
 template <int DB, bool TREE>
 void launch_f32(const WalkArgs &a, hipStream_t st) {
-  hipLaunchKernelGGL((walk_attn_f32<DB, TREE>), dim3(8 * a.slots), dim3(64 * kF32Waves), 0, st, a);
-  if (a.cslots) hipLaunchKernelGGL((walk_combine<DB, false>), dim3(8 * a.cslots), dim3(256), 0, st, a);
+  hipLaunchKernelGGL((walk_attn_f32<DB, TREE>), dim3(a.blocks), dim3(64 * kF32Waves), 0, st, a);
+  if (a.cblocks) hipLaunchKernelGGL((walk_combine<DB, false>), dim3(a.cblocks), dim3(256), 0, st, a);
 }
 
 template <bool TREE>
@@ -737,8 +731,8 @@ void launch_f32(const WalkArgs &a, hipStream_t st) {
 
 template <bool TREE>
 void launch_bf16(const WalkArgs &a, hipStream_t st) {
-  hipLaunchKernelGGL((walk_attn_bf16<TREE>), dim3(8 * a.slots), dim3(64 * kBf16Waves), 0, st, a);
-  if (a.cslots) hipLaunchKernelGGL((walk_combine<D / 32, true>), dim3(8 * a.cslots), dim3(256), 0, st, a);
+  hipLaunchKernelGGL((walk_attn_bf16<TREE>), dim3(a.blocks), dim3(64 * kBf16Waves), 0, st, a);
+  if (a.cblocks) hipLaunchKernelGGL((walk_combine<D / 32, true>), dim3(a.cblocks), dim3(256), 0, st, a);
 }
 
 }  // namespace

@@ -162,21 +162,18 @@ void plan_walk(int dt, bool causal, const std::vector<WalkSeq> &seqs, int n_kv, 
   std::iota(order.begin(), order.end(), 0);
   std::stable_sort(order.begin(), order.end(), [&](int x, int y) { return size[x] > size[y]; });
   for (size_t i = 0; i < n; ++i) place[order[i]] = (int)i;
-  const int fan = 8 / std::gcd(n_kv, 8), units = n_kv * fan / 8;
-  p->fan = fan;
-  p->units = units;
-  int64_t slot = 0, cslot = 0, part = 0;
+  int64_t block = 0, cblock = 0, part = 0;
   for (int i : order) {
     WalkSet s = sets[i];
     if (s.shared >= 0) s.shared = place[s.shared];
-    s.cum = (int)slot;
-    slot += (int64_t)ceil_div(s.items, fan) * units;
+    s.cum = (int)block;
+    block += (int64_t)s.items * n_kv;
     s.part0 = -1;
     if (s.nch > 1 || s.parts) {
       s.part0 = (int)part;
       part += (int64_t)s.items * n_kv * (s.rb / 32);
     }
-    s.ccum = (int)cslot;
+    s.ccum = (int)cblock;
     WalkSetPacked q{};
     q.base_lo = (uint32_t)s.base;
     q.base_hi = (uint8_t)(s.base >> 32);
@@ -195,10 +192,10 @@ void plan_walk(int dt, bool causal, const std::vector<WalkSeq> &seqs, int n_kv, 
     q.ccum = s.ccum;
     q.shared = s.shared;
     p->sets.push_back(q);
-    cslot += (int64_t)ceil_div(walk_expand(q, g).citems, fan) * units;
+    cblock += (int64_t)walk_expand(q, g).citems * n_kv;
   }
-  p->slots = slot;
-  p->cslots = cslot;
+  p->blocks = block;
+  p->cblocks = cblock;
   p->parts = part;
 }
 
