@@ -1044,7 +1044,7 @@ int specmemo_logit_rules(specmemo_dtype dt, const specmemo_trees *t, int32_t voc
     a.bias_val = rules->bias_val;
     a.n_bias = rules->n_bias;
     a.vocab = vocab;
-    return hip_status(launch_logit_rules(dt, a, ti.B, ti.max_nodes, static_cast<hipStream_t>(stream)), "logit rules launch");
+    return hip_status(launch_logit_rules(dt, a, ti.B, ti.total, ti.max_nodes, static_cast<hipStream_t>(stream)), "logit rules launch");
   });
 }
 

@@ -285,7 +285,7 @@ struct RulesArgs {
   int32_t penalties;         // any of the three is given
   int32_t rows, groups;      // node rows a block, row groups of the largest tree
 };
-hipError_t launch_logit_rules(int dt, const RulesArgs &a, int B, int max_nodes, hipStream_t st);
+hipError_t launch_logit_rules(int dt, const RulesArgs &a, int B, int total, int max_nodes, hipStream_t st);
 struct CountArgs {
   const int32_t *tok_off, *tokens;
   int32_t *counts;
