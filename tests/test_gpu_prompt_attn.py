@@ -161,6 +161,17 @@ def test_largest_batch(dtype, d):
     parity(Batch(dtype, 2, 1, d, n, draw(12, 20, 4096), [600] * 4096, [i // 1024 for i in range(4096)], seed=13))
 
 
+@pytest.mark.parametrize("name", ["gqa_odd", "prefix_decode", "one_long_gqa"])
+def test_rows_past_the_batch(name):
+    """A larger output than the batch: rows after the last token keep what they held."""
+    n_q, n_kv, n, L, P, shared = BF16[name]
+    x = Batch("bf16", n_q, n_kv, 128, n, L, P, shared, seed=10).upload()
+    x.out = torch.full((x.qd.shape[0] + 300, n_q, 128), 777.0, dtype=x.dtype, device="cuda")
+    run(x)
+    assert (x.out[x.qd.shape[0]:] == 777.0).all()
+    check(x.out[:x.qd.shape[0]], *x.reference(lambda b: causal(x.n[b])))
+
+
 def test_two_calls_at_once():
     """Calls on two streams, each with a workspace of its own, one of them with its table of sets there."""
     xs = []
