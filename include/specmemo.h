@@ -425,7 +425,7 @@ typedef struct {
   const int32_t *bias_off;    /* device [B+1]: entries bias_off[b] .. bias_off[b+1] - 1 are sequence b's */
   const int32_t *bias_id;     /* device [n_bias]: token ids; ids outside [0, vocab) are ignored, of equal ids the last counts */
   const float *bias_val;      /* device [n_bias] */
-  int32_t n_bias;             /* all sequences' entries; 0: no biases (the three arrays may be NULL) */
+  int32_t n_bias;             /* all sequences' entries, < 2^30; 0: no biases (the three arrays may be NULL) */
   const uint32_t *mask;       /* device [n_masks][mask_words]: bit v % 32 of word v / 32 set = token v is allowed */
   const int32_t *mask_idx;    /* device [sum N_b]: mask of each node's row; outside [0, n_masks): every token is allowed */
   int32_t n_masks;            /* 0: no masks (the two arrays may be NULL) */

@@ -1019,6 +1019,7 @@ int specmemo_logit_rules(specmemo_dtype dt, const specmemo_trees *t, int32_t voc
     if (a.penalties && !al(node_tok, 4)) return fail(SPECMEMO_E_ARG, "node_tok must be non-NULL and 4-byte aligned");
     if (rules->n_bias < 0 || rules->n_masks < 0)
       return fail(SPECMEMO_E_ARG, "n_bias=%d n_masks=%d", rules->n_bias, rules->n_masks);
+    if (rules->n_bias > INT32_MAX / 2) return fail(SPECMEMO_E_ARG, "n_bias=%d, at most %d", rules->n_bias, INT32_MAX / 2);   // an entry's index plus a step in 32 bits
     if (rules->n_bias > 0 && (!al(rules->bias_off, 4) || !al(rules->bias_id, 4) || !al(rules->bias_val, 4)))
       return fail(SPECMEMO_E_ARG, "bias arrays must be non-NULL and 4-byte aligned");
     if (rules->n_masks > 0) {
