@@ -144,6 +144,7 @@ int hip_status(hipError_t e, const char *what) {
 // ---- tree attention planning ------------------------------------------------------
 constexpr int kMaxSlabRows = 1 << 23;   // bf16 attention: slab bytes below 2^31
 constexpr int kMaxRulesVocab = 1 << 30; // column arithmetic of the logit rules in 32 bits
+static_assert(SPECMEMO_MAX_BATCH * (kMaxNodes / kRulesRows) <= kMaxGridY, "the largest batch of logit rules fits one launch");
 constexpr int kMinChunk = 160;      // fewest keys per chunk when splitting the KV range
 
 // Tuning overrides (they change the work split, never the result beyond

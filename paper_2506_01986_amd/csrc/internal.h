@@ -285,6 +285,18 @@ struct RulesArgs {
   int32_t penalties;         // any of the three is given
   int32_t rows, groups;      // node rows a block, row groups of the largest tree
 };
+// Node rows of a block (at most kRulesRows), for `segs` segments of the vocabulary:
+// fewer where the chip is not full, whose work is the block's chain (504 rows of uneven
+// trees, 8264 values: 17.2 us eight a block, 12.1 four), and more again where the row
+// groups of the largest tree times the sequences pass the blocks that a launch takes in
+// y (eight rows a block keep the largest batch, 4096 trees of 128 nodes, within them).
+constexpr int kRulesRows = 8, kMaxGridY = 65536;
+inline int rules_rows(int segs, int B, int total, int max_nodes, int cus) {
+  int rows = kRulesRows;
+  while (rows > 1 && (int64_t)segs * total < (int64_t)rows * 2 * cus) rows /= 2;
+  while (rows < kRulesRows && B * ((max_nodes + rows - 1) / rows) > kMaxGridY) rows *= 2;
+  return rows;
+}
 hipError_t launch_logit_rules(int dt, const RulesArgs &a, int B, int total, int max_nodes, hipStream_t st);
 struct CountArgs {
   const int32_t *tok_off, *tokens;

@@ -20,7 +20,7 @@ namespace {
 
 constexpr int kNT = 256;          // threads of a rules block
 static_assert(kNT >= kMaxNodes, "one thread per tree node");
-constexpr int kRows = 8;          // most node rows of a block, all their loads in flight at once
+constexpr int kRows = kRulesRows;   // most node rows of a block, all their loads in flight at once
 
 // Chunks of 16 bytes at 16-byte aligned addresses; a row whose length keeps it from
 // starting or ending on one has up to 2 (V - 1) single values, before and after.
@@ -313,10 +313,7 @@ __global__ __launch_bounds__(64) void count_accepted_kernel(AcceptedArgs a) {
 hipError_t launch_logit_rules(int dt, const RulesArgs &args, int B, int total, int max_nodes, hipStream_t st) {
   RulesArgs a = args;
   const int seg = kNT * (dt == 0 ? 4 : 8), segs = (a.vocab + seg - 1) / seg;
-  // fewer rows a block where the chip is not full: their work is the block's chain (504
-  // rows of uneven trees, 8264 values: 17.2 us eight a block, 12.1 four)
-  a.rows = kRows;
-  while (a.rows > 1 && (int64_t)segs * total < (int64_t)a.rows * 2 * device_cus()) a.rows /= 2;
+  a.rows = rules_rows(segs, B, total, max_nodes, device_cus());
   a.groups = (max_nodes + a.rows - 1) / a.rows;
   const dim3 grid(segs, B * a.groups);
   if (dt == 0) hipLaunchKernelGGL(logit_rules_kernel<0>, grid, dim3(kNT), 0, st, a);
