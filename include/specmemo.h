@@ -437,7 +437,8 @@ typedef struct {
  *   x = z;  if c > 0: x = (x > 0 ? x / repetition[b] : x * repetition[b])
  *                         - frequency[b] * c - presence[b]
  *   out[u][v] = x + bias[b][v], or -inf where u's mask does not allow v
- * in fp32, rounded once to `dt`.  logits, out: device [sum N_b][vocab] in `dt`,
+ * in fp32 (of bf16 logits x / repetition may be a product with the rounded
+ * reciprocal), rounded once to `dt`.  logits, out: device [sum N_b][vocab] in `dt`,
  * 16-byte aligned, the same buffer or not overlapping.  node_tok: device int32
  * [sum N_b], read only with one of the three penalties (else it may be NULL);
  * tokens outside [0, vocab) count for nothing.  A row whose mask allows no token

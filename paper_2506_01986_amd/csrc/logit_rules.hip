@@ -78,6 +78,10 @@ __global__ __launch_bounds__(kNT) void logit_rules_kernel(RulesArgs a) {
     }
   }
   const float rep = a.repetition ? a.repetition[b] : 1.f, inv_rep = 1.f / rep;
+  // fp32 quotients are rounded once.  For bf16 a whole chunk's are products with the
+  // reciprocal (2^-24 of a quotient more; the result's own rounding is 2^-8), unless fp32
+  // does not hold the reciprocal as a normal number: then one by one, as tokens on the path.
+  const bool single = DT == 1 && !(rep >= 0x1p-126f && rep <= 0x1p126f);
   const float pres = a.presence ? a.presence[b] : 0.f, freq = a.frequency ? a.frequency[b] : 0.f;
   const int j0 = a.n_bias > 0 ? max(a.bias_off[b], 0) : 0, j1 = a.n_bias > 0 ? min(a.bias_off[b + 1], a.n_bias) : 0;
   const int col0 = blockIdx.x * SEG, chunk = blockIdx.x * kNT + tid;
@@ -188,9 +192,8 @@ __global__ __launch_bounds__(kNT) void logit_rules_kernel(RulesArgs a) {
   }
   __syncthreads();
 
-  // (x / repetition as a product with its reciprocal: one rounding of 2^-24 more, far below the logits' own)
   auto apply = [&](float x, int c, float bias, bool allowed) {
-    const float y = fmaf(-freq, (float)c, (x > 0.f ? x * inv_rep : x * rep) - pres);
+    const float y = fmaf(-freq, (float)c, (x > 0.f ? x / rep : x * rep) - pres);
     x = c > 0 ? y : x;
     return allowed ? x + bias : -INFINITY;
   };
@@ -222,14 +225,14 @@ __global__ __launch_bounds__(kNT) void logit_rules_kernel(RulesArgs a) {
         }
       }
       // tokens of this row's path among the thread's columns
-      uint32_t onpath = 0;
+      uint32_t onpath = single && touched ? (1u << V) - 1 : 0;
       for (int u = first; u >= 0; u = s_after[u]) onpath |= (unsigned)(s_loc[u] - l0) < V ? 1u << (s_loc[u] - l0) : 0u;
       const bool masked = (bits[f] & ((1u << V) - 1)) != (1u << V) - 1;
       if (touched || masked || onpath) {
 #pragma unroll
         for (int e = 0; e < V; ++e) {
           const float z = Chunk<DT>::get(w[f], e);
-          x[e] = fmaf(z, z > 0.f ? pos[e] : neg[e], add[e]);
+          x[e] = DT == 0 ? (z > 0.f ? z / neg[e] : z * neg[e]) + add[e] : fmaf(z, z > 0.f ? pos[e] : neg[e], add[e]);
         }
         if (onpath) {
 #pragma unroll
