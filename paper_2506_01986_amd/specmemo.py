@@ -467,10 +467,22 @@ def tree_attn_prefix(dt: int, trees: Trees, kv: KVPool, prefix: Prefix, n_q: int
 
 # ---- rules on logits ----------------------------------------------------------------
 
+_INT32, _FLOAT32 = ("torch.int32",), ("torch.float32",)
+
+
+def _check_tensor(name: str, x, dtypes: tuple):
+    """Tensors are read as they lie: of one of these types, without gaps (addresses are taken as they are)."""
+    if hasattr(x, "is_contiguous") and (str(x.dtype) not in dtypes or not x.is_contiguous()):
+        raise ValueError(f"{name}: a contiguous tensor of {' or '.join(dtypes)} expected, got {x.dtype} of strides {x.stride()}")
+
+
 class LogitRules:
     """Device arrays of the penalties, biases and masks (include/specmemo.h, specmemo_rules); None leaves a rule out."""
 
     def __init__(self, counts=None, repetition=None, presence=None, frequency=None):
+        _check_tensor("counts", counts, _INT32)
+        for name, x in (("repetition", repetition), ("presence", presence), ("frequency", frequency)):
+            _check_tensor(name, x, _FLOAT32)
         self.counts, self.repetition, self.presence, self.frequency = counts, repetition, presence, frequency
         self.bias_off = self.bias_id = self.bias_val = self.mask = self.mask_idx = None
         self.n_bias = self.n_masks = self.mask_words = 0
@@ -479,12 +491,17 @@ class LogitRules:
         """Sequence b's biases are entries off[b] .. off[b+1] - 1 of ids and values."""
         if ids.numel() != values.numel():
             raise ValueError(f"{ids.numel()} bias ids, {values.numel()} values")
+        _check_tensor("bias offsets", off, _INT32)
+        _check_tensor("bias ids", ids, _INT32)
+        _check_tensor("bias values", values, _FLOAT32)
         self.bias_off, self.bias_id, self.bias_val, self.n_bias = off, ids, values, int(ids.numel())
 
     def set_mask(self, mask, idx):
         """mask: [masks][words] 32-bit words (bit v % 32 of word v / 32: token v is allowed); idx: mask of each node, -1 for none."""
-        self.mask, self.mask_idx = mask, idx
-        self.n_masks, self.mask_words = (int(s) for s in mask.shape)
+        _check_tensor("masks", mask, _INT32 + ("torch.uint32",))
+        _check_tensor("mask indices", idx, _INT32)
+        n, words = (int(s) for s in mask.shape)
+        self.mask, self.mask_idx, self.n_masks, self.mask_words = mask, idx, n, words
 
     def struct(self) -> _Rules:
         return _Rules(_ptr(self.counts), _ptr(self.repetition), _ptr(self.presence), _ptr(self.frequency),
