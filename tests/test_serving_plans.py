@@ -4,8 +4,9 @@ launch sizes they lead to, and the forms that the GPU tests' cases are there for
 import os
 import subprocess
 
-import numpy as np
 import pytest
+
+from tests import serving_forms
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
@@ -49,3 +50,43 @@ def test_rules_rows_fill_the_chip(plan):
     assert rules(plan, "bf16", 32000, [64] * 10) == [8, 80]
     assert rules(plan, "bf16", 8263, [63] * 8) == [4, 128]
     assert rules(plan, "fp32", 1000, [16]) == [1, 16]
+
+
+def sets(plan, name, dt, head_dim):
+    """Kinds of the sets of a case, as serving_forms.WANT names them."""
+    causal = name in serving_forms.PROMPTS
+    case = serving_forms.PROMPTS[name] if causal else serving_forms.TREES[name][1:]
+    n_q, n_kv, L, P, shared = *case[:2], *case[-3:]
+    n = serving_forms.nodes(name)
+    shared = list(range(len(n))) if shared is None else shared
+    words = ["walk", int(dt == "bf16"), int(causal), n_kv, n_q // n_kv, head_dim, CUS, len(n)]
+    for b in range(len(n)):
+        words += [n[b], L[b], P[shared.index(shared[b])], 10 ** 5 * shared[b], 10 ** 8 + 10 ** 5 * b]
+    head, *rows = plan(*words)
+    out = {"table"} if head[3] else set()
+    for _, rb, _, _, nch, slab, _, with_packed in rows:
+        out.add(("own" if slab else "packed") + ("+" if with_packed >= 0 else "") + f" {rb} " + ("cut" if nch > 1 else "whole"))
+    return out
+
+
+@pytest.mark.parametrize("name", list(serving_forms.WANT))
+def test_cases_take_the_forms_they_are_for(plan, name):
+    assert sets(plan, name, "bf16", 128) >= serving_forms.WANT[name]
+
+
+def test_fp32_cases_pack(plan):
+    for name in ("packed128", "packed128_table", "t16_packed128", "single_two_prefixes", "single_table"):
+        got = sets(plan, name, "fp32", 48)
+        assert any(s.startswith("packed 32") for s in got) and any(s.startswith("own+ 32") for s in got), name
+    assert "packed 32 cut" in sets(plan, "single_two_prefixes", "fp32", 48)
+
+
+@pytest.mark.parametrize("keys", [2, 300, 9000, 16000])
+def test_a_lost_or_doubled_key_shows(keys):
+    """The form of test_every_key_counts_once, with the mistake in the reference: some of 128 columns of values 1 and -1
+    are off by more than twice the tolerance of bf16 results."""
+    import numpy as np
+    v = np.where(np.random.default_rng(keys).random((keys, 128)) < 0.5, 1.0, -1.0)
+    ref = v.mean(0)
+    for wrong in (v[1:].mean(0), (v.sum(0) + v[0]) / (keys + 1)):
+        assert (np.abs(wrong - ref) > 2 * (2.0 ** -8 + 2.0 ** -22) * np.abs(ref)).sum() >= 8
