@@ -6,7 +6,7 @@ import subprocess
 
 import pytest
 
-from tests import serving_forms
+from tests import serving_forms, test_gpu_rules_batches
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
@@ -50,6 +50,11 @@ def test_rules_rows_fill_the_chip(plan):
     assert rules(plan, "bf16", 32000, [64] * 10) == [8, 80]
     assert rules(plan, "bf16", 8263, [63] * 8) == [4, 128]
     assert rules(plan, "fp32", 1000, [16]) == [1, 16]
+
+
+@pytest.mark.parametrize("dt,vocab,times,rows", test_gpu_rules_batches.CASES)
+def test_rules_cases_take_the_rows_they_are_for(plan, dt, vocab, times, rows):
+    assert rules(plan, dt, vocab, test_gpu_rules_batches.SIZES * times)[0] == rows
 
 
 def sets(plan, name, dt, head_dim):
