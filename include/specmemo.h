@@ -379,6 +379,9 @@ typedef struct {
  * with KV head kv = hq / (n_q / n_kv):
  *   keys = prefix rows 0 .. P_b - 1 (if any), slab rows 0 .. L_b + i
  *   out[new_off[b] + i][hq] = softmax(scale * q . K[kv][key]) . V[kv][key]
+ * bf16: scores, maxima and sums are fp32; each softmax weight is rounded to bf16,
+ * the operand type of the product with V, and the sum of weights is that of the
+ * rounded ones.
  * new_off_h: host [B+1], new_off_h[0] = 0, non-decreasing, 1 <= B <=
  * SPECMEMO_MAX_BATCH.  q, out: device [new_off_h[B]][n_q][head_dim] in `dt`;
  * out may not overlap q (both are ignored where no sequence brings a token).
@@ -416,7 +419,11 @@ size_t specmemo_tree_attn_prefix_bytes(specmemo_dtype dt, const specmemo_trees *
  * base model's logits of every tree node before specmemo_accept or
  * specmemo_sample_next reads them.  A node's history is the sequence's committed
  * tokens (counts) and the tokens on its own root path (App. A.1: a candidate is
- * verified as the continuation of its path).  1 <= vocab <= 2^30. */
+ * verified as the continuation of its path).  One table of counts serves the three
+ * penalties.  Where they count different tokens (say repetition the prompt's too,
+ * presence and frequency those generated alone), each takes a call of its own, the
+ * biases and masks in the last one, with a rounding to `dt` between the calls.
+ * 1 <= vocab <= 2^30. */
 typedef struct {
   const int32_t *counts;      /* device [B][vocab]: times each token occurred so far; NULL: none did */
   const float *repetition;    /* device [B] > 0, or NULL: 1 */

@@ -627,8 +627,8 @@ __global__ __launch_bounds__(64 * kF32Waves, 2) void walk_attn_f32(WalkArgs a) {
 
 // Merge the parts of 32 query rows of a set: its own chunks, then those of the
 // prefix's set, where the rows lie among the packed rows of all its sequences.
-// Wave w takes the column entries w DB .. + DB - 1 of the accumulator order; the
-// maximum over all parts first (their m alone), so that the sums need no rescaling.
+// Wave w takes the column entries w DB .. + DB - 1 of the accumulator order, and the
+// parts one after another, four a turn: a running maximum, the sums rescaled once a turn.
 template <int DB, bool BF16>
 __global__ __launch_bounds__(256) void walk_combine(WalkArgs a) {
   constexpr int UF = walk_unit_floats(DB);
@@ -656,8 +656,7 @@ __global__ __launch_bounds__(256) void walk_combine(WalkArgs a) {
     return a.part + (int64_t)(walk_part(a, H, kvh, hr >> hsh, p - nown) + ((hr & (H.rb - 1)) >> 5)) * UF;
   };
   if (!row_ok) return;
-  // The first G parts are read at once, everything of them; a running maximum takes
-  // in the others G at a time.
+  // G parts are read at once, everything of them.
   constexpr int G = 4;
   float M = -INFINITY, l = 0.f;
   f32x4 o[DB];

@@ -13,8 +13,14 @@ namespace {
 constexpr int kMaxCausalChunks = 64;   // one a lane (decode_walk)
 
 // Rules of the split, in us of a block's time (two blocks share a compute unit): a
-// 64-key tile takes a block of 64 rows kTileSmall and one of 128 rows kTileLarge
-// (fp32, 32 rows: kTileF32 for each 32 columns of the head).
+// 64-key tile takes a block of 64 rows kTileSmall and one of 128 rows kTileLarge.
+// kTileF32, for each 32 columns of an fp32 head, is no such time (32 rows against a tile
+// of 128 columns take 7.4 us with two blocks a unit: 4 x 1024 rows x 16 heads, 253 us, the
+// same with any weight tried) but the weight that cuts and packs best on the whole.
+// 0.9 cuts more: 2 x 500 rows x 8 heads of 64 columns 25.8 us, 17.2 with 0.45; 1024 x 4 of
+// 128 39.1, 28.2; 8 trees of 16 nodes over a prefix of 512, 4 KV heads of 128 19.8, 25.0;
+// 2 KV heads of 64 17.6, 20.9.  0.22 cuts less: 8 tokens over 2048 keys, 4 KV heads of 64
+// 29.4, 23.7, of 128 38.0, 43.2; 8 x 1 to 8 tokens over 512 to 2048, 2 of 96 29.6, 21.2.
 constexpr double kTileSmall = 1.05, kTileLarge = 2.0, kTileF32 = 0.45;
 // A chunk's start and its share of the merge.  Below about this much work a chunk
 // is mostly that: 8 sequences of 1 to 8 tokens over 500 to 4000 keys, 64 query heads,
