@@ -88,3 +88,33 @@ def test_every_key_counts_once(name, dtype):
         ref = torch.matmul(vis, v) / vis.sum(1)[None, :, None]                 # [n_kv][n][d]
         ref = ref.repeat_interleave(g, 0).transpose(0, 1)
         check(got[int(x.off[b]):int(x.off[b + 1])], ref, (half + 2.0 ** -22) * ref.abs())
+
+
+@pytest.mark.parametrize("name", ["packed128_table", "split128_prefix", "t16_packed128", "single_table"])
+def test_captured(name):
+    """Replays between eager calls on other queries give the eager result, bit for bit."""
+    x, run = batch(name, "bf16")
+    x.upload()
+    want = run().clone()
+    if name in PROMPTS:
+        n = sm.prompt_attn_bytes(x.dt, x.off, x.kv, x.n_q, x.px)
+        call = lambda: sm.prompt_attn(x.dt, x.off, x.kv, x.n_q, x.qd, x.out, prefix=x.px, ws=ws, ws_bytes=n)
+    else:
+        n = sm.tree_attn_prefix_bytes(x.dt, x.trees, x.kv, x.px, x.n_q)
+        call = lambda: sm.tree_attn_prefix(x.dt, x.trees, x.kv, x.px, x.n_q, x.qd, x.out, ws=ws, ws_bytes=n)
+    ws = torch.full((n,), 255, dtype=torch.uint8, device="cuda")
+    side, graph, q0 = torch.cuda.Stream(), torch.cuda.CUDAGraph(), x.qd.clone()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        with torch.cuda.graph(graph, stream=side):
+            call()
+        for i in range(3):
+            x.out.fill_(555.0)
+            ws.fill_(255)
+            x.qd.copy_(q0)
+            graph.replay()
+            side.synchronize()
+            assert torch.equal(x.out.view(torch.int16), want.view(torch.int16)), i
+            x.qd.normal_()
+            call()
+            side.synchronize()
