@@ -12,9 +12,12 @@
  *   specmemo_accept        (c) greedy / typical acceptance of the longest path
  *   specmemo_kv_compact    (d) in-place compaction of the accepted K/V
  *
- * Around a step: specmemo_prompt_attn (the prompt's attention over the pool),
+ * Around a step: specmemo_kv_append (norm, position rotation and the pool's new
+ * rows), specmemo_prompt_attn (the prompt's attention over the pool),
  * specmemo_tree_attn_prefix ((b) over a prefix that sequences share) and
- * specmemo_logit_rules (penalties, biases and masks before (c)).
+ * specmemo_logit_rules (penalties, biases and masks before (c)).  The
+ * specmemo_kv4_* calls are (b), (d) and the prompt's attention over a pool whose
+ * rows are held in 4 bits.
  *
  * Symbols follow the paper's memory model (Sec. 3.1): b = batch (B),
  * k = KV heads (n_kv), d = head dim (head_dim), x = KV length
@@ -412,6 +415,108 @@ int specmemo_tree_attn_prefix(specmemo_dtype dt, const specmemo_trees *t, const 
                               void *ws, size_t ws_bytes, void *stream);
 size_t specmemo_tree_attn_prefix_bytes(specmemo_dtype dt, const specmemo_trees *t, const specmemo_kv *kv,
                                        const specmemo_prefix *prefix, int32_t n_q);
+
+/* ---- New rows of the pool -------------------------------------------------------
+ *
+ * A step's or a prompt's tokens bring q, k and v of one layer from its
+ * projections.  One call norms the heads of q and k, rotates them to the tokens'
+ * positions and writes k and v to the slabs, where the attention calls read them
+ * (Sec. 3.1: the preallocated cache is written before verification). */
+typedef enum { SPECMEMO_ROT_HALVES = 0, SPECMEMO_ROT_PAIRS = 1 } specmemo_rot_style;
+
+/* Token i's heads lie at q + i * q_stride, [n_q][head_dim] without gaps, in `dt`;
+ * k and v alike with n_kv heads.  Strides are in elements, at least a token's
+ * heads and a multiple of 16 bytes: the three may be slices of one buffer. */
+typedef struct {
+  const void *q;              /* device; NULL with n_q = 0: keys and values alone */
+  const void *k, *v;          /* device */
+  int64_t q_stride, k_stride, v_stride;
+  const void *q_norm, *k_norm; /* device [head_dim] in `dt`, or NULL: no norm */
+  float eps;                  /* of the norm, >= 0 */
+  const float *cos, *sin;     /* device fp32 [n_pos][rot_dim / 2] */
+  const int32_t *pos;         /* device [tokens]: row of cos and sin of each token */
+  int32_t n_pos;
+  int32_t rot_dim;            /* rotated columns, the first of each head; 0: none (cos, sin, pos may be NULL) */
+  int32_t rot_style;          /* specmemo_rot_style */
+} specmemo_rows;
+
+/* For token i = 0 .. T_b - 1 of sequence b (row t = new_off_h[b] + i of the inputs), and
+ * each head x of q and k:
+ *   y = x / sqrt(mean(x^2) + eps) * norm            (where a norm is given)
+ *   (y_a, y_b) <- (y_a cos - y_b sin, y_b cos + y_a sin), angle j < rot_dim / 2 of row
+ *       pos[t]; HALVES: a = j, b = j + rot_dim / 2; PAIRS: a = 2 j, b = 2 j + 1
+ *   q_out[t][head] = y;  slab row L_b + i of K = y, of V = v    (L_b = kv->seq_len_h[b])
+ * in fp32, rounded once to `dt`.  A token whose position is outside [0, n_pos) writes
+ * nothing: its rows of q_out, K and V stay as they were.  All other rows of the pool
+ * stay as they were.  The lengths are the caller's to advance; kv->seq_len is not read.
+ * new_off_h: host [B+1], new_off_h[0] = 0, non-decreasing, 1 <= B <=
+ * SPECMEMO_MAX_BATCH; L_b + T_b <= seq_cap[b].  head_dim as in specmemo_tree_attn;
+ * rot_dim <= head_dim, a multiple of 16 (bf16) or 8 (fp32).  q_out: device
+ * [tokens][n_q][head_dim]; it may be q itself where q has no gaps, and the outputs may
+ * not overlap the inputs otherwise.  n_q >= 0, any number. */
+int specmemo_kv_append(specmemo_dtype dt, int32_t B, const int32_t *new_off_h, const specmemo_rows *x, int32_t n_q,
+                       const specmemo_kv *kv, void *q_out, void *stream);
+
+/* ---- The pool in 4 bits -----------------------------------------------------------
+ *
+ * The cache is what the memory budget goes to (Sec. 3.1, Eq. 1); in 4 bits a row of
+ * 128 columns takes 68 bytes instead of 256.  A row of a head is groups of 32
+ * columns.  A column is a sign (bit 3) and one of the magnitudes 0, 1/2, 1, 3/2, 2, 3,
+ * 4, 6 (codes 0 .. 7), times its group's 2^E; column 2 i is the low half of byte i.
+ * The scale byte is E + 127.  Rows move and are dropped as those of specmemo_kv are:
+ * every row has its own scales, so nothing is ever rounded twice. */
+typedef struct {
+  void *k, *v;                /* device uint8 [n_kv][cap_total][head_dim / 2]: codes */
+  void *k_scale, *v_scale;    /* device uint8 [n_kv][cap_total][head_dim / 32] */
+  int64_t cap_total;          /* the rest as in specmemo_kv */
+  int32_t n_kv;
+  int32_t head_dim;           /* a multiple of 32 */
+  int32_t *seq_len;
+  const int64_t *seq_base_h;
+  const int32_t *seq_cap_h;
+  const int32_t *seq_len_h;
+} specmemo_kv4;
+
+/* Eq. 1 for such a pool: bytes of codes and scales of K and V, 2 * layers * batch *
+ * n_kv * tokens * (head_dim / 2 + head_dim / 32).  Arguments must be >= 0, head_dim a
+ * multiple of 32.  Returns -1 otherwise or on overflow. */
+int64_t specmemo_mem_kv4_bytes(int32_t layers, int32_t batch, int32_t n_kv, int32_t head_dim, int64_t tokens);
+
+/* specmemo_kv_append into a 4-bit pool.  A group's E is the least in [-125, 125] for
+ * which no magnitude passes 7 x 2^E, and every value becomes the nearest of the group's,
+ * ties to the even code.  Keys are normed and rotated in fp64, so that the code is that
+ * of the exact value; q_out is as in specmemo_kv_append.  A group with an infinity, a
+ * NaN or a magnitude past fp32's range gets the scale byte 255 (all its values are NaN). */
+int specmemo_kv4_append(specmemo_dtype dt, int32_t B, const int32_t *new_off_h, const specmemo_rows *x, int32_t n_q,
+                        const specmemo_kv4 *kv, void *q_out, void *stream);
+
+/* Slab rows L_b .. L_b + T_b - 1 (T_b and the order of tokens as above) as values:
+ * k_out, v_out: device [tokens][n_kv][head_dim] in `dt`, exact. */
+int specmemo_kv4_read(specmemo_dtype dt, int32_t B, const int32_t *new_off_h, const specmemo_kv4 *kv, void *k_out,
+                      void *v_out, void *stream);
+
+/* specmemo_prompt_attn over a 4-bit pool: keys and values are those that the pool's
+ * bytes stand for.  Same arguments, limits (head_dim a multiple of 32) and workspace;
+ * q must be finite, and the groups that a call walks too (scale bytes 2 .. 252).  bf16: a
+ * score is that of the bf16 query with the 4-bit keys, columns of magnitude below 2^-8 of
+ * the largest of their 32 within 2^-16 of it, summed in fp32; the weights' rounding is
+ * that of specmemo_prompt_attn. */
+int specmemo_kv4_prompt_attn(specmemo_dtype dt, int32_t B, const int32_t *new_off_h, const specmemo_kv4 *kv,
+                             const specmemo_prefix *prefix, int32_t n_q, float scale, const void *q, void *out,
+                             void *ws, size_t ws_bytes, void *stream);
+size_t specmemo_kv4_prompt_attn_bytes(specmemo_dtype dt, int32_t B, const int32_t *new_off_h, const specmemo_kv4 *kv,
+                                      const specmemo_prefix *prefix, int32_t n_q);
+
+/* specmemo_tree_attn_prefix over a 4-bit pool; prefix may be NULL. */
+int specmemo_kv4_tree_attn(specmemo_dtype dt, const specmemo_trees *t, const specmemo_kv4 *kv,
+                           const specmemo_prefix *prefix, int32_t n_q, float scale, const void *q, void *out, void *ws,
+                           size_t ws_bytes, void *stream);
+size_t specmemo_kv4_tree_attn_bytes(specmemo_dtype dt, const specmemo_trees *t, const specmemo_kv4 *kv,
+                                    const specmemo_prefix *prefix, int32_t n_q);
+
+/* specmemo_kv_compact of a 4-bit pool: codes and scales of the accepted rows move. */
+int specmemo_kv4_compact(const specmemo_trees *t, const specmemo_kv4 *kv, const int32_t *accept_len,
+                         const int32_t *path, int32_t path_stride, void *stream);
 
 /* ---- Rules on logits ------------------------------------------------------------
  *

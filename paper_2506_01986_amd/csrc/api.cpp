@@ -813,9 +813,7 @@ int check_walk(int dt, const TreeInfo &ti, const int32_t *off_h, const specmemo_
   return check_prefix(px, kv, dt, ti.B);
 }
 
-int check_prompt(int dt, int B, const int32_t *off, const specmemo_kv *kv, const specmemo_prefix *px, int n_q, TreeInfo *ti) {
-  int rc;
-  if ((rc = check_dtype(dt))) return rc;
+int check_offsets(int B, const int32_t *off, TreeInfo *ti) {
   if (B < 1 || B > SPECMEMO_MAX_BATCH) return fail(SPECMEMO_E_ARG, "B=%d outside [1, %d]", B, SPECMEMO_MAX_BATCH);
   if (!off) return fail(SPECMEMO_E_ARG, "new_off_h is NULL");
   if (off[0] != 0) return fail(SPECMEMO_E_ARG, "new_off[0]=%d, expected 0", off[0]);
@@ -823,6 +821,13 @@ int check_prompt(int dt, int B, const int32_t *off, const specmemo_kv *kv, const
     if (off[b + 1] < off[b]) return fail(SPECMEMO_E_ARG, "new_off[%d]=%d after %d", b + 1, off[b + 1], off[b]);
   ti->B = B;
   ti->total = off[B];
+  return SPECMEMO_OK;
+}
+
+int check_prompt(int dt, int B, const int32_t *off, const specmemo_kv *kv, const specmemo_prefix *px, int n_q, TreeInfo *ti) {
+  int rc;
+  if ((rc = check_dtype(dt))) return rc;
+  if ((rc = check_offsets(B, off, ti))) return rc;
   return check_walk(dt, *ti, off, kv, px, n_q);
 }
 
@@ -857,7 +862,7 @@ size_t walk_ws_bytes(const WalkPlan &p, int head_dim) {
 
 int run_walk(int dt, bool tree, const TreeInfo &ti, const int32_t *off_h, const int32_t *parent, const specmemo_kv *kv,
              const specmemo_prefix *px, int n_q, float scale, const void *q, void *out, void *ws, size_t ws_bytes,
-             void *stream) {
+             void *stream, const specmemo_kv4 *kv4 = nullptr) {
   if (!(scale > 0.f)) scale = 1.0f / std::sqrt((float)kv->head_dim);
   if (!std::isfinite(scale)) return fail(SPECMEMO_E_ARG, "scale is not finite");
   if (ti.total == 0) return ok();
@@ -897,7 +902,19 @@ int run_walk(int dt, bool tree, const TreeInfo &ti, const int32_t *off_h, const 
     std::copy(p.sets.begin(), p.sets.end(), a.set);
   }
   a.part = reinterpret_cast<float *>(w + tab);
-  return hip_status(launch_walk_attn(dt, tree, a, st), tree ? "tree attention launch" : "prompt attention launch");
+  if (kv4) {
+    a.ks = static_cast<const uint8_t *>(kv4->k_scale);
+    a.vs = static_cast<const uint8_t *>(kv4->v_scale);
+  }
+  return hip_status(kv4 ? launch_walk4_attn(dt, tree, a, st) : launch_walk_attn(dt, tree, a, st),
+                    tree ? "tree attention launch" : "prompt attention launch");
+}
+
+int check_tree_walk(int dt, const specmemo_trees *t, const specmemo_kv *kv, const specmemo_prefix *px, int n_q, TreeInfo *ti) {
+  int rc;
+  if ((rc = check_dtype(dt))) return rc;
+  if ((rc = check_trees(t, ti))) return rc;
+  return check_walk(dt, *ti, t->node_off_h, kv, px, n_q);
 }
 
 int check_tree_prefix(int dt, const specmemo_trees *t, const specmemo_kv *kv, const specmemo_prefix *px, int n_q, TreeInfo *ti) {
@@ -1216,6 +1233,316 @@ int specmemo_accept_compact(specmemo_dtype dt, const specmemo_trees *t, const sp
     if ((e = launch_accept_compact(dt, a, c, st)) != hipSuccess) return hip_status(e, "acceptance and compaction launch");
   }
   return ok();
+}
+
+}  // extern "C"
+
+// ---- new rows of the pool, and the pool in 4 bits ----------------------------------------
+
+namespace {
+
+// The arguments of a specmemo_kv4 that the checks of a pool look at.
+specmemo_kv as_kv(const specmemo_kv4 &p) {
+  return specmemo_kv{p.k, p.v, p.cap_total, p.n_kv, p.head_dim, p.seq_len, p.seq_base_h, p.seq_cap_h, p.seq_len_h};
+}
+
+int check_kv4(const specmemo_kv4 *kv) {
+  if (!kv) return fail(SPECMEMO_E_ARG, "kv is NULL");
+  if (!al(kv->k_scale, 16) || !al(kv->v_scale, 16))
+    return fail(SPECMEMO_E_ARG, "kv->k_scale / kv->v_scale must be non-NULL and 16-byte aligned");
+  if (kv->head_dim % kKv4Group) return fail(SPECMEMO_E_DTYPE, "4-bit pools need a head_dim that is a multiple of %d, got %d", kKv4Group, kv->head_dim);
+  return SPECMEMO_OK;
+}
+
+struct Span {   // bytes of a buffer
+  uintptr_t lo, hi;
+  bool meets(const Span &o) const { return lo < o.hi && o.lo < hi; }
+};
+// n rows of `width` elements, `stride` apart
+Span span(const void *p, int64_t n, int64_t stride, int64_t width, int es) {
+  const uintptr_t lo = (uintptr_t)p;
+  return Span{lo, p && n > 0 ? lo + (uintptr_t)(((n - 1) * stride + width) * es) : lo};
+}
+
+constexpr int64_t kMaxStride = INT64_C(1) << 28;   // elements: sizes in bytes stay within 64 bits
+constexpr int64_t kMaxPoolRows = INT64_C(1) << 46;
+constexpr int kMaxHeadsAppend = 1 << 20;   // heads of a token: q, k and v together
+
+int check_rows(int dt, const specmemo_rows *x, const TreeInfo &ti, int n_q, const specmemo_kv *kv, const specmemo_kv4 *kv4,
+               const void *q_out) {
+  if (!x) return fail(SPECMEMO_E_ARG, "rows is NULL");
+  const int es = dt == SPECMEMO_BF16 ? 2 : 4, d = kv->head_dim, n_kv = kv->n_kv;
+  if (n_q < 0 || (int64_t)n_q + 2 * (int64_t)n_kv > kMaxHeadsAppend) return fail(SPECMEMO_E_ARG, "n_q=%d, n_kv=%d", n_q, n_kv);
+  if (kv->cap_total >= kMaxPoolRows / n_kv) return fail(SPECMEMO_E_ARG, "a pool of %d x %lld rows", n_kv, (long long)kv->cap_total);
+  const int step = 2 * 16 / es;   // both columns of a rotated pair in whole 16-byte chunks
+  if (x->rot_dim < 0 || x->rot_dim > d || x->rot_dim % step)
+    return fail(SPECMEMO_E_ARG, "rot_dim=%d, expected a multiple of %d up to %d", x->rot_dim, step, d);
+  if (x->rot_style != SPECMEMO_ROT_HALVES && x->rot_style != SPECMEMO_ROT_PAIRS) return fail(SPECMEMO_E_ARG, "rot_style=%d", x->rot_style);
+  if ((x->q_norm || x->k_norm) && !(x->eps >= 0.f && std::isfinite(x->eps))) return fail(SPECMEMO_E_ARG, "eps must be finite and not negative");
+  if ((x->q_norm && !al(x->q_norm, 16)) || (x->k_norm && !al(x->k_norm, 16))) return fail(SPECMEMO_E_ARG, "q_norm / k_norm must be 16-byte aligned");
+  if (ti.total == 0) return SPECMEMO_OK;
+  if (x->rot_dim > 0) {
+    if (x->n_pos < 1) return fail(SPECMEMO_E_ARG, "n_pos=%d", x->n_pos);
+    if (!al(x->cos, 16) || !al(x->sin, 16)) return fail(SPECMEMO_E_ARG, "cos / sin must be non-NULL and 16-byte aligned");
+    if (!al(x->pos, 4)) return fail(SPECMEMO_E_ARG, "pos must be non-NULL and 4-byte aligned");
+  }
+  struct {
+    const char *name;
+    const void *p;
+    int64_t stride;
+    int heads;
+  } in[3] = {{"q", x->q, x->q_stride, n_q}, {"k", x->k, x->k_stride, n_kv}, {"v", x->v, x->v_stride, n_kv}};
+  Span is[3];
+  for (int i = 0; i < 3; ++i) {
+    const int64_t width = (int64_t)in[i].heads * d;
+    if (width == 0) {
+      is[i] = Span{0, 0};
+      continue;
+    }
+    if (!al(in[i].p, 16)) return fail(SPECMEMO_E_ARG, "%s must be non-NULL and 16-byte aligned", in[i].name);
+    if (in[i].stride < width || in[i].stride > kMaxStride || in[i].stride * es % 16)
+      return fail(SPECMEMO_E_ARG, "%s_stride=%lld, expected a multiple of 16 bytes of at least %lld elements", in[i].name,
+                  (long long)in[i].stride, (long long)width);
+    is[i] = span(in[i].p, ti.total, in[i].stride, width, es);
+  }
+  if (n_q > 0 && !al(q_out, 16)) return fail(SPECMEMO_E_ARG, "q_out must be non-NULL and 16-byte aligned");
+  const int64_t rows = (int64_t)n_kv * kv->cap_total;
+  const Span out = span(n_q > 0 ? q_out : nullptr, ti.total, (int64_t)n_q * d, (int64_t)n_q * d, es);
+  Span pool[4];
+  const int np = kv4 ? 4 : 2;
+  if (kv4) {
+    pool[0] = span(kv4->k, rows, d / 2, d / 2, 1);
+    pool[1] = span(kv4->v, rows, d / 2, d / 2, 1);
+    pool[2] = span(kv4->k_scale, rows, d / kKv4Group, d / kKv4Group, 1);
+    pool[3] = span(kv4->v_scale, rows, d / kKv4Group, d / kKv4Group, 1);
+  } else {
+    pool[0] = span(kv->k, rows, d, d, es);
+    pool[1] = span(kv->v, rows, d, d, es);
+  }
+  const bool in_place = q_out == x->q && x->q_stride == (int64_t)n_q * d;
+  for (int i = 0; i < 3; ++i) {
+    if (out.meets(is[i]) && !(i == 0 && in_place)) return fail(SPECMEMO_E_ARG, "q_out overlaps %s", in[i].name);
+    for (int j = 0; j < np; ++j)
+      if (pool[j].meets(is[i])) return fail(SPECMEMO_E_ARG, "%s overlaps the pool", in[i].name);
+  }
+  for (int j = 0; j < np; ++j) {
+    if (pool[j].meets(out)) return fail(SPECMEMO_E_ARG, "q_out overlaps the pool");
+    for (int i = 0; i < j; ++i)
+      if (pool[j].meets(pool[i])) return fail(SPECMEMO_E_ARG, "the pool's buffers overlap");
+  }
+  return SPECMEMO_OK;
+}
+
+// Calls launch(args) for every range of tokens that one launch covers: at most
+// kMaxRowsSeq sequences and `per_launch` tokens.
+template <class Args, class F>
+int for_token_ranges(Args &a, const TreeInfo &ti, const int32_t *off, const specmemo_kv *kv, int64_t per_launch, F launch) {
+  int b = 0, tok = 0;
+  while (tok < ti.total) {
+    a.nseq = 0;
+    a.tok0 = tok;
+    const int64_t stop = std::min<int64_t>(ti.total, tok + per_launch);
+    for (; b < ti.B && off[b] < stop && a.nseq < kMaxRowsSeq; ++b) {
+      if (off[b + 1] <= std::max(off[b], tok)) continue;   // nothing left of it
+      const uint64_t row0 = (uint64_t)(kv->seq_base_h[b] + kv->seq_len_h[b] - off[b]);
+      a.seq[a.nseq++] = RowsSeq{off[b], (int32_t)(uint32_t)row0, (int32_t)(uint32_t)(row0 >> 32)};
+      tok = (int)std::min<int64_t>(off[b + 1], stop);
+      if (off[b + 1] > stop) break;                        // the rest comes with the next launch
+    }
+    a.tok1 = tok;
+    const int rc = launch();
+    if (rc) return rc;
+  }
+  return ok();
+}
+
+int append_impl(int dt, int B, const int32_t *off, const specmemo_rows *x, int n_q, const specmemo_kv *kv,
+                const specmemo_kv4 *kv4, void *q_out, void *stream) {
+  TreeInfo ti;
+  int rc;
+  if ((rc = check_dtype(dt))) return rc;
+  if ((rc = check_offsets(B, off, &ti))) return rc;
+  if ((rc = check_kv(dt, kv, ti, off))) return rc;
+  if ((rc = check_rows(dt, x, ti, n_q, kv, kv4, q_out))) return rc;
+  AppendArgs a{};
+  a.q = x->q;
+  a.k = x->k;
+  a.v = x->v;
+  a.q_stride = x->q_stride;
+  a.k_stride = x->k_stride;
+  a.v_stride = x->v_stride;
+  a.q_norm = x->q_norm;
+  a.k_norm = x->k_norm;
+  a.eps = x->eps;
+  a.q_out = q_out;
+  a.pool_k = kv->k;
+  a.pool_v = kv->v;
+  if (kv4) {
+    a.ks = static_cast<uint8_t *>(kv4->k_scale);
+    a.vs = static_cast<uint8_t *>(kv4->v_scale);
+  }
+  a.cap_total = kv->cap_total;
+  a.n_q = n_q;
+  a.n_kv = kv->n_kv;
+  a.head_dim = kv->head_dim;
+  if (x->rot_dim > 0) {
+    a.cos = x->cos;
+    a.sin = x->sin;
+    a.pos = x->pos;
+    a.n_pos = x->n_pos;
+    a.rot_dim = x->rot_dim;
+    a.pairs = x->rot_style == SPECMEMO_ROT_PAIRS;
+  }
+  // at most 2^30 threads a launch, of up to 32 a head
+  const int64_t per_launch = std::max<int64_t>(1, (INT64_C(1) << 25) / (n_q + 2 * kv->n_kv));
+  return for_token_ranges(a, ti, off, kv, per_launch, [&] {
+    return hip_status(launch_append(dt, kv4 != nullptr, a, static_cast<hipStream_t>(stream)), "append launch");
+  });
+}
+
+}  // namespace
+
+extern "C" {
+
+int specmemo_kv_append(specmemo_dtype dt, int32_t B, const int32_t *new_off_h, const specmemo_rows *x, int32_t n_q,
+                       const specmemo_kv *kv, void *q_out, void *stream) {
+  return guarded((int)SPECMEMO_E_ARG, [&] { return append_impl(dt, B, new_off_h, x, n_q, kv, nullptr, q_out, stream); });
+}
+
+int specmemo_kv4_append(specmemo_dtype dt, int32_t B, const int32_t *new_off_h, const specmemo_rows *x, int32_t n_q,
+                        const specmemo_kv4 *kv, void *q_out, void *stream) {
+  return guarded((int)SPECMEMO_E_ARG, [&] {
+    int rc;
+    if ((rc = check_kv4(kv))) return rc;
+    const specmemo_kv view = as_kv(*kv);
+    return append_impl(dt, B, new_off_h, x, n_q, &view, kv, q_out, stream);
+  });
+}
+
+int specmemo_kv4_read(specmemo_dtype dt, int32_t B, const int32_t *new_off_h, const specmemo_kv4 *kv, void *k_out,
+                      void *v_out, void *stream) {
+  return guarded((int)SPECMEMO_E_ARG, [&] {
+    TreeInfo ti;
+    int rc;
+    if ((rc = check_dtype(dt))) return rc;
+    if ((rc = check_offsets(B, new_off_h, &ti))) return rc;
+    if ((rc = check_kv4(kv))) return rc;
+    const specmemo_kv view = as_kv(*kv);
+    if ((rc = check_kv(dt, &view, ti, new_off_h))) return rc;
+    if (kv->n_kv > kMaxHeadsAppend / 2) return fail(SPECMEMO_E_ARG, "n_kv=%d", kv->n_kv);
+    if (kv->cap_total >= kMaxPoolRows / kv->n_kv) return fail(SPECMEMO_E_ARG, "a pool of %d x %lld rows", kv->n_kv, (long long)kv->cap_total);
+    if (ti.total == 0) return ok();
+    if (!al(k_out, 16) || !al(v_out, 16)) return fail(SPECMEMO_E_ARG, "k_out / v_out must be non-NULL and 16-byte aligned");
+    const int64_t width = (int64_t)kv->n_kv * kv->head_dim, rows = (int64_t)kv->n_kv * kv->cap_total;
+    const int es = dt == SPECMEMO_BF16 ? 2 : 4;
+    const Span out[2] = {span(k_out, ti.total, width, width, es), span(v_out, ti.total, width, width, es)};
+    const int cb = kv->head_dim / 2, sb = kv->head_dim / kKv4Group;
+    const Span pool[4] = {span(kv->k, rows, cb, cb, 1), span(kv->v, rows, cb, cb, 1), span(kv->k_scale, rows, sb, sb, 1),
+                          span(kv->v_scale, rows, sb, sb, 1)};
+    if (out[0].meets(out[1])) return fail(SPECMEMO_E_ARG, "k_out overlaps v_out");
+    for (const Span &o : out)
+      for (const Span &p : pool)
+        if (o.meets(p)) return fail(SPECMEMO_E_ARG, "k_out / v_out overlap the pool");
+    ReadArgs a{};
+    a.k = static_cast<const uint8_t *>(kv->k);
+    a.v = static_cast<const uint8_t *>(kv->v);
+    a.ks = static_cast<const uint8_t *>(kv->k_scale);
+    a.vs = static_cast<const uint8_t *>(kv->v_scale);
+    a.k_out = k_out;
+    a.v_out = v_out;
+    a.cap_total = kv->cap_total;
+    a.n_kv = kv->n_kv;
+    a.head_dim = kv->head_dim;
+    // at most 2^30 threads a launch, of up to 16 a row of K or V
+    const int64_t per_launch = std::max<int64_t>(1, (INT64_C(1) << 25) / kv->n_kv);
+    return for_token_ranges(a, ti, new_off_h, &view, per_launch,
+                            [&] { return hip_status(launch_kv4_read(dt, a, static_cast<hipStream_t>(stream)), "read launch"); });
+  });
+}
+
+int specmemo_kv4_prompt_attn(specmemo_dtype dt, int32_t B, const int32_t *new_off_h, const specmemo_kv4 *kv,
+                             const specmemo_prefix *prefix, int32_t n_q, float scale, const void *q, void *out, void *ws,
+                             size_t ws_bytes, void *stream) {
+  return guarded((int)SPECMEMO_E_ARG, [&] {
+    TreeInfo ti;
+    int rc;
+    if ((rc = check_kv4(kv))) return rc;
+    const specmemo_kv view = as_kv(*kv);
+    if ((rc = check_prompt(dt, B, new_off_h, &view, prefix, n_q, &ti))) return rc;
+    return run_walk(dt, false, ti, new_off_h, nullptr, &view, prefix, n_q, scale, q, out, ws, ws_bytes, stream, kv);
+  });
+}
+
+size_t specmemo_kv4_prompt_attn_bytes(specmemo_dtype dt, int32_t B, const int32_t *new_off_h, const specmemo_kv4 *kv,
+                                      const specmemo_prefix *prefix, int32_t n_q) {
+  return guarded((size_t)0, [&] {
+    TreeInfo ti;
+    if (check_kv4(kv)) return (size_t)0;
+    const specmemo_kv view = as_kv(*kv);
+    if (check_prompt(dt, B, new_off_h, &view, prefix, n_q, &ti)) return (size_t)0;
+    return walk_ws_bytes(make_walk(dt, true, ti, new_off_h, &view, prefix, n_q), kv->head_dim);
+  });
+}
+
+int specmemo_kv4_tree_attn(specmemo_dtype dt, const specmemo_trees *t, const specmemo_kv4 *kv,
+                           const specmemo_prefix *prefix, int32_t n_q, float scale, const void *q, void *out, void *ws,
+                           size_t ws_bytes, void *stream) {
+  return guarded((int)SPECMEMO_E_ARG, [&] {
+    TreeInfo ti;
+    int rc;
+    if ((rc = check_kv4(kv))) return rc;
+    const specmemo_kv view = as_kv(*kv);
+    if ((rc = check_tree_walk(dt, t, &view, prefix, n_q, &ti))) return rc;
+    return run_walk(dt, true, ti, t->node_off_h, t->parent, &view, prefix, n_q, scale, q, out, ws, ws_bytes, stream, kv);
+  });
+}
+
+size_t specmemo_kv4_tree_attn_bytes(specmemo_dtype dt, const specmemo_trees *t, const specmemo_kv4 *kv,
+                                    const specmemo_prefix *prefix, int32_t n_q) {
+  return guarded((size_t)0, [&] {
+    TreeInfo ti;
+    if (check_kv4(kv)) return (size_t)0;
+    const specmemo_kv view = as_kv(*kv);
+    if (check_tree_walk(dt, t, &view, prefix, n_q, &ti)) return (size_t)0;
+    return walk_ws_bytes(make_walk(dt, false, ti, t->node_off_h, &view, prefix, n_q), kv->head_dim);
+  });
+}
+
+int specmemo_kv4_compact(const specmemo_trees *t, const specmemo_kv4 *kv, const int32_t *accept_len,
+                         const int32_t *path, int32_t path_stride, void *stream) {
+  return guarded((int)SPECMEMO_E_ARG, [&] {
+    TreeInfo ti;
+    int rc;
+    if ((rc = check_trees(t, &ti))) return rc;
+    if ((rc = check_kv4(kv))) return rc;
+    const specmemo_kv view = as_kv(*kv);
+    if ((rc = check_kv(SPECMEMO_FP32, &view, ti, t->node_off_h))) return rc;   // head_dim up to 128
+    if (kv->n_kv > kMaxGridY) return fail(SPECMEMO_E_ARG, "n_kv=%d exceeds %d", kv->n_kv, kMaxGridY);
+    if (!al(kv->seq_len, 4) || !al(accept_len, 4) || !al(path, 4))
+      return fail(SPECMEMO_E_ARG, "seq_len / accept_len / path must be non-NULL and 4-byte aligned");
+    if (path_stride < 1) return fail(SPECMEMO_E_ARG, "path_stride=%d", path_stride);
+    Compact4Args a{};
+    a.k = static_cast<uint8_t *>(kv->k);
+    a.v = static_cast<uint8_t *>(kv->v);
+    a.ks = static_cast<uint8_t *>(kv->k_scale);
+    a.vs = static_cast<uint8_t *>(kv->v_scale);
+    a.cap_total = kv->cap_total;
+    a.accept_len = accept_len;
+    a.path = path;
+    a.seq_len = kv->seq_len;
+    a.n_kv = kv->n_kv;
+    a.head_dim = kv->head_dim;
+    a.path_stride = path_stride;
+    for (int b = 0; b < ti.B; b += kMaxCompact4Seq) {
+      a.b0 = b;
+      a.nseq = std::min(kMaxCompact4Seq, ti.B - b);
+      for (int s = 0; s < a.nseq; ++s)
+        a.seq[s] = Compact4Seq{kv->seq_base_h[b + s], kv->seq_len_h[b + s], t->node_off_h[b + s + 1] - t->node_off_h[b + s]};
+      const hipError_t e = launch_kv4_compact(a, static_cast<hipStream_t>(stream));
+      if (e != hipSuccess) return hip_status(e, "compaction launch");
+    }
+    return ok();
+  });
 }
 
 }  // extern "C"

@@ -96,6 +96,18 @@ int64_t specmemo_mem_kv_bytes(int32_t layers, int32_t batch, int32_t n_kv, int32
   return r;
 }
 
+int64_t specmemo_mem_kv4_bytes(int32_t layers, int32_t batch, int32_t n_kv, int32_t head_dim, int64_t tokens) {
+  if (layers < 0 || batch < 0 || n_kv < 0 || head_dim < 0 || head_dim % kKv4Group || tokens < 0) {
+    fail(SPECMEMO_E_ARG, "4-bit kv bytes: negative size or head_dim not a multiple of %d", kKv4Group);
+    return -1;
+  }
+  // a group's codes and scale
+  const int64_t r = kv_bytes(layers, batch, n_kv, head_dim / kKv4Group, tokens, kKv4Group / 2 + 1);
+  if (r < 0) fail(SPECMEMO_E_ARG, "kv bytes overflow int64");
+  else ok();
+  return r;
+}
+
 int64_t specmemo_mem_buffer_bytes(int32_t batch, int32_t nodes, int32_t seqs, int32_t levels, int32_t vocab,
                                   int32_t elem_bytes) {
   if (batch < 0 || nodes < 0 || seqs < 0 || levels < 0 || vocab < 0 || elem_bytes < 1) {

@@ -14,6 +14,7 @@ constexpr int kMaxNodes = 128;
 constexpr int kMaxPath = 16;           // max depth + 1
 constexpr int kMaxTopk = 32;
 constexpr int kMaxHeads = 15;
+constexpr int kKv4Group = 32;          // columns of a 4-bit row that share a scale
 
 // Host tables written into device memory by kernels whose arguments carry up
 // to kUploadWords words each (csrc/upload.hip); bytes may be any size, dst
@@ -167,7 +168,8 @@ constexpr int kMaxWalkSets = 76;   // sets described in the kernel arguments
 struct WalkArgs {
   const void *q;
   void *out;
-  const void *k, *v;
+  const void *k, *v;          // rows in the queries' type, or 4-bit codes
+  const uint8_t *ks, *vs;     // scale bytes of a 4-bit pool
   const int32_t *parent;
   float *part;
   const WalkSetPacked *tab;   // more than kMaxWalkSets sets: in the workspace
@@ -232,6 +234,9 @@ __host__ __device__ inline WalkSet walk_expand(const WalkSetPacked &p, int g) {
 // 4-byte words of a part of 32 rows: O in fp32, m and l
 __host__ __device__ constexpr int walk_unit_floats(int dblocks) { return 32 * 32 * dblocks + 64; }
 hipError_t launch_walk_attn(int dt, bool tree, const WalkArgs &a, hipStream_t st);
+hipError_t launch_walk_combine(int dt, const WalkArgs &a, hipStream_t st);
+// The same over a 4-bit pool (kv4_attn.hip); head_dim a multiple of 32.
+hipError_t launch_walk4_attn(int dt, bool tree, const WalkArgs &a, hipStream_t st);
 
 // Host plan (walk_plan.cpp): the batch's sequences with query nodes, in order.
 struct WalkSeq {
@@ -245,6 +250,39 @@ struct WalkPlan {
 };
 void plan_walk(int dt, bool causal, const std::vector<WalkSeq> &seqs, int n_kv, int group, int head_dim, int cus,
                WalkPlan *p);
+
+// ---- new rows of the pool (kv_rows.hip) ------------------------------------------------
+// Token i of the sequence with the last off <= i lies at pool row row0 + i.
+struct RowsSeq {
+  int32_t off, row0_lo, row0_hi;
+};
+constexpr int kMaxRowsSeq = 316;   // sequences of a launch
+struct AppendArgs {
+  const void *q, *k, *v;          // token i's heads at i * stride elements
+  int64_t q_stride, k_stride, v_stride;
+  const void *q_norm, *k_norm;    // [head_dim] or null
+  const float *cos, *sin;         // [n_pos][rot_dim / 2]
+  const int32_t *pos;             // null: no rotation
+  void *q_out;                    // [tokens][n_q][head_dim]
+  void *pool_k, *pool_v;          // [n_kv][cap_total][head_dim], or codes
+  uint8_t *ks, *vs;               // scale bytes of a 4-bit pool
+  int64_t cap_total;
+  int32_t n_q, n_kv, head_dim, n_pos, rot_dim, pairs;
+  float eps;
+  int32_t tok0, tok1;             // tokens of this launch
+  int32_t nseq;
+  RowsSeq seq[kMaxRowsSeq];
+};
+static_assert(sizeof(AppendArgs) <= 4096, "kernel arguments are limited to 4 KB");
+hipError_t launch_append(int dt, bool four, const AppendArgs &a, hipStream_t st);
+struct ReadArgs {
+  const uint8_t *k, *v, *ks, *vs;
+  void *k_out, *v_out;            // [tokens][n_kv][head_dim]
+  int64_t cap_total;
+  int32_t n_kv, head_dim, tok0, tok1, nseq;
+  RowsSeq seq[kMaxRowsSeq];
+};
+hipError_t launch_kv4_read(int dt, const ReadArgs &a, hipStream_t st);
 
 // ---- acceptance ------------------------------------------------------------------
 struct AcceptArgs {
@@ -327,6 +365,22 @@ struct CompactArgs {
   CompactSeq seq[kMaxSeqPerLaunch];
 };
 hipError_t launch_kv_compact(const CompactArgs &a, hipStream_t st);
+// Compaction of a 4-bit pool: a row is codes and scales.
+struct Compact4Seq {
+  int64_t base;
+  int32_t L, N;
+};
+constexpr int kMaxCompact4Seq = 240;
+struct Compact4Args {
+  uint8_t *k, *v, *ks, *vs;
+  int64_t cap_total;
+  const int32_t *accept_len, *path;
+  int32_t *seq_len;
+  int32_t n_kv, head_dim, path_stride, b0, nseq;
+  Compact4Seq seq[kMaxCompact4Seq];
+};
+static_assert(sizeof(Compact4Args) <= 4096, "kernel arguments are limited to 4 KB");
+hipError_t launch_kv4_compact(const Compact4Args &a, hipStream_t st);
 // Acceptance with the compaction fused into its second pass (one launch group
 // of sequences; the row pass of launch_accept_rows must precede it).
 hipError_t launch_accept_rows(int dt, const AcceptArgs &a, int total_nodes, hipStream_t st);

@@ -1,0 +1,415 @@
+// Attention over a pool in 4 bits (kv4.h): prompt tokens, chunks of prompts and single
+// tokens (causal), and candidate trees, with or without a prefix that sequences share.
+//
+// SpecMemo Sec. 3.1: the cache is what the memory budget goes to; a row of 128
+// columns takes 68 bytes instead of 256.  Work items, masks, the one-pass softmax and
+// the merge of parts are those of the attention over key ranges (walk.h,
+// walk_tile.h); what differs is how the rows reach the matrix cores.
+//
+// bf16 queries:
+//   S^T = K Q^T   K's codes and scales are operands as they lie: the scaled product
+//                 of 32 x 32 x 64 takes 4-bit values with a scale for each lane's 32
+//                 columns.  Its other operand holds six bits, so a query is three of
+//                 them, q = q0 2^e + q1 2^(e-4) + q2 2^(e-10), each the rest of the one
+//                 before: with e from the 32 columns' largest magnitude (in (3.75,
+//                 7.5] x 2^e) that is every bf16 value down to 2^-8 of the largest, and
+//                 smaller ones within 2^-16 of the largest.  Three such products take
+//                 0.76 of the time of the bf16 products of the same columns (15.9 ns
+//                 against 2 x 15.6 for 32 columns x 2), and K is neither converted nor
+//                 read from LDS in 16 bits.
+//   O^T = V^T P^T V is contracted over keys, whose scales differ, so a tile is
+//                 converted to bf16 once (by the block's four waves, on its way to LDS)
+//                 and read by the transposing loads.
+#include <type_traits>
+
+#include "device.h"
+#include "internal.h"
+#include "kv4.h"
+#include "walk.h"
+#include "walk_tile.h"
+
+namespace specmemo {
+
+namespace {
+
+constexpr int D = kAttnHeadDim;
+constexpr int TK = kAttnKeyTile;
+constexpr int kRow4 = D / 2;                  // bytes of a row's codes
+constexpr int kScales = D / kKv4Group;        // and of its scales
+constexpr int kWaves4 = 4;
+constexpr int kKTile4 = TK * kRow4;           // 4 KB of codes
+constexpr int kVTile4 = TK * D * 2;           // 16 KB in bf16
+
+typedef int i32x8_t __attribute__((ext_vector_type(8)));
+typedef uint32_t u32x6_t __attribute__((ext_vector_type(6)));
+typedef __bf16 bf16x32_t __attribute__((ext_vector_type(32)));
+
+// A wave's queries as the scaled product's operands: step s takes columns 64 s + 32 h
+// .. + 31 of a lane's row, scale byte i of sc[s] is part i's.
+struct Query6 {
+  u32x6_t part[2][3];
+  uint32_t sc[2];
+
+  __device__ __forceinline__ void load(bool ok, const uint16_t *row, int h) {
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      uint4 w[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[i] = ld16_or_zero(ok, row + 64 * s + 32 * h + 8 * i);
+      bf16x32_t x;
+      __builtin_memcpy(&x, w, sizeof(x));
+      float top = 0.f;
+#pragma unroll
+      for (int i = 0; i < 32; ++i) top = fmaxf(top, fabsf((float)x[i]));
+      // 7.5 = 1.875 x 4; magnitudes under 2^-113 are lost (scores of nothing)
+      const uint32_t u = __float_as_uint(top);
+      const uint32_t e = max((int)(u >> 23) - 2 + ((u & 0x7FFFFFu) > 0x700000u), 14);
+      sc[s] = e | (e - 4) << 8 | (e - 10) << 16;
+#pragma unroll
+      for (int p = 0; p < 3; ++p) {
+        const float unit = __uint_as_float((e - (p == 0 ? 0 : p == 1 ? 4 : 10)) << 23);
+        part[s][p] = __builtin_amdgcn_cvt_scalef32_pk32_fp6_bf16(x, unit);
+        if (p < 2) {
+          const bf16x32_t y = __builtin_amdgcn_cvt_scalef32_pk32_bf16_fp6(part[s][p], unit);
+#pragma unroll
+          for (int i = 0; i < 32; ++i) x[i] = (__bf16)((float)x[i] - (float)y[i]);   // exact
+        }
+      }
+    }
+  }
+};
+
+template <int STEP, int PART>
+__device__ __forceinline__ f32x16 qk_part(uint4 k, const Query6 &q, f32x16 c, uint32_t kscale) {
+  const i32x8_t a = {(int)k.x, (int)k.y, (int)k.z, (int)k.w, 0, 0, 0, 0};
+  const u32x6_t &w = q.part[STEP][PART];
+  const i32x8_t b = {(int)w[0], (int)w[1], (int)w[2], (int)w[3], (int)w[4], (int)w[5], 0, 0};
+  // formats: 4 = four bits, 2 = six bits; the scale byte of each operand is chosen by number
+  return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, c, 4, 2, 2 * STEP, (int)kscale, PART, (int)q.sc[STEP]);
+}
+
+// Four waves per block; K codes and V values each have a two-slot ring of 64-key
+// tiles.  KSPLIT as in the attention over rows of 16 bits: 1: every wave takes whole
+// tiles for its 32 rows; 2: two groups of waves over the same rows, one for each half
+// of a tile's keys, merged at the end.
+template <int KSPLIT, bool TREE>
+__device__ __forceinline__ void walk4(const WalkArgs &a, const WalkItem &it, uint8_t (*kring)[kKTile4], uint8_t (*vring)[kVTile4]) {
+  constexpr int RW = kWaves4 / KSPLIT, RB = 32 * RW, NSB = 2 / KSPLIT;
+  int *const par = reinterpret_cast<int *>(vring[1]);   // filled after the first loop barrier
+  static_assert(kWaves4 * 64 >= kMaxNodes && kMaxNodes * 4 <= kVTile4, "one thread per tree node");
+  static_assert(KSPLIT == 1 || (RW * 64 * 64 * 4 <= 2 * kVTile4 && RW * 2 * 64 * 4 <= kKTile4), "merge buffers fit the rings");
+
+  const WalkSet &S = it.S;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int rwave = __builtin_amdgcn_readfirstlane(wave % RW), ksb = __builtin_amdgcn_readfirstlane(wave / RW);
+  const int h = lane >> 5, g = a.group, L = S.L, P = S.P;
+  const int rows = S.T * g;
+  const int np = (P + TK - 1) / TK;                     // prefix tiles
+  const int kend = walk_keys(S, it.rb, g);              // slab keys of this row block
+  const int j0 = it.ch * S.ct, j1 = min(np + (kend + TK - 1) / TK, j0 + S.ct);
+
+  const int64_t head = (int64_t)it.kvh * a.cap_total;
+  const int64_t prow = head + S.pbase, srow = head + S.base;
+  const uint8_t *const K0 = static_cast<const uint8_t *>(a.k), *const V0 = static_cast<const uint8_t *>(a.v);
+
+  // K codes: wave w loads rows 16 w .. + 15 of a tile, lane l bytes [16 l, +16) of its
+  // kilobyte: row 16 w + l / 4, whose logical chunk c lies at c ^ (row / 4 % 4), so that
+  // 16 lanes that read one chunk of 16 rows meet 16 different bank groups.
+  const int krow = 16 * wave + (lane >> 2);
+  const uint32_t kcol = 16 * ((lane & 3) ^ ((lane >> 4) & 3));
+  // V codes: thread t has word t % 4 of each of the four groups of row t / 4, so that the
+  // values' 16-byte chunks 4 i + t % 4 spread over the banks as the rows' swizzle does.
+  const int vrow = tid >> 2, vword = tid & 3;
+  struct Raw {
+    uint32_t code[4], scale;
+  };
+  auto place = [&](int j, int &kt, int &end, int64_t &row0) __attribute__((always_inline)) {
+    const bool pre = j < np;
+    kt = (pre ? j : j - np) * TK;
+    end = pre ? P : kend;
+    row0 = pre ? prow : srow;
+  };
+  // rows past the end repeat the last one (finite values, masked out)
+  auto issue_k = [&](uint8_t *dst, int j) __attribute__((always_inline)) {
+    int kt, end;
+    int64_t row0;
+    place(j, kt, end, row0);
+    const uint8_t *src = uniform_ptr(K0 + row0 * kRow4);
+    const uint32_t lds = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_void_t *)(dst + 1024 * wave));
+    lds_load16(src, (uint32_t)min(kt + krow, end - 1) * kRow4 + kcol, lds);
+  };
+  auto load_v = [&](Raw &w, int j) __attribute__((always_inline)) {
+    int kt, end;
+    int64_t row0;
+    place(j, kt, end, row0);
+    const uint32_t r = (uint32_t)min(kt + vrow, end - 1);
+    const uint8_t *src = V0 + row0 * kRow4;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w.code[i] = *reinterpret_cast<const uint32_t *>(src + r * kRow4 + 16 * i + 4 * vword);
+    w.scale = *reinterpret_cast<const uint32_t *>(a.vs + row0 * kScales + r * kScales);
+  };
+  auto store_v = [&](const Raw &w, uint8_t *dst) __attribute__((always_inline)) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      *reinterpret_cast<uint4 *>(dst + vrow * (D * 2) + 16 * vswz(vrow, 4 * i + vword)) =
+          kv4_bf16x8(w.code[i], kv4_scale(w.scale >> (8 * i) & 255u));
+  };
+  // K scales: a lane's rows of the sub-blocks, shifted to its half's groups (h and 2 + h)
+  auto load_ks = [&](uint32_t (&sc)[NSB], int j) __attribute__((always_inline)) {
+    int kt, end;
+    int64_t row0;
+    place(j, kt, end, row0);
+#pragma unroll
+    for (int sb = 0; sb < NSB; ++sb) {
+      const uint32_t r = (uint32_t)min(kt + 32 * (ksb * NSB + sb) + (lane & 31), end - 1);
+      sc[sb] = *reinterpret_cast<const uint32_t *>(a.ks + row0 * kScales + r * kScales);
+    }
+  };
+
+  Raw raw;
+  uint32_t ksn[NSB];
+  issue_k(kring[0], j0);
+  load_v(raw, j0);
+  load_ks(ksn, j0);
+  const bool tree = TREE && S.slab;      // the set's slab rows end in a tree
+  const int pn = tree && tid < S.T ? a.parent[S.row0 + tid] : -1;
+  const int row0 = it.rb * RB + rwave * 32, my_row = row0 + (lane & 31);
+  const bool row_ok = my_row < rows;
+  const int node = row_ok ? my_row / g : S.T - 1;
+  const int hq = it.kvh * g + (row_ok ? my_row % g : 0);
+  Query6 Q;
+  Q.load(row_ok, static_cast<const uint16_t *>(a.q) + ((int64_t)(S.row0 + node) * a.n_q + hq) * D, h);
+  if (tree && tid < S.T) par[tid] = pn;
+  WalkMask M{L, P, h, node};
+  if (TREE) {
+    ring_barrier();
+    if (tree) M.root_path(par, node);
+  }
+  const int lim_hi = L + min(rows - 1, row0 + 31) / g;   // causal: the last slab key of the wave's last row
+  const bool wave_rows = row0 < rows;    // a wave without rows only loads, converts and waits
+  store_v(raw, vring[0]);
+  if (j0 + 1 < j1) load_v(raw, j0 + 1);
+
+  int kro[2];
+#pragma unroll
+  for (int s = 0; s < 2; ++s) kro[s] = (lane & 31) * kRow4 + 16 * ((2 * s + h) ^ ((lane >> 2) & 3));
+  int vro[D / 32];
+  walk_v_offsets(vro);
+  const int sb0 = ksb * NSB;
+  WalkAcc A;
+
+  auto work = [&](const uint8_t *ks, const uint8_t *vs, const uint32_t (&ksc)[NSB], int j) __attribute__((always_inline)) {
+    const bool pre = j < np;
+    const int kt = (pre ? j : j - np) * TK;
+    if (!pre && !TREE && kt + 32 * sb0 > lim_hi) return;   // past every row of the wave
+    f32x16 Sc[NSB];
+    uint4 kf[NSB][2];
+#pragma unroll
+    for (int sb = 0; sb < NSB; ++sb)
+#pragma unroll
+      for (int s = 0; s < 2; ++s) kf[sb][s] = *reinterpret_cast<const uint4 *>(ks + (sb0 + sb) * 32 * kRow4 + kro[s]);
+#pragma unroll
+    for (int sb = 0; sb < NSB; ++sb) {
+#pragma unroll
+      for (int r2 = 0; r2 < 16; ++r2) Sc[sb][r2] = 0.f;
+      const uint32_t sc = ksc[sb] >> (8 * h);
+      Sc[sb] = qk_part<0, 2>(kf[sb][0], Q, Sc[sb], sc);
+      Sc[sb] = qk_part<1, 2>(kf[sb][1], Q, Sc[sb], sc);
+      Sc[sb] = qk_part<0, 1>(kf[sb][0], Q, Sc[sb], sc);
+      Sc[sb] = qk_part<1, 1>(kf[sb][1], Q, Sc[sb], sc);
+      Sc[sb] = qk_part<0, 0>(kf[sb][0], Q, Sc[sb], sc);
+      Sc[sb] = qk_part<1, 0>(kf[sb][1], Q, Sc[sb], sc);
+    }
+    walk_mask<NSB, TREE>(Sc, M, pre, kt, pre ? P : kend, 32 * sb0);
+    walk_softmax_pv<NSB>(Sc, A, vs + 32 * sb0 * (D * 2), vro, a.scale_log2);
+  };
+
+  // Iteration j waits for tile j's loads; after its barrier every wave is done with
+  // tile j - 1, whose slots take tile j + 1: K's codes by direct loads, V's from the
+  // registers that they were loaded to an iteration ago.
+  auto tile = [&](int j, auto slot_c) __attribute__((always_inline)) {
+    constexpr int slot = decltype(slot_c)::value;
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    ring_barrier();
+    uint32_t ksc[NSB];
+#pragma unroll
+    for (int sb = 0; sb < NSB; ++sb) ksc[sb] = ksn[sb];
+    if (j + 1 < j1) {
+      issue_k(kring[slot ^ 1], j + 1);
+      load_ks(ksn, j + 1);
+      store_v(raw, vring[slot ^ 1]);
+      if (j + 2 < j1) load_v(raw, j + 2);
+    }
+    if (wave_rows) work(kring[slot], vring[slot], ksc, j);
+  };
+  for (int j = j0; j < j1; j += 2) {
+    tile(j, std::integral_constant<int, 0>{});
+    if (j + 1 < j1) tile(j + 1, std::integral_constant<int, 1>{});
+  }
+
+  walk_finish<KSPLIT>(a, it, A, row_ok, wave_rows, node, hq, rwave, ksb, reinterpret_cast<float *>(vring[0]),
+                      reinterpret_cast<float *>(kring[0]));
+}
+
+template <bool TREE>
+__global__ __launch_bounds__(kWaves4 * 64, 2) void walk4_attn_bf16(WalkArgs a) {
+  __shared__ __attribute__((aligned(1024))) uint8_t kring[2][kKTile4];
+  __shared__ __attribute__((aligned(1024))) uint8_t vring[2][kVTile4];
+  WalkItem it;
+  decode_walk(a, blockIdx.x, it);
+  if (it.S.rb == 64) walk4<2, TREE>(a, it, kring, vring);
+  else walk4<1, TREE>(a, it, kring, vring);
+}
+
+// fp32 queries: the arrangement of the fp32 attention over rows of 32 bits (32 query
+// rows a block on the 32x32x2 product, the waves taking 32-key tiles in turn, merged
+// through LDS), with the rows converted to fp32 as they are read.  DB: 32-column
+// groups of the head; lane half h contracts columns 16 DB h .. + 16 DB - 1.
+constexpr int kF32Waves = 4;
+
+template <int DB, bool TREE>
+__global__ __launch_bounds__(64 * kF32Waves, 2) void walk4_attn_f32(WalkArgs a) {
+  constexpr int RB = 32, W = kF32Waves, UF = walk_unit_floats(DB), DD = 32 * DB;
+  constexpr int VR = DB <= 2 ? 16 : 4;   // key rows of V loaded together
+  __shared__ __attribute__((aligned(16))) float merge[W][UF];
+  __shared__ int par[kMaxNodes];
+  WalkItem it;
+  decode_walk(a, blockIdx.x, it);
+  const WalkSet &S = it.S;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int h = lane >> 5, g = a.group, L = S.L, P = S.P;
+  const int rows = S.T * g;
+  const int np = (P + TK - 1) / TK;
+  const int kend = walk_keys(S, it.rb, g);
+  const int j0 = it.ch * S.ct, j1 = min(np + (kend + TK - 1) / TK, j0 + S.ct);
+  const int64_t head = (int64_t)it.kvh * a.cap_total;
+  const uint8_t *const K0 = static_cast<const uint8_t *>(a.k), *const V0 = static_cast<const uint8_t *>(a.v);
+
+  const bool tree = TREE && S.slab;
+  const int my_row = it.rb * RB + (lane & 31);
+  const bool row_ok = my_row < rows;
+  const int node = row_ok ? my_row / g : S.T - 1;
+  const int hq = it.kvh * g + (row_ok ? my_row % g : 0);
+  f32x4 qf[4 * DB];
+  {
+    const float *qp = static_cast<const float *>(a.q) + ((int64_t)(S.row0 + node) * a.n_q + hq) * DD + 16 * DB * h;
+#pragma unroll
+    for (int t = 0; t < 4 * DB; ++t) {
+      qf[t] = f32x4{0.f, 0.f, 0.f, 0.f};
+      if (row_ok) qf[t] = *reinterpret_cast<const f32x4 *>(qp + 4 * t);
+    }
+  }
+  WalkMask M{L, P, h, node};
+  if (TREE) {
+    if (tree && tid < S.T) par[tid] = a.parent[S.row0 + tid];
+    ring_barrier();                                  // (does not wait for the queries)
+    if (tree) M.root_path(par, node);
+  }
+
+  float m = -INFINITY, l = 0.f;
+  f32x16 O[DB];
+#pragma unroll
+  for (int i = 0; i < DB; ++i)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) O[i][r] = 0.f;
+  for (int t2 = 2 * j0 + wave; t2 < 2 * j1; t2 += W) {
+    const bool pre = (t2 >> 1) < np;
+    const int kt = (pre ? t2 : t2 - 2 * np) * 32, end = pre ? P : kend;
+    if (kt >= end) continue;
+    const int64_t base = head + (pre ? S.pbase : S.base);
+    const int64_t kr = base + min(kt + (lane & 31), end - 1);
+    uint2 kc[DB];                                    // 16 columns each
+    uint32_t ksc[DB];                                // and their scale
+#pragma unroll
+    for (int i = 0; i < DB; ++i) {
+      kc[i] = *reinterpret_cast<const uint2 *>(K0 + kr * (DD / 2) + 8 * (DB * h + i));
+      ksc[i] = a.ks[kr * DB + ((DB * h + i) >> 1)];
+    }
+    uint32_t vc[VR][DB], vsc[VR][DB];                // a column's byte of key rows, and its scale
+    auto load_v = [&](int r0) __attribute__((always_inline)) {
+#pragma unroll
+      for (int r = 0; r < VR; ++r) {
+        const int64_t vr = base + min(kt + 8 * ((r0 + r) >> 2) + 4 * h + ((r0 + r) & 3), end - 1);
+#pragma unroll
+        for (int i = 0; i < DB; ++i) {
+          vc[r][i] = V0[vr * (DD / 2) + 16 * i + ((lane & 31) >> 1)];
+          vsc[r][i] = a.vs[vr * DB + i];
+        }
+      }
+    };
+    if (VR == 16) load_v(0);
+    f32x16 Sc[1];
+#pragma unroll
+    for (int r = 0; r < 16; ++r) Sc[0][r] = 0.f;
+#pragma unroll
+    for (int i = 0; i < DB; ++i) {
+      const float s = kv4_scale(ksc[i]);
+      const f32x2_t kv[8] = {kv4_f32x2<0>(kc[i].x, s), kv4_f32x2<1>(kc[i].x, s), kv4_f32x2<2>(kc[i].x, s), kv4_f32x2<3>(kc[i].x, s),
+                             kv4_f32x2<0>(kc[i].y, s), kv4_f32x2<1>(kc[i].y, s), kv4_f32x2<2>(kc[i].y, s), kv4_f32x2<3>(kc[i].y, s)};
+#pragma unroll
+      for (int c = 0; c < 16; ++c)
+        Sc[0] = __builtin_amdgcn_mfma_f32_32x32x2f32(kv[c >> 1][c & 1], qf[4 * i + (c >> 2)][c & 3], Sc[0], 0, 0, 0);
+    }
+    walk_mask<1, TREE>(Sc, M, pre, kt, end, 0);
+    float tm = -INFINITY;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) tm = fmaxf(tm, Sc[0][r]);
+    const float mn = fmaxf(m, max_with_other_half(tm) * a.scale_log2);
+    const float m_use = mn == -INFINITY ? 0.f : mn;
+    const float alpha = m == -INFINITY ? 0.f : fast_exp2(m - m_use);
+    m = mn;
+    l *= alpha;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      Sc[0][r] = fast_exp2(fmaf(Sc[0][r], a.scale_log2, -m_use));
+      l += Sc[0][r];
+    }
+#pragma unroll
+    for (int i = 0; i < DB; ++i)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) O[i][r] *= alpha;
+#pragma unroll
+    for (int r0 = 0; r0 < 16; r0 += VR) {
+      if (VR < 16) load_v(r0);
+#pragma unroll
+      for (int r = 0; r < VR; ++r)
+#pragma unroll
+        for (int i = 0; i < DB; ++i) {
+          const f32x2_t v = kv4_f32x2<0>(vc[r][i], kv4_scale(vsc[r][i]));
+          O[i] = __builtin_amdgcn_mfma_f32_32x32x2f32(lane & 1 ? v[1] : v[0], Sc[0][r0 + r], O[i], 0, 0, 0);
+        }
+    }
+  }
+  walk_finish_f32<DB, W>(a, it, O, m, l, row_ok, node, hq, merge);
+}
+
+template <int DB, bool TREE>
+void launch4_f32(const WalkArgs &a, hipStream_t st) {
+  hipLaunchKernelGGL((walk4_attn_f32<DB, TREE>), dim3(a.blocks), dim3(64 * kF32Waves), 0, st, a);
+}
+
+template <bool TREE>
+void launch4_f32(const WalkArgs &a, hipStream_t st) {
+  switch (a.head_dim / 32) {
+    case 1: return launch4_f32<1, TREE>(a, st);
+    case 2: return launch4_f32<2, TREE>(a, st);
+    case 3: return launch4_f32<3, TREE>(a, st);
+    default: return launch4_f32<4, TREE>(a, st);
+  }
+}
+
+}  // namespace
+
+hipError_t launch_walk4_attn(int dt, bool tree, const WalkArgs &a, hipStream_t st) {
+  if (dt == 0) {
+    tree ? launch4_f32<true>(a, st) : launch4_f32<false>(a, st);
+  } else if (tree) {
+    hipLaunchKernelGGL((walk4_attn_bf16<true>), dim3(a.blocks), dim3(kWaves4 * 64), 0, st, a);
+  } else {
+    hipLaunchKernelGGL((walk4_attn_bf16<false>), dim3(a.blocks), dim3(kWaves4 * 64), 0, st, a);
+  }
+  const hipError_t e = hipGetLastError();
+  return e != hipSuccess || !a.cblocks ? e : launch_walk_combine(dt, a, st);
+}
+
+}  // namespace specmemo

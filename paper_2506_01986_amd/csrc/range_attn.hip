@@ -23,9 +23,10 @@
 // taking 32-key tiles in turn straight from memory, merged through LDS.
 #include <type_traits>
 
-#include "attn_tile.h"
 #include "device.h"
 #include "internal.h"
+#include "walk.h"
+#include "walk_tile.h"
 
 namespace specmemo {
 
@@ -33,130 +34,6 @@ namespace {
 
 constexpr int D = kAttnHeadDim;
 constexpr int TK = kAttnKeyTile;
-constexpr float kRescaleSlack = 8.f;   // log2 units: softmax weights stay <= 256 between rescales
-
-struct WalkItem {
-  WalkSet S;
-  int kvh, rb, ch;
-};
-
-// The kernel arguments where they lie, read by scalar loads (an array of the
-// arguments indexed through a pointer that may also point elsewhere would be copied
-// to scratch memory as a whole).
-typedef __attribute__((address_space(4))) const WalkArgs KernArgs;
-__device__ __forceinline__ KernArgs *kern_args() { return (KernArgs *)__builtin_amdgcn_kernarg_segment_ptr(); }
-
-// The set that block k belongs to: the last one with first block <= k.
-template <bool COMBINE>
-__device__ __forceinline__ int find_set(const WalkArgs &a, int k) {
-  const int lane = threadIdx.x & 63;
-  int lo = 0, cnt = a.nset;
-  while (cnt > 1) {   // 64 ways a round: two rounds for up to 4096 sets
-    const int st = (cnt + 63) >> 6, at = lane * st;
-    int first = 0;
-    if (at < cnt) {
-      if (a.tab) first = COMBINE ? a.tab[lo + at].ccum : a.tab[lo + at].cum;
-      else first = COMBINE ? a.set[lo + at].ccum : a.set[lo + at].cum;
-    }
-    const int p = __builtin_popcountll(__builtin_amdgcn_ballot_w64(at < cnt && first <= k)) - 1;
-    lo += p * st;
-    cnt = min(st, cnt - p * st);
-  }
-  return lo;
-}
-
-// Set s, in SGPRs (the direct loads need their base there): from the arguments by
-// scalar loads, from the workspace table one word a lane.
-__device__ __forceinline__ WalkSet get_set(const WalkArgs &a, int s) {
-  constexpr int N = sizeof(WalkSetPacked) / 4;
-  static_assert(sizeof(WalkSetPacked) % 4 == 0 && N <= 64, "copied by words");
-  s = __builtin_amdgcn_readfirstlane(s);
-  int w[N];
-  if (a.tab) {
-    const int v = reinterpret_cast<const int *>(a.tab + s)[min((int)(threadIdx.x & 63), N - 1)];
-#pragma unroll
-    for (int i = 0; i < N; ++i) w[i] = __builtin_amdgcn_readlane(v, i);
-  } else {
-    const auto *p = (__attribute__((address_space(4))) const int *)&kern_args()->set[s];
-#pragma unroll
-    for (int i = 0; i < N; ++i) w[i] = p[i];
-  }
-  WalkSetPacked P;
-  __builtin_memcpy(&P, w, sizeof(P));
-  return walk_expand(P, a.group);
-}
-
-// A set's blocks are its items times the KV heads, KV head fastest, without gaps.
-// Blocks reach the eight XCDs round-robin and every set begins at a multiple of
-// n_kv, so a KV head's items run on the XCDs that equal it modulo gcd(n_kv, 8), on
-// one where n_kv is a multiple of eight, and read its K/V through those L2s.
-// (Empty blocks that even out the XCDs' counts set by set push two of the others to
-// one compute unit: one KV head, 40 trees of 64 nodes x 4 heads over a prefix of 4096
-// keys 79.4 us, 68.9 without; 256 single tokens over 200 to 1000 keys 42.7, 29.6.)
-template <bool COMBINE>
-__device__ __forceinline__ void decode_unit(const WalkArgs &a, int bid, WalkSet &S, int &kvh, int &i) {
-  S = get_set(a, find_set<COMBINE>(a, bid));
-  const int n = bid - (COMBINE ? S.ccum : S.cum);
-  kvh = n % a.n_kv;
-  i = n / a.n_kv;
-}
-
-__device__ __forceinline__ void decode_walk(const WalkArgs &a, int bid, WalkItem &it) {
-  int i;
-  decode_unit<false>(a, bid, it.S, it.kvh, i);
-  const WalkSet &S = it.S;
-  if (S.nch == 1) {              // longest row blocks first
-    it.ch = 0;
-    it.rb = S.nrb - 1 - i;
-  } else if (!S.causal || S.nrb == 1) {
-    it.ch = i / S.nrb;
-    it.rb = i % S.nrb;
-  } else {                       // chunk by chunk, the row blocks that reach it: at most 64 chunks, one a lane
-    const int lane = threadIdx.x & 63;
-    const int r0 = lane < S.nch ? walk_first_rb(S, lane, a.group) : S.nrb;
-    int before = S.nrb - r0;
-#pragma unroll
-    for (int off = 1; off < 64; off <<= 1) {
-      const int o = __shfl_up(before, off);
-      before += lane >= off ? o : 0;
-    }
-    const int c = __builtin_popcountll(__builtin_amdgcn_ballot_w64(lane < S.nch && before <= i));
-    it.ch = c;
-    it.rb = i - (__shfl(before, c) - (S.nrb - __shfl(r0, c))) + __shfl(r0, c);
-  }
-  it.rb = __builtin_amdgcn_readfirstlane(it.rb);
-  it.ch = __builtin_amdgcn_readfirstlane(it.ch);
-}
-
-// First 32-row unit of the parts of (row block, chunk).
-__device__ __forceinline__ int walk_part(const WalkArgs &a, const WalkSet &S, int kvh, int rb, int ch) {
-  int i;   // index among the set's items
-  if (S.nch == 1) i = S.nrb - 1 - rb;
-  else if (!S.causal || S.nrb == 1) i = ch * S.nrb + rb;
-  else {
-    i = rb - walk_first_rb(S, ch, a.group);
-    for (int c = 0; c < ch; ++c) i += S.nrb - walk_first_rb(S, c, a.group);
-  }
-  return S.part0 + (kvh * S.items + i) * (S.rb >> 5);
-}
-
-// A wave's 32 rows of unnormalised O^T (accumulator order, so that a store of whole
-// rows is 1 KB in one piece), m and l; rows that do not exist are left out (64
-// sequences of 8 rows: a quarter of the traffic).
-template <int DB>
-__device__ __forceinline__ void write_part(float *u, const f32x16 (&O)[DB], float m, float l, bool row_ok) {
-  const int lane = threadIdx.x & 63;
-  if (!row_ok) return;
-#pragma unroll
-  for (int i = 0; i < DB; ++i)
-#pragma unroll
-    for (int q = 0; q < 4; ++q)
-      *reinterpret_cast<f32x4 *>(u + ((4 * i + q) * 64 + lane) * 4) = f32x4{O[i][4 * q], O[i][4 * q + 1], O[i][4 * q + 2], O[i][4 * q + 3]};
-  if (lane < 32) {
-    u[DB * 1024 + lane] = m;
-    u[DB * 1024 + 32 + lane] = l;
-  }
-}
 
 constexpr int kBf16Waves = 4;
 constexpr int kTileBytes = TK * D * 2;        // one K or V tile (16 KB)
@@ -234,39 +111,23 @@ __device__ __forceinline__ void walk_bf16(const WalkArgs &a, const WalkItem &it,
   // land the Q loads here: a load pending at loop entry is waited for on every iteration
 #pragma unroll
   for (int ks = 0; ks < D / 16; ++ks) asm volatile("" ::"v"(qf[ks]));
-  uint64_t alo = 0, ahi = 0;             // ancestor-or-self bits of this lane's node
+  WalkMask M{L, P, h, node};
   if (TREE) {
     ring_barrier();
-    if (tree)
-      for (int u = node; u >= 0; u = par[u]) {
-        alo |= u < 64 ? 1ull << (u & 63) : 0ull;
-        ahi |= u < 64 ? 0ull : 1ull << (u & 63);
-      }
+    if (tree) M.root_path(par, node);
   }
-  // causal: the last slab key of this lane's row, and of the wave's first and last row
-  const int lim = L + node;
-  const int lim_lo = L + __builtin_amdgcn_readfirstlane(node);
+  // causal: the last slab key of the wave's last row
   const int lim_hi = L + min(rows - 1, row0 + 31) / g;
   const bool wave_rows = row0 < rows;    // a wave without rows only loads and waits
 
   int kro[D / 16];
 #pragma unroll
   for (int ks = 0; ks < D / 16; ++ks) kro[ks] = (lane & 31) * (D * 2) + 16 * ((2 * ks + h) ^ (lane & 15));
-  const int tj = (lane & 15) >> 2, tq = lane & 3;
-  const int te = 2 * ((lane >> 4) & 1) + (tq >> 1);
   int vro[D / 32];
-#pragma unroll
-  for (int i = 0; i < D / 32; ++i) vro[i] = (4 * h + tj) * (D * 2) + 64 * (i ^ tj) + 16 * te + 8 * (tq & 1);
+  walk_v_offsets(vro);
   const int sb0 = ksb * NSB;
 
-  float m = -INFINITY, lsum = 0.f;
-  f32x16 O[D / 32];
-#pragma unroll
-  for (int i = 0; i < D / 32; ++i)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) O[i][r] = 0.f;
-  const bf16x2_t ones = __builtin_bit_cast(bf16x2_t, 0x3F803F80u);
-
+  WalkAcc A;
   auto work = [&](const uint8_t *ks, const uint8_t *vs, int j) __attribute__((always_inline)) {
     const bool pre = j < np;
     const int kt = (pre ? j : j - np) * TK;
@@ -290,81 +151,8 @@ __device__ __forceinline__ void walk_bf16(const WalkArgs &a, const WalkItem &it,
       __builtin_amdgcn_sched_group_barrier(0x100, NSB, 0);
       __builtin_amdgcn_sched_group_barrier(0x008, NSB, 0);
     }
-    // Accumulator entry r of sub-block sb is key kt + 32 (sb0 + sb) + 8 (r / 4) + 4 h + r % 4.
-    if (TREE && !pre) {
-      if (kt + TK > L) {
-#pragma unroll
-        for (int sb = 0; sb < NSB; ++sb)
-#pragma unroll
-          for (int r2 = 0; r2 < 16; ++r2) {
-            const int t = kt + 32 * (sb0 + sb) + 8 * (r2 >> 2) + 4 * h + (r2 & 3);
-            const uint32_t rel = (uint32_t)(t - L) & 127u;
-            const bool anc = ((rel < 64 ? alo : ahi) >> (rel & 63)) & 1u;
-            Sc[sb][r2] = (t < kend) & ((t < L) | anc) ? Sc[sb][r2] : -INFINITY;
-          }
-      }
-    } else if (kt + TK - 1 > (pre ? P - 1 : lim_lo)) {
-      const int vis = (pre ? P - 1 : lim) - kt - 32 * sb0 - 4 * h;
-#pragma unroll
-      for (int sb = 0; sb < NSB; ++sb)
-#pragma unroll
-        for (int r2 = 0; r2 < 16; ++r2)
-          Sc[sb][r2] = 32 * sb + 8 * (r2 >> 2) + (r2 & 3) <= vis ? Sc[sb][r2] : -INFINITY;
-    }
-    float tm;
-    if constexpr (NSB == 2) {
-      tm = tile_max32(Sc);
-    } else {
-      const f32x16 &x = Sc[0];
-      const float u0 = fmaxf(fmaxf(x[0], x[1]), x[2]), u1 = fmaxf(fmaxf(x[3], x[4]), x[5]);
-      const float u2 = fmaxf(fmaxf(x[6], x[7]), x[8]), u3 = fmaxf(fmaxf(x[9], x[10]), x[11]);
-      const float u4 = fmaxf(fmaxf(x[12], x[13]), x[14]);
-      tm = fmaxf(fmaxf(fmaxf(u0, u1), fmaxf(u2, u3)), fmaxf(u4, x[15]));
-    }
-    const float tmax = max_with_other_half(tm) * a.scale_log2;
-    // Lazy rescaling: m moves only when a score exceeds it by more than kRescaleSlack.
-    const bool need = tmax > m + kRescaleSlack;
-    if (__builtin_amdgcn_ballot_w64(need)) {
-      const float m_new = need ? tmax : m;
-      const float alpha = need ? (m == -INFINITY ? 0.f : fast_exp2(m - m_new)) : 1.f;
-      m = m_new;
-      lsum *= alpha;
-#pragma unroll
-      for (int i = 0; i < D / 32; ++i)
-#pragma unroll
-        for (int r2 = 0; r2 < 16; ++r2) O[i][r2] *= alpha;
-    }
-    const float m_use = m == -INFINITY ? 0.f : m;
-    // Weights are rounded to bf16, the matrix product's operand type (2^-8 of a
-    // weight, as the inputs' own type); their sum is taken of the rounded ones.
-    uint32_t pk[2 * NSB][4];
-#pragma unroll
-    for (int sb = 0; sb < NSB; ++sb)
-#pragma unroll
-      for (int half = 0; half < 2; ++half)
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const float p0 = fast_exp2(fmaf(Sc[sb][8 * half + 2 * q], a.scale_log2, -m_use));
-          const float p1 = fast_exp2(fmaf(Sc[sb][8 * half + 2 * q + 1], a.scale_log2, -m_use));
-          pk[2 * sb + half][q] = pack_bf16x2(p0, p1);
-        }
-#pragma unroll
-    for (int mh = 0; mh < 2 * NSB; ++mh)
-#pragma unroll
-      for (int q = 0; q < 4; ++q)
-        lsum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, pk[mh][q]), ones, lsum, false);
-#pragma unroll
-    for (int mh = 0; mh < 2 * NSB; ++mh) {
-      const bf16x8 pf = __builtin_bit_cast(bf16x8, uint4{pk[mh][0], pk[mh][1], pk[mh][2], pk[mh][3]});
-#pragma unroll
-      for (int i = 0; i < D / 32; ++i) {
-        const uint8_t *p = vs + 16 * (2 * sb0 + mh) * (D * 2) + vro[i];
-        const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t *)p);
-        const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t *)(p + 8 * (D * 2)));
-        const bf16x8 vf = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-        O[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf, O[i], 0, 0, 0);
-      }
-    }
+    walk_mask<NSB, TREE>(Sc, M, pre, kt, pre ? P : kend, 32 * sb0);
+    walk_softmax_pv<NSB>(Sc, A, vs + 32 * sb0 * (D * 2), vro, a.scale_log2);
   };
 
   // Iteration j waits for tile j's loads; after its barrier every wave is done
@@ -384,56 +172,8 @@ __device__ __forceinline__ void walk_bf16(const WalkArgs &a, const WalkItem &it,
     if (j + 1 < j1) tile(j + 1, std::integral_constant<int, 1>{});
   }
 
-  float ltot = sum_with_other_half(lsum);
-  if constexpr (KSPLIT == 2) {
-    // Every wave is past its last read of the rings and no load is in flight:
-    // the K ring takes the second group's O, the V ring its m and l.
-    ring_barrier();
-    float *const mo = reinterpret_cast<float *>(kring[0]);
-    float *const ml = reinterpret_cast<float *>(vring[0]);
-    if (ksb == 1) {
-#pragma unroll
-      for (int i = 0; i < D / 32; ++i)
-#pragma unroll
-        for (int r2 = 0; r2 < 16; ++r2) mo[(rwave * 64 + 16 * i + r2) * 64 + lane] = O[i][r2];
-      ml[(rwave * 2) * 64 + lane] = m;
-      ml[(rwave * 2 + 1) * 64 + lane] = ltot;
-    }
-    ring_barrier();
-    if (ksb == 1) return;
-    const float m1 = ml[(rwave * 2) * 64 + lane], l1 = ml[(rwave * 2 + 1) * 64 + lane];
-    const float mn = fmaxf(m, m1);
-    const float w0 = m == -INFINITY ? 0.f : fast_exp2(m - mn);
-    const float w1 = m1 == -INFINITY ? 0.f : fast_exp2(m1 - mn);
-#pragma unroll
-    for (int i = 0; i < D / 32; ++i)
-#pragma unroll
-      for (int r2 = 0; r2 < 16; ++r2) O[i][r2] = O[i][r2] * w0 + mo[(rwave * 64 + 16 * i + r2) * 64 + lane] * w1;
-    ltot = ltot * w0 + l1 * w1;
-    m = mn;
-  }
-  if (!wave_rows) return;
-  if (walk_direct(S, it.rb, g)) {
-    if (!row_ok) return;
-    // O^T entry r of d-block i is d = 32 i + 8 (r / 4) + 4 h + r % 4 of this lane's row.
-    // The halves of a row trade four columns, so that a lane stores 16 bytes and a row
-    // 32 in one piece (13B-shaped prompts of 100 to 700: 32.9 us with 8-byte stores,
-    // 31.0; through LDS, for whole rows, 32.5).
-    const float inv = 1.f / ltot;
-    uint16_t *op = static_cast<uint16_t *>(a.out) + ((int64_t)(S.row0 + node) * a.n_q + hq) * D;
-#pragma unroll
-    for (int i = 0; i < D / 32; ++i)
-#pragma unroll
-      for (int p = 0; p < 2; ++p) {
-        const auto &o = O[i];
-        const uint32_t a0 = pack_bf16x2(o[8 * p] * inv, o[8 * p + 1] * inv), a1 = pack_bf16x2(o[8 * p + 2] * inv, o[8 * p + 3] * inv);
-        const uint32_t b0 = pack_bf16x2(o[8 * p + 4] * inv, o[8 * p + 5] * inv), b1 = pack_bf16x2(o[8 * p + 6] * inv, o[8 * p + 7] * inv);
-        const auto s0 = __builtin_amdgcn_permlane32_swap(a0, b0, false, false), s1 = __builtin_amdgcn_permlane32_swap(a1, b1, false, false);
-        *reinterpret_cast<uint4 *>(op + 32 * i + 16 * p + 8 * h) = uint4{s0[0], s1[0], s0[1], s1[1]};
-      }
-  } else {
-    write_part<D / 32>(a.part + (int64_t)(walk_part(a, S, it.kvh, it.rb, it.ch) + rwave) * walk_unit_floats(D / 32), O, m, ltot, row_ok);
-  }
+  walk_finish<KSPLIT>(a, it, A, row_ok, wave_rows, node, hq, rwave, ksb, reinterpret_cast<float *>(kring[0]),
+                      reinterpret_cast<float *>(vring[0]));
 }
 
 template <bool TREE>
@@ -587,42 +327,7 @@ __global__ __launch_bounds__(64 * kF32Waves, 2) void walk_attn_f32(WalkArgs a) {
         for (int i = 0; i < DB; ++i) O[i] = __builtin_amdgcn_mfma_f32_32x32x2f32(vf[r][i], Sc[r0 + r], O[i], 0, 0, 0);
     }
   }
-  write_part<DB>(merge[wave], O, m, sum_with_other_half(l), true);
-  __syncthreads();
-  // Wave w merges entries 4 DB / W w ... of all waves' parts.
-  float mw[W], M = -INFINITY, lt = 0.f;
-#pragma unroll
-  for (int w = 0; w < W; ++w) {
-    mw[w] = merge[w][DB * 1024 + (lane & 31)];
-    M = fmaxf(M, mw[w]);
-  }
-#pragma unroll
-  for (int w = 0; w < W; ++w) {
-    mw[w] = mw[w] == -INFINITY ? 0.f : fast_exp2(mw[w] - M);
-    lt = fmaf(merge[w][DB * 1024 + 32 + (lane & 31)], mw[w], lt);
-  }
-  const bool direct = walk_direct(S, it.rb, g);
-  float *const u = direct ? nullptr : a.part + (int64_t)walk_part(a, S, it.kvh, it.rb, it.ch) * UF;
-  const float inv = direct ? 1.f / lt : 1.f;
-  for (int iq = wave; iq < 4 * DB; iq += W) {        // d-block iq / 4, entries 4 (iq % 4) .. + 3
-    f32x4 o = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int w = 0; w < W; ++w) {
-      const f32x4 v = *reinterpret_cast<const f32x4 *>(&merge[w][(iq * 64 + lane) * 4]);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) o[e] = fmaf(v[e], mw[w], o[e]);
-    }
-    const int col = 32 * (iq >> 2) + 8 * (iq & 3) + 4 * h;
-    if (!row_ok) continue;
-    if (!direct) *reinterpret_cast<f32x4 *>(u + (iq * 64 + lane) * 4) = o;
-    else if (col < d)
-      *reinterpret_cast<f32x4 *>(static_cast<float *>(a.out) + ((int64_t)(S.row0 + node) * a.n_q + hq) * d + col) =
-          f32x4{o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
-  }
-  if (!direct && wave == 0 && lane < 32) {
-    u[DB * 1024 + lane] = M;
-    u[DB * 1024 + 32 + lane] = lt;
-  }
+  walk_finish_f32<DB, W>(a, it, O, m, l, row_ok, node, hq, merge);
 }
 
 // Merge the parts of 32 query rows of a set: its own chunks, then those of the
@@ -715,7 +420,6 @@ __global__ __launch_bounds__(256) void walk_combine(WalkArgs a) {
 template <int DB, bool TREE>
 void launch_f32(const WalkArgs &a, hipStream_t st) {
   hipLaunchKernelGGL((walk_attn_f32<DB, TREE>), dim3(a.blocks), dim3(64 * kF32Waves), 0, st, a);
-  if (a.cblocks) hipLaunchKernelGGL((walk_combine<DB, false>), dim3(a.cblocks), dim3(256), 0, st, a);
 }
 
 template <bool TREE>
@@ -731,15 +435,30 @@ void launch_f32(const WalkArgs &a, hipStream_t st) {
 template <bool TREE>
 void launch_bf16(const WalkArgs &a, hipStream_t st) {
   hipLaunchKernelGGL((walk_attn_bf16<TREE>), dim3(a.blocks), dim3(64 * kBf16Waves), 0, st, a);
-  if (a.cblocks) hipLaunchKernelGGL((walk_combine<D / 32, true>), dim3(a.cblocks), dim3(256), 0, st, a);
 }
 
 }  // namespace
 
+hipError_t launch_walk_combine(int dt, const WalkArgs &a, hipStream_t st) {
+  const dim3 grid(a.cblocks), block(256);
+  if (dt != 0) {
+    hipLaunchKernelGGL((walk_combine<D / 32, true>), grid, block, 0, st, a);
+  } else {
+    switch ((a.head_dim + 31) / 32) {
+      case 1: hipLaunchKernelGGL((walk_combine<1, false>), grid, block, 0, st, a); break;
+      case 2: hipLaunchKernelGGL((walk_combine<2, false>), grid, block, 0, st, a); break;
+      case 3: hipLaunchKernelGGL((walk_combine<3, false>), grid, block, 0, st, a); break;
+      default: hipLaunchKernelGGL((walk_combine<4, false>), grid, block, 0, st, a);
+    }
+  }
+  return hipGetLastError();
+}
+
 hipError_t launch_walk_attn(int dt, bool tree, const WalkArgs &a, hipStream_t st) {
   if (dt == 0) tree ? launch_f32<true>(a, st) : launch_f32<false>(a, st);
   else tree ? launch_bf16<true>(a, st) : launch_bf16<false>(a, st);
-  return hipGetLastError();
+  const hipError_t e = hipGetLastError();
+  return e != hipSuccess || !a.cblocks ? e : launch_walk_combine(dt, a, st);
 }
 
 }  // namespace specmemo

@@ -23,6 +23,7 @@ FP32, BF16 = 0, 1
 GREEDY, TYPICAL = 0, 1
 HEADS_ROWMAJOR, HEADS_PACKED, HEADS_INPUT_PER_HEAD = 0, 1, 2
 WS_TOPK, WS_ATTN, WS_ACCEPT, WS_PAD, WS_SAMPLE = 0, 1, 2, 3, 4
+ROT_HALVES, ROT_PAIRS = 0, 1
 
 STATUS = {0: "OK", -1: "E_ARG", -2: "E_DTYPE", -3: "E_TREE", -4: "E_BUDGET", -5: "E_WORKSPACE", -6: "E_HIP"}
 
@@ -48,6 +49,19 @@ class _KV(C.Structure):
 
 class _Prefix(C.Structure):
     _fields_ = [("base_h", C.c_void_p), ("len_h", C.c_void_p)]
+
+
+class _Rows(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("k", C.c_void_p), ("v", C.c_void_p), ("q_stride", C.c_int64), ("k_stride", C.c_int64),
+                ("v_stride", C.c_int64), ("q_norm", C.c_void_p), ("k_norm", C.c_void_p), ("eps", C.c_float),
+                ("cos", C.c_void_p), ("sin", C.c_void_p), ("pos", C.c_void_p), ("n_pos", C.c_int32),
+                ("rot_dim", C.c_int32), ("rot_style", C.c_int32)]
+
+
+class _KV4(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("k_scale", C.c_void_p), ("v_scale", C.c_void_p),
+                ("cap_total", C.c_int64), ("n_kv", C.c_int32), ("head_dim", C.c_int32), ("seq_len", C.c_void_p),
+                ("seq_base_h", C.c_void_p), ("seq_cap_h", C.c_void_p), ("seq_len_h", C.c_void_p)]
 
 
 class _Rules(C.Structure):
@@ -122,6 +136,22 @@ def load():
         lib.specmemo_tree_attn_prefix.restype = C.c_int
         lib.specmemo_tree_attn_prefix_bytes.argtypes = [i32, PT, PK, PP, i32]
         lib.specmemo_tree_attn_prefix_bytes.restype = sz
+        PR, P4 = C.POINTER(_Rows), C.POINTER(_KV4)
+        lib.specmemo_kv_append.argtypes = [i32, i32, vp, PR, i32, PK, vp, vp]
+        lib.specmemo_kv4_append.argtypes = [i32, i32, vp, PR, i32, P4, vp, vp]
+        lib.specmemo_kv4_read.argtypes = [i32, i32, vp, P4, vp, vp, vp]
+        lib.specmemo_kv4_prompt_attn.argtypes = [i32, i32, vp, P4, PP, i32, f32, vp, vp, vp, sz, vp]
+        lib.specmemo_kv4_prompt_attn_bytes.argtypes = [i32, i32, vp, P4, PP, i32]
+        lib.specmemo_kv4_tree_attn.argtypes = [i32, PT, P4, PP, i32, f32, vp, vp, vp, sz, vp]
+        lib.specmemo_kv4_tree_attn_bytes.argtypes = [i32, PT, P4, PP, i32]
+        lib.specmemo_kv4_compact.argtypes = [PT, P4, vp, vp, i32, vp]
+        for f in ("specmemo_kv_append", "specmemo_kv4_append", "specmemo_kv4_read", "specmemo_kv4_prompt_attn",
+                  "specmemo_kv4_tree_attn", "specmemo_kv4_compact"):
+            getattr(lib, f).restype = C.c_int
+        for f in ("specmemo_kv4_prompt_attn_bytes", "specmemo_kv4_tree_attn_bytes"):
+            getattr(lib, f).restype = sz
+        lib.specmemo_mem_kv4_bytes.argtypes = [i32, i32, i32, i32, i64]
+        lib.specmemo_mem_kv4_bytes.restype = i64
         lib.specmemo_logit_rules.argtypes = [i32, PT, i32, C.POINTER(_Rules), vp, vp, vp, vp]
         lib.specmemo_token_counts.argtypes = [i32, i32, vp, vp, vp, vp, i32, vp]
         lib.specmemo_count_accepted.argtypes = [PT, i32, vp, vp, vp, i32, vp, vp]
@@ -465,6 +495,146 @@ def tree_attn_prefix(dt: int, trees: Trees, kv: KVPool, prefix: Prefix, n_q: int
                                             _ptr(q), _ptr(out), _ptr(ws), ws_bytes, _stream(stream)))
 
 
+# ---- new rows of the pool, and the pool in 4 bits -------------------------------------
+
+class KV4Pool:
+    """One layer's pool in 4 bits: codes [n_kv][rows][head_dim / 2] and scale bytes [n_kv][rows][head_dim / 32] of K and V
+    (uint8 tensors), device seq_len, host mirrors."""
+
+    def __init__(self, k, v, k_scale, v_scale, seq_len_dev, seq_base, seq_cap, seq_len):
+        self.n_kv, self.cap_total, half = (int(s) for s in k.shape)
+        self.head_dim = 2 * half
+        for name, x, w in (("k", k, half), ("v", v, half), ("k_scale", k_scale, half // 16), ("v_scale", v_scale, half // 16)):
+            _check_tensor(name, x, ("torch.uint8",))
+            if tuple(x.shape) != (self.n_kv, self.cap_total, w):
+                raise ValueError(f"{name}: shape {tuple(x.shape)}, expected {(self.n_kv, self.cap_total, w)}")
+        self.k, self.v, self.k_scale, self.v_scale, self.seq_len = k, v, k_scale, v_scale, seq_len_dev
+        self.seq_base_h = np.ascontiguousarray(seq_base, dtype=np.int64)
+        self.seq_cap_h = _i32(seq_cap)
+        self.seq_len_h = _i32(seq_len)
+
+    def struct(self) -> _KV4:
+        return _KV4(_ptr(self.k), _ptr(self.v), _ptr(self.k_scale), _ptr(self.v_scale), self.cap_total, self.n_kv,
+                    self.head_dim, _ptr(self.seq_len), _host_addr(self.seq_base_h), _host_addr(self.seq_cap_h),
+                    _host_addr(self.seq_len_h))
+
+
+_VALUES = ("torch.float32", "torch.bfloat16")
+
+
+class QKVRows:
+    """New tokens' q, k and v [tokens][heads][head_dim], the norm and the rotation (include/specmemo.h, specmemo_rows).
+
+    The three may be slices of one buffer: a token's heads lie together, tokens at one stride.  q: None for keys and
+    values alone.  cos, sin: fp32 [positions][rot_dim / 2]; pos: int32 [tokens]; rot_dim None: cos's columns twice, 0: no
+    rotation."""
+
+    def __init__(self, q, k, v, pos=None, cos=None, sin=None, rot_dim: Optional[int] = None, rot_style: int = ROT_HALVES,
+                 q_norm=None, k_norm=None, eps: float = 1e-5):
+        d = int(k.shape[2])
+        for name, x in (("q", q), ("k", k), ("v", v)):
+            if x is None:
+                if name == "q":
+                    continue
+                raise ValueError(f"{name} is missing")
+            if x.dim() != 3 or int(x.shape[0]) != int(k.shape[0]) or int(x.shape[2]) != d or x.dtype != k.dtype or str(x.dtype) not in _VALUES:
+                raise ValueError(f"{name}: {tuple(x.shape)} of {x.dtype} beside keys {tuple(k.shape)} of {k.dtype}")
+            if x.stride(2) != 1 or (x.shape[1] > 1 and x.stride(1) != d):
+                raise ValueError(f"{name}: a token's heads must lie together, got strides {x.stride()}")
+        if v.shape != k.shape:
+            raise ValueError(f"values {tuple(v.shape)} beside keys {tuple(k.shape)}")
+        for name, w in (("q_norm", q_norm), ("k_norm", k_norm)):
+            _check_tensor(name, w, (str(k.dtype),))
+            if w is not None and w.numel() != d:
+                raise ValueError(f"{name}: {w.numel()} weights for heads of {d}")
+        if rot_dim is None:
+            rot_dim = 0 if cos is None else 2 * int(cos.shape[1])
+        n_pos = 0
+        if rot_dim:
+            if cos is None or sin is None or pos is None:
+                raise ValueError("a rotation needs cos, sin and pos")
+            _check_tensor("cos", cos, _FLOAT32)
+            _check_tensor("sin", sin, _FLOAT32)
+            _check_tensor("pos", pos, _INT32)
+            n_pos = int(cos.shape[0])
+            if tuple(cos.shape) != (n_pos, rot_dim // 2) or cos.shape != sin.shape:
+                raise ValueError(f"cos {tuple(cos.shape)}, sin {tuple(sin.shape)} for {rot_dim} rotated columns")
+            if int(pos.numel()) != int(k.shape[0]):
+                raise ValueError(f"{pos.numel()} positions for {k.shape[0]} tokens")
+        self.q, self.k, self.v, self.pos, self.cos, self.sin = q, k, v, pos, cos, sin
+        self.q_norm, self.k_norm, self.eps = q_norm, k_norm, eps
+        self.tokens, self.n_q, self.n_kv, self.head_dim = int(k.shape[0]), 0 if q is None else int(q.shape[1]), int(k.shape[1]), d
+        self.rot_dim, self.rot_style, self.n_pos = rot_dim, rot_style, n_pos
+
+    def _stride(self, x) -> int:
+        return 0 if x is None else int(x.stride(0)) if self.tokens > 1 else int(x.shape[1]) * self.head_dim
+
+    def struct(self) -> _Rows:
+        return _Rows(_ptr(self.q), _ptr(self.k), _ptr(self.v), self._stride(self.q), self._stride(self.k), self._stride(self.v),
+                     _ptr(self.q_norm), _ptr(self.k_norm), self.eps, _ptr(self.cos), _ptr(self.sin), _ptr(self.pos), self.n_pos,
+                     self.rot_dim, self.rot_style)
+
+
+def _append(fn, dt: int, new_off, rows: QKVRows, kv, q_out, stream):
+    off, ks, rs = _new_off(new_off, kv), kv.struct(), rows.struct()
+    if int(off[-1]) != rows.tokens or rows.n_kv != kv.n_kv or rows.head_dim != kv.head_dim:
+        raise ValueError(f"{rows.tokens} tokens of {rows.n_kv} KV heads of {rows.head_dim} for {int(off[-1])} tokens and a pool "
+                         f"of {kv.n_kv} heads of {kv.head_dim}")
+    if str(rows.k.dtype) != _VALUES[dt]:
+        raise ValueError(f"rows of {rows.k.dtype} for type {dt}")
+    _check_tensor("q_out", q_out, (_VALUES[dt],))
+    if hasattr(q_out, "numel") and q_out.numel() != rows.tokens * rows.n_q * rows.head_dim:
+        raise ValueError(f"q_out of {q_out.numel()} values for {rows.tokens} tokens of {rows.n_q} heads")
+    _check(fn(dt, len(off) - 1, _host_addr(off), C.byref(rs), rows.n_q, C.byref(ks), _ptr(q_out), _stream(stream)))
+
+
+def kv_append(dt: int, new_off, rows: QKVRows, kv: KVPool, q_out, stream=None):
+    _append(load().specmemo_kv_append, dt, new_off, rows, kv, q_out, stream)
+
+
+def kv4_append(dt: int, new_off, rows: QKVRows, kv: KV4Pool, q_out, stream=None):
+    _append(load().specmemo_kv4_append, dt, new_off, rows, kv, q_out, stream)
+
+
+def kv4_read(dt: int, new_off, kv: KV4Pool, k_out, v_out, stream=None):
+    off, ks = _new_off(new_off, kv), kv.struct()
+    for name, x in (("k_out", k_out), ("v_out", v_out)):
+        _check_tensor(name, x, (_VALUES[dt],))
+        if hasattr(x, "numel") and x.numel() != int(off[-1]) * kv.n_kv * kv.head_dim:
+            raise ValueError(f"{name} of {x.numel()} values for {int(off[-1])} tokens")
+    _check(load().specmemo_kv4_read(dt, len(off) - 1, _host_addr(off), C.byref(ks), _ptr(k_out), _ptr(v_out), _stream(stream)))
+
+
+def kv4_prompt_attn_bytes(dt: int, new_off, kv: KV4Pool, n_q: int, prefix: Optional[Prefix] = None) -> int:
+    off, ks = _new_off(new_off, kv), kv.struct()
+    return int(load().specmemo_kv4_prompt_attn_bytes(dt, len(off) - 1, _host_addr(off), C.byref(ks),
+                                                     _prefix_ref(prefix, len(off) - 1), n_q))
+
+
+def kv4_prompt_attn(dt: int, new_off, kv: KV4Pool, n_q: int, q, out, prefix: Optional[Prefix] = None, scale: float = 0.0,
+                    ws=None, ws_bytes: int = 0, stream=None):
+    off, ks = _new_off(new_off, kv), kv.struct()
+    _check(load().specmemo_kv4_prompt_attn(dt, len(off) - 1, _host_addr(off), C.byref(ks), _prefix_ref(prefix, len(off) - 1),
+                                           n_q, scale, _ptr(q), _ptr(out), _ptr(ws), ws_bytes, _stream(stream)))
+
+
+def kv4_tree_attn_bytes(dt: int, trees: Trees, kv: KV4Pool, n_q: int, prefix: Optional[Prefix] = None) -> int:
+    ts, ks = trees.struct(), kv.struct()
+    return int(load().specmemo_kv4_tree_attn_bytes(dt, C.byref(ts), C.byref(ks), _prefix_ref(prefix, trees.B), n_q))
+
+
+def kv4_tree_attn(dt: int, trees: Trees, kv: KV4Pool, n_q: int, q, out, prefix: Optional[Prefix] = None, scale: float = 0.0,
+                  ws=None, ws_bytes: int = 0, stream=None):
+    ts, ks = trees.struct(), kv.struct()
+    _check(load().specmemo_kv4_tree_attn(dt, C.byref(ts), C.byref(ks), _prefix_ref(prefix, trees.B), n_q, scale, _ptr(q),
+                                         _ptr(out), _ptr(ws), ws_bytes, _stream(stream)))
+
+
+def kv4_compact(trees: Trees, kv: KV4Pool, accept_len, path, path_stride: int, stream=None):
+    ts, ks = trees.struct(), kv.struct()
+    _check(load().specmemo_kv4_compact(C.byref(ts), C.byref(ks), _ptr(accept_len), _ptr(path), path_stride, _stream(stream)))
+
+
 # ---- rules on logits ----------------------------------------------------------------
 
 _INT32, _FLOAT32 = ("torch.int32",), ("torch.float32",)
@@ -538,6 +708,10 @@ def _bytes(v: int) -> int:
 
 def mem_kv_bytes(layers: int, batch: int, n_kv: int, head_dim: int, tokens: int, elem_bytes: int) -> int:
     return _bytes(load().specmemo_mem_kv_bytes(layers, batch, n_kv, head_dim, tokens, elem_bytes))
+
+
+def mem_kv4_bytes(layers: int, batch: int, n_kv: int, head_dim: int, tokens: int) -> int:
+    return _bytes(load().specmemo_mem_kv4_bytes(layers, batch, n_kv, head_dim, tokens))
 
 
 def mem_buffer_bytes(batch: int, nodes: int, seqs: int, levels: int, vocab: int, elem_bytes: int) -> int:
