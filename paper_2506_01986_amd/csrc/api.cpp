@@ -832,7 +832,7 @@ int check_prompt(int dt, int B, const int32_t *off, const specmemo_kv *kv, const
 }
 
 WalkPlan make_walk(int dt, bool causal, const TreeInfo &ti, const int32_t *off_h, const specmemo_kv *kv,
-                   const specmemo_prefix *px, int n_q) {
+                   const specmemo_prefix *px, int n_q, bool four = false) {
   std::vector<WalkSeq> seqs;
   for (int b = 0; b < ti.B; ++b) {
     WalkSeq s{};
@@ -848,7 +848,7 @@ WalkPlan make_walk(int dt, bool causal, const TreeInfo &ti, const int32_t *off_h
     seqs.push_back(s);
   }
   WalkPlan p;
-  plan_walk(dt, causal, seqs, kv->n_kv, n_q / kv->n_kv, kv->head_dim, device_cus(), &p);
+  plan_walk(dt, causal, seqs, kv->n_kv, n_q / kv->n_kv, kv->head_dim, device_cus(), &p, four);
   return p;
 }
 
@@ -869,7 +869,7 @@ int run_walk(int dt, bool tree, const TreeInfo &ti, const int32_t *off_h, const 
   if (!al(q, 16) || !al(out, 16)) return fail(SPECMEMO_E_ARG, "q / out must be non-NULL and 16-byte aligned");
   const size_t bytes = (size_t)ti.total * n_q * kv->head_dim * (dt == SPECMEMO_BF16 ? 2 : 4);
   if ((uintptr_t)q < (uintptr_t)out + bytes && (uintptr_t)out < (uintptr_t)q + bytes) return fail(SPECMEMO_E_ARG, "out overlaps q");
-  const WalkPlan p = make_walk(dt, !tree, ti, off_h, kv, px, n_q);
+  const WalkPlan p = make_walk(dt, !tree, ti, off_h, kv, px, n_q, kv4 != nullptr);
   constexpr int64_t most = UINT32_MAX / 256;   // blocks of 256 threads: a launch has at most 2^32 - 1 threads
   if (p.blocks > most || p.cblocks > most || p.parts > INT32_MAX)
     return fail(SPECMEMO_E_ARG, "too many work items: %lld", (long long)std::max(p.blocks, p.cblocks));
@@ -1480,7 +1480,7 @@ size_t specmemo_kv4_prompt_attn_bytes(specmemo_dtype dt, int32_t B, const int32_
     if (check_kv4(kv)) return (size_t)0;
     const specmemo_kv view = as_kv(*kv);
     if (check_prompt(dt, B, new_off_h, &view, prefix, n_q, &ti)) return (size_t)0;
-    return walk_ws_bytes(make_walk(dt, true, ti, new_off_h, &view, prefix, n_q), kv->head_dim);
+    return walk_ws_bytes(make_walk(dt, true, ti, new_off_h, &view, prefix, n_q, true), kv->head_dim);
   });
 }
 
@@ -1504,7 +1504,7 @@ size_t specmemo_kv4_tree_attn_bytes(specmemo_dtype dt, const specmemo_trees *t, 
     if (check_kv4(kv)) return (size_t)0;
     const specmemo_kv view = as_kv(*kv);
     if (check_tree_walk(dt, t, &view, prefix, n_q, &ti)) return (size_t)0;
-    return walk_ws_bytes(make_walk(dt, false, ti, t->node_off_h, &view, prefix, n_q), kv->head_dim);
+    return walk_ws_bytes(make_walk(dt, false, ti, t->node_off_h, &view, prefix, n_q, true), kv->head_dim);
   });
 }
 

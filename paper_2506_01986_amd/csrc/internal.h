@@ -249,7 +249,7 @@ struct WalkPlan {
   std::vector<WalkSetPacked> sets;
 };
 void plan_walk(int dt, bool causal, const std::vector<WalkSeq> &seqs, int n_kv, int group, int head_dim, int cus,
-               WalkPlan *p);
+               WalkPlan *p, bool four = false);   // four: a 4-bit pool
 
 // ---- new rows of the pool (kv_rows.hip) ------------------------------------------------
 // Token i of the sequence with the last off <= i lies at pool row row0 + i.

@@ -44,18 +44,24 @@ typedef int i32x8_t __attribute__((ext_vector_type(8)));
 typedef uint32_t u32x6_t __attribute__((ext_vector_type(6)));
 typedef __bf16 bf16x32_t __attribute__((ext_vector_type(32)));
 
-// A wave's queries as the scaled product's operands: step s takes columns 64 s + 32 h
-// .. + 31 of a lane's row, scale byte i of sc[s] is part i's.
+// A wave's queries as the scaled product's operands, in STEPS products over the
+// columns: step s takes group (4 / STEPS) s + h of a lane's row, scale byte i of sc[s]
+// is part i's.
+template <int STEPS>
 struct Query6 {
-  u32x6_t part[2][3];
-  uint32_t sc[2];
+  u32x6_t part[STEPS][3];
+  uint32_t sc[STEPS];
 
+  __device__ __forceinline__ i32x8_t operand(int s, int p) const {
+    const u32x6_t &w = part[s][p];
+    return i32x8_t{(int)w[0], (int)w[1], (int)w[2], (int)w[3], (int)w[4], (int)w[5], 0, 0};
+  }
   __device__ __forceinline__ void load(bool ok, const uint16_t *row, int h) {
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
+    for (int s = 0; s < STEPS; ++s) {
       uint4 w[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) w[i] = ld16_or_zero(ok, row + 64 * s + 32 * h + 8 * i);
+      for (int i = 0; i < 4; ++i) w[i] = ld16_or_zero(ok, row + (D / STEPS) * s + kKv4Group * h + 8 * i);
       bf16x32_t x;
       __builtin_memcpy(&x, w, sizeof(x));
       float top = 0.f;
@@ -80,10 +86,9 @@ struct Query6 {
 };
 
 template <int STEP, int PART>
-__device__ __forceinline__ f32x16 qk_part(uint4 k, const Query6 &q, f32x16 c, uint32_t kscale) {
+__device__ __forceinline__ f32x16 qk_part(uint4 k, const Query6<2> &q, f32x16 c, uint32_t kscale) {
   const i32x8_t a = {(int)k.x, (int)k.y, (int)k.z, (int)k.w, 0, 0, 0, 0};
-  const u32x6_t &w = q.part[STEP][PART];
-  const i32x8_t b = {(int)w[0], (int)w[1], (int)w[2], (int)w[3], (int)w[4], (int)w[5], 0, 0};
+  const i32x8_t b = q.operand(STEP, PART);
   // formats: 4 = four bits, 2 = six bits; the scale byte of each operand is chosen by number
   return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, c, 4, 2, 2 * STEP, (int)kscale, PART, (int)q.sc[STEP]);
 }
@@ -177,7 +182,7 @@ __device__ __forceinline__ void walk4(const WalkArgs &a, const WalkItem &it, uin
   const bool row_ok = my_row < rows;
   const int node = row_ok ? my_row / g : S.T - 1;
   const int hq = it.kvh * g + (row_ok ? my_row % g : 0);
-  Query6 Q;
+  Query6<2> Q;
   Q.load(row_ok, static_cast<const uint16_t *>(a.q) + ((int64_t)(S.row0 + node) * a.n_q + hq) * D, h);
   if (tree && tid < S.T) par[tid] = pn;
   WalkMask M{L, P, h, node};
@@ -251,13 +256,233 @@ __device__ __forceinline__ void walk4(const WalkArgs &a, const WalkItem &it, uin
                       reinterpret_cast<float *>(kring[0]));
 }
 
+// Rows of few queries (up to 16: a token's query heads, or a small tree's nodes) are
+// bound by memory: the waves of a block share nothing but the merge at the end, and
+// each takes every fourth tile of the item with the next one's loads in flight
+// (8.7 KB a wave, 70 KB a compute unit).  Queries fill the 16-wide products: a tile's
+// scores are 16 to a lane, half of those of the 32-wide ones.
+//   S^T: 16 keys x 128 columns a product.  A lane's operand is the codes of one group
+//        of its key, 16 bytes as they lie in memory, and that group's scale.
+//   O^T: V is converted as it arrives, through the wave's own 16 KB of LDS.  A product
+//        contracts 32 keys, the four of each lane group from two blocks of 16, which is
+//        where the scores left the weights.
+constexpr int kFewRows = 16;
+
+// Chunk of 16 bytes c of V row r: eight lanes that write (two rows, four groups) and 32
+// that read (eight rows, one pair of chunks) meet different banks.
+__device__ __forceinline__ int few_swz(int r, int c) { return c ^ ((r & 3) << 2) ^ (((r ^ (r >> 2)) & 1) << 1); }
+
+// The maximum or sum over the four lanes l % 16 + 16 G.
+__device__ __forceinline__ float max_of_groups(float x) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return max_with_other_half(fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])));
+}
+__device__ __forceinline__ float sum_of_groups(float x) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return sum_with_other_half(__uint_as_float(r[0]) + __uint_as_float(r[1]));
+}
+
+template <bool TREE>
+__device__ __forceinline__ void walk4_few(const WalkArgs &a, const WalkItem &it, uint8_t (*lds)[kVTile4], int *par) {
+  const WalkSet &S = it.S;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int q16 = lane & 15, G = lane >> 4, g = a.group, L = S.L, P = S.P;
+  const int rows = S.T * g;
+  const int np = (P + TK - 1) / TK;
+  const int kend = walk_keys(S, 0, g);
+  const int j0 = it.ch * S.ct, j1 = min(np + (kend + TK - 1) / TK, j0 + S.ct);
+  const int64_t head = (int64_t)it.kvh * a.cap_total;
+  const int64_t prow = head + S.pbase, srow = head + S.base;
+  const uint8_t *const K0 = static_cast<const uint8_t *>(a.k), *const V0 = static_cast<const uint8_t *>(a.v);
+  uint8_t *const mem = lds[wave];
+
+  // A tile as it is loaded: K codes of the four blocks of 16 keys (key q16, group G), V codes of
+  // rows 16 n + lane / 4 (group lane % 4), and their scales.
+  struct Raw {
+    uint4 k[4], v[4];
+    uint32_t ks[4], vs[4];
+  };
+  auto load = [&](Raw &w, int j) __attribute__((always_inline)) {
+    const bool pre = j < np;
+    const int kt = (pre ? j : j - np) * TK, end = pre ? P : kend;
+    const int64_t row0 = pre ? prow : srow;
+    const uint8_t *const kb = K0 + row0 * kRow4, *const vb = V0 + row0 * kRow4;
+    const uint8_t *const ksb = a.ks + row0 * kScales, *const vsb = a.vs + row0 * kScales;
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {       // rows past the end repeat the last one (finite values, masked out)
+      const uint32_t r = (uint32_t)min(kt + 16 * n + q16, end - 1);
+      w.k[n] = *reinterpret_cast<const uint4 *>(kb + r * kRow4 + 16 * G);
+      w.ks[n] = ksb[r * kScales + G];
+    }
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+      const uint32_t r = (uint32_t)min(kt + 16 * n + (lane >> 2), end - 1);
+      w.v[n] = *reinterpret_cast<const uint4 *>(vb + r * kRow4 + 16 * (lane & 3));
+      w.vs[n] = vsb[r * kScales + (lane & 3)];
+    }
+  };
+
+  Raw nxt;
+  const int jw = j0 + wave;
+  if (jw < j1) load(nxt, jw);
+  const bool tree = TREE && S.slab;
+  const bool row_ok = q16 < rows;
+  const int node = row_ok ? q16 / g : S.T - 1;
+  const int hq = it.kvh * g + (row_ok ? q16 % g : 0);
+  Query6<1> Q;
+  Q.load(row_ok, static_cast<const uint16_t *>(a.q) + ((int64_t)(S.row0 + node) * a.n_q + hq) * D, G);
+  WalkMask M{L, P, 0, node};
+  if (TREE) {
+    if (tree && tid < S.T) par[tid] = a.parent[S.row0 + tid];
+    ring_barrier();                       // (does not wait for the tile)
+    if (tree) M.root_path(par, node);
+  }
+
+  float m = -INFINITY, lsum = 0.f;
+  f32x4 O[D / 16];
+#pragma unroll
+  for (int i = 0; i < D / 16; ++i) O[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+  const bf16x2_t ones = __builtin_bit_cast(bf16x2_t, 0x3F803F80u);
+
+  for (int j = jw; j < j1; j += kWaves4) {
+    const Raw cur = nxt;
+    if (j + kWaves4 < j1) load(nxt, j + kWaves4);
+    const bool pre = j < np;
+    const int kt = (pre ? j : j - np) * TK;
+    f32x4 Sc[4];
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+      const i32x8_t ka = {(int)cur.k[n].x, (int)cur.k[n].y, (int)cur.k[n].z, (int)cur.k[n].w, 0, 0, 0, 0};
+      Sc[n] = f32x4{0.f, 0.f, 0.f, 0.f};
+      Sc[n] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(ka, Q.operand(0, 2), Sc[n], 4, 2, 0, (int)cur.ks[n], 2, (int)Q.sc[0]);
+      Sc[n] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(ka, Q.operand(0, 1), Sc[n], 4, 2, 0, (int)cur.ks[n], 1, (int)Q.sc[0]);
+      Sc[n] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(ka, Q.operand(0, 0), Sc[n], 4, 2, 0, (int)cur.ks[n], 0, (int)Q.sc[0]);
+    }
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+      const int r = 16 * n + (lane >> 2), c = lane & 3;
+      const float unit = kv4_scale(cur.vs[n]);
+      const uint32_t w[4] = {cur.v[n].x, cur.v[n].y, cur.v[n].z, cur.v[n].w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) *reinterpret_cast<uint4 *>(mem + r * (D * 2) + 16 * few_swz(r, 4 * c + i)) = kv4_bf16x8(w[i], unit);
+    }
+    // entry r of block n is key kt + 16 n + 4 G + r
+    if (TREE && !pre) {
+      if (kt + TK > L) {
+#pragma unroll
+        for (int n = 0; n < 4; ++n)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const int t = kt + 16 * n + 4 * G + r;
+            const uint32_t rel = (uint32_t)(t - L) & 127u;
+            const bool anc = ((rel < 64 ? M.alo : M.ahi) >> (rel & 63)) & 1u;
+            Sc[n][r] = (t < kend) & ((t < L) | anc) ? Sc[n][r] : -INFINITY;
+          }
+      }
+    } else if (kt + TK - 1 > (pre ? P - 1 : M.lim_lo)) {
+      const int vis = (pre ? P - 1 : M.lim) - kt - 4 * G;
+#pragma unroll
+      for (int n = 0; n < 4; ++n)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) Sc[n][r] = 16 * n + r <= vis ? Sc[n][r] : -INFINITY;
+    }
+    float tm = fmaxf(fmaxf(Sc[0][0], Sc[0][1]), Sc[0][2]);
+#pragma unroll
+    for (int e = 3; e < 15; e += 2) tm = fmaxf(fmaxf(tm, Sc[e >> 2][e & 3]), Sc[(e + 1) >> 2][(e + 1) & 3]);
+    tm = fmaxf(tm, Sc[3][3]);
+    const float tmax = max_of_groups(tm) * a.scale_log2;
+    const bool need = tmax > m + kRescaleSlack;       // as in walk_softmax_pv
+    if (__builtin_amdgcn_ballot_w64(need)) {
+      const float m_new = need ? tmax : m;
+      const float alpha = need ? (m == -INFINITY ? 0.f : fast_exp2(m - m_new)) : 1.f;
+      m = m_new;
+      lsum *= alpha;
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i) O[i] *= alpha;
+    }
+    const float m_use = m == -INFINITY ? 0.f : m;
+    // weights in bf16, the product's operand type, and their sum of the rounded ones
+    uint32_t pk[2][4];
+#pragma unroll
+    for (int n = 0; n < 4; ++n)
+#pragma unroll
+      for (int r = 0; r < 4; r += 2) {
+        const float p0 = fast_exp2(fmaf(Sc[n][r], a.scale_log2, -m_use)), p1 = fast_exp2(fmaf(Sc[n][r + 1], a.scale_log2, -m_use));
+        pk[n >> 1][2 * (n & 1) + (r >> 1)] = pack_bf16x2(p0, p1);
+      }
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) lsum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, pk[b][e]), ones, lsum, false);
+      const bf16x8 pf = __builtin_bit_cast(bf16x8, uint4{pk[b][0], pk[b][1], pk[b][2], pk[b][3]});
+#pragma unroll
+      for (int i = 0; i < D / 16; ++i) {
+        // lane e of a group of 16 gives the place of piece e % 4 (8 bytes) of row e / 4 and gets column e of four rows
+        const int r0 = 32 * b + 4 * G + (q16 >> 2), r1 = r0 + 16;
+        const int at0 = r0 * (D * 2) + 16 * few_swz(r0, 2 * i + ((q16 & 3) >> 1)) + 8 * (q16 & 1);
+        const int at1 = r1 * (D * 2) + 16 * few_swz(r1, 2 * i + ((q16 & 3) >> 1)) + 8 * (q16 & 1);
+        const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t *)(mem + at0));
+        const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t *)(mem + at1));
+        const bf16x8 vf = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+        O[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf, O[i], 0, 0, 0);
+      }
+    }
+  }
+
+  // The waves' parts: O[i] of a lane is columns 16 i + 4 G .. + 3 of row q16.
+  float *const part = reinterpret_cast<float *>(mem);
+#pragma unroll
+  for (int i = 0; i < D / 16; ++i) *reinterpret_cast<f32x4 *>(part + ((4 * i + G) * kFewRows + q16) * 4) = O[i];
+  const float ltot = sum_of_groups(lsum);
+  if (G == 0) {
+    part[D * kFewRows + q16] = m;
+    part[D * kFewRows + kFewRows + q16] = ltot;
+  }
+  __syncthreads();
+  const bool direct = walk_direct(S, 0, g);
+  float *const u = direct ? nullptr : a.part + (int64_t)walk_part(a, S, it.kvh, 0, it.ch) * walk_unit_floats(D / 32);
+#pragma unroll
+  for (int e = 0; e < 2; ++e) {
+    const int row = tid & 15, quad = (tid >> 4) + 16 * e;     // columns 4 quad .. + 3
+    if (row >= rows) break;
+    float w[kWaves4], mx = -INFINITY, lt = 0.f;
+#pragma unroll
+    for (int v = 0; v < kWaves4; ++v) {
+      w[v] = reinterpret_cast<const float *>(lds[v])[D * kFewRows + row];
+      mx = fmaxf(mx, w[v]);
+    }
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int v = 0; v < kWaves4; ++v) {
+      const float *pv = reinterpret_cast<const float *>(lds[v]);
+      const float wt = w[v] == -INFINITY ? 0.f : fast_exp2(w[v] - mx);
+      lt = fmaf(pv[D * kFewRows + kFewRows + row], wt, lt);
+      const f32x4 x = *reinterpret_cast<const f32x4 *>(pv + (quad * kFewRows + row) * 4);
+#pragma unroll
+      for (int c = 0; c < 4; ++c) o[c] = fmaf(x[c], wt, o[c]);
+    }
+    if (direct) {
+      const float inv = 1.f / lt;
+      const int64_t at = ((int64_t)(S.row0 + row / g) * a.n_q + it.kvh * g + row % g) * D + 4 * quad;
+      *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(a.out) + at) = uint2{pack_bf16x2(o[0] * inv, o[1] * inv), pack_bf16x2(o[2] * inv, o[3] * inv)};
+    } else {                              // in the order of write_part: row % 32 + 32 h, columns 32 i + 8 q + 4 h
+      *reinterpret_cast<f32x4 *>(u + ((quad >> 1) * 64 + row + 32 * (quad & 1)) * 4) = o;
+      if (quad == 0) {
+        u[(D / 32) * 1024 + row] = mx;
+        u[(D / 32) * 1024 + 32 + row] = lt;
+      }
+    }
+  }
+}
+
 template <bool TREE>
 __global__ __launch_bounds__(kWaves4 * 64, 2) void walk4_attn_bf16(WalkArgs a) {
   __shared__ __attribute__((aligned(1024))) uint8_t kring[2][kKTile4];
-  __shared__ __attribute__((aligned(1024))) uint8_t vring[2][kVTile4];
+  __shared__ __attribute__((aligned(1024))) uint8_t vring[4][kVTile4];   // two slots, or a tile of each wave
   WalkItem it;
   decode_walk(a, blockIdx.x, it);
-  if (it.S.rb == 64) walk4<2, TREE>(a, it, kring, vring);
+  if (it.S.rb == 32) walk4_few<TREE>(a, it, vring, reinterpret_cast<int *>(kring[0]));
+  else if (it.S.rb == 64) walk4<2, TREE>(a, it, kring, vring);
   else walk4<1, TREE>(a, it, kring, vring);
 }
 

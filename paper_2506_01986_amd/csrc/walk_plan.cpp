@@ -53,7 +53,7 @@ int64_t count_tiles(const WalkSet &s, int g) {
 
 }  // namespace
 
-void plan_walk(int dt, bool causal, const std::vector<WalkSeq> &seqs, int n_kv, int g, int head_dim, int cus, WalkPlan *p) {
+void plan_walk(int dt, bool causal, const std::vector<WalkSeq> &seqs, int n_kv, int g, int head_dim, int cus, WalkPlan *p, bool four) {
   const bool f32 = dt == 0;
   const int nseq = (int)seqs.size();
   auto rows_of = [&](int i) { return (int64_t)seqs[i].T * g; };
@@ -143,7 +143,7 @@ void plan_walk(int dt, bool causal, const std::vector<WalkSeq> &seqs, int n_kv, 
   double work = 0;
   for (WalkSet &s : sets) {
     const int64_t rows = (int64_t)s.T * g;
-    s.rb = f32 ? 32 : rows <= 64 || small ? 64 : 128;
+    s.rb = f32 || (four && rows <= 16) ? 32 : rows <= 64 || small ? 64 : 128;
     s.nrb = ceil_div(rows, s.rb);
     work += (double)count_tiles(s, g) * tile_us(s) * n_kv;
   }
