@@ -1395,8 +1395,9 @@ int append_impl(int dt, int B, const int32_t *off, const specmemo_rows *x, int n
   }
   // at most 2^30 threads a launch, of up to 32 a head
   const int64_t per_launch = std::max<int64_t>(1, (INT64_C(1) << 25) / (n_q + 2 * kv->n_kv));
+  const int cus = device_cus();
   return for_token_ranges(a, ti, off, kv, per_launch, [&] {
-    return hip_status(launch_append(dt, kv4 != nullptr, a, static_cast<hipStream_t>(stream)), "append launch");
+    return hip_status(launch_append(dt, kv4 != nullptr, a, cus, static_cast<hipStream_t>(stream)), "append launch");
   });
 }
 
@@ -1455,8 +1456,9 @@ int specmemo_kv4_read(specmemo_dtype dt, int32_t B, const int32_t *new_off_h, co
     a.head_dim = kv->head_dim;
     // at most 2^30 threads a launch, of up to 16 a row of K or V
     const int64_t per_launch = std::max<int64_t>(1, (INT64_C(1) << 25) / kv->n_kv);
+    const int cus = device_cus();
     return for_token_ranges(a, ti, new_off_h, &view, per_launch,
-                            [&] { return hip_status(launch_kv4_read(dt, a, static_cast<hipStream_t>(stream)), "read launch"); });
+                            [&] { return hip_status(launch_kv4_read(dt, a, cus, static_cast<hipStream_t>(stream)), "read launch"); });
   });
 }
 

@@ -256,7 +256,7 @@ void plan_walk(int dt, bool causal, const std::vector<WalkSeq> &seqs, int n_kv, 
 struct RowsSeq {
   int32_t off, row0_lo, row0_hi;
 };
-constexpr int kMaxRowsSeq = 316;   // sequences of a launch
+constexpr int kMaxRowsSeq = 310;   // sequences of a launch
 struct AppendArgs {
   const void *q, *k, *v;          // token i's heads at i * stride elements
   int64_t q_stride, k_stride, v_stride;
@@ -270,11 +270,13 @@ struct AppendArgs {
   int32_t n_q, n_kv, head_dim, n_pos, rot_dim, pairs;
   float eps;
   int32_t tok0, tok1;             // tokens of this launch
+  int32_t lph_log2, q_log2, kv_log2, q_turns, kv_turns;   // the launch's own split (append_kernel)
+  uint32_t four_blocks;
   int32_t nseq;
   RowsSeq seq[kMaxRowsSeq];
 };
 static_assert(sizeof(AppendArgs) <= 4096, "kernel arguments are limited to 4 KB");
-hipError_t launch_append(int dt, bool four, const AppendArgs &a, hipStream_t st);
+hipError_t launch_append(int dt, bool four, AppendArgs &a, int cus, hipStream_t st);
 struct ReadArgs {
   const uint8_t *k, *v, *ks, *vs;
   void *k_out, *v_out;            // [tokens][n_kv][head_dim]
@@ -282,7 +284,7 @@ struct ReadArgs {
   int32_t n_kv, head_dim, tok0, tok1, nseq;
   RowsSeq seq[kMaxRowsSeq];
 };
-hipError_t launch_kv4_read(int dt, const ReadArgs &a, hipStream_t st);
+hipError_t launch_kv4_read(int dt, const ReadArgs &a, int cus, hipStream_t st);
 
 // ---- acceptance ------------------------------------------------------------------
 struct AcceptArgs {

@@ -9,6 +9,9 @@
 // for q and k; v is stored as it is.  Everything is one read of the inputs and one
 // write of the outputs: the kernels are bound by memory, or where there are few rows
 // by one launch's latency.
+#include <algorithm>
+#include <type_traits>
+
 #include "device.h"
 #include "internal.h"
 #include "kv4.h"
@@ -20,7 +23,8 @@ namespace {
 constexpr int kThreads = 256;
 
 // The sequence that holds token `tok`: the last one with off <= tok.  The wave's first
-// token is searched 64 ways a round; the other lanes' lie a few sequences on.
+// token is searched 64 ways a round, by all lanes of the wave (no call from a branch that
+// only some of them take); the other lanes' lie a few sequences on.
 __device__ __forceinline__ int find_seq(const RowsSeq *seq, int nseq, int tok) {
   const int lane = threadIdx.x & 63, first = __builtin_amdgcn_readfirstlane(tok);
   int lo = 0, cnt = nseq;
@@ -39,18 +43,12 @@ __device__ __forceinline__ int64_t pool_row(const RowsSeq *seq, int nseq, int to
   return (int64_t)((uint64_t)(uint32_t)s.row0_hi << 32 | (uint32_t)s.row0_lo) + tok;
 }
 
+// The 16 bytes of a row that a lane has, as E numbers.
 template <typename T, int E>
-__device__ __forceinline__ void load_cols(T (&x)[E], const void *p, bool bf16) {
-  if (bf16) {
-    const uint4 w = *static_cast<const uint4 *>(p);
-    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+__device__ __forceinline__ void unpack(T (&x)[E], uint4 w) {
+  const uint32_t u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-    for (int i = 0; i < E; ++i) x[i] = bf16_to_f32((uint16_t)(u[i >> 1] >> (16 * (i & 1))));
-  } else {
-    const f32x4 w = *static_cast<const f32x4 *>(p);
-#pragma unroll
-    for (int i = 0; i < E; ++i) x[i] = w[i & 3];
-  }
+  for (int i = 0; i < E; ++i) x[i] = E == 8 ? bf16_to_f32((uint16_t)(u[i >> 1] >> (16 * (i & 1)))) : __uint_as_float(u[i & 3]);
 }
 
 // fp64 -> fp32 with the last bit set where bits are lost: comparisons with numbers of
@@ -62,173 +60,305 @@ __device__ __forceinline__ float sticky_f32(double d) {
 }
 __device__ __forceinline__ float sticky_f32(float f) { return f; }
 
-// One row chunk of E columns a lane (16 bytes of the inputs), LPH lanes to a head.  T
-// is the type of the arithmetic: 32 bits, and 64 for keys that go to 4 bits, where a
-// value next to a border between two codes must fall on its own side of it.
-template <typename T, int E, bool BF16>
-struct Chunk {
-  T x[E];
-
-  __device__ __forceinline__ void norm(const void *w, int d, int lph, float eps, bool on) {
-    T s = 0;
-#pragma unroll
-    for (int i = 0; i < E; ++i) s += on ? x[i] * x[i] : T(0);
-    for (int m = 1; m < lph; m <<= 1) s += __shfl_xor(s, m);
-    const T r = T(1) / sqrt(s / T(d) + T(eps));
-    T g[E];
-    if (on) load_cols(g, w, BF16);
-#pragma unroll
-    for (int i = 0; i < E; ++i) x[i] = on ? x[i] * r * g[i] : T(0);
+// Sum over the lph lanes of a head, in each of them: a row of 16 lanes by DPP, as in
+// wave_max.
+__device__ __forceinline__ float head_sum(float v, int lph) {
+  if (lph == 16) {
+    v += dpp_f<0xB1>(v);
+    v += dpp_f<0x4E>(v);
+    v += dpp_f<0x141>(v);
+    return v + dpp_f<0x140>(v);
   }
-
-  // Columns c .. c + E - 1 of a head of which `rot` are rotated; halves: column c < rot / 2
-  // turns with c + rot / 2, which another lane of the head holds; pairs: 2 i with 2 i + 1.
-  __device__ __forceinline__ void rotate(const float *cs, const float *sn, int c, int rot, bool pairs) {
-    if (pairs) {
-      if (c >= rot) return;
-#pragma unroll
-      for (int i = 0; i < E; i += 2) {
-        const T co = cs[(c + i) >> 1], si = sn[(c + i) >> 1], a = x[i], b = x[i + 1];
-        x[i] = a * co - b * si;
-        x[i + 1] = b * co + a * si;
-      }
-      return;
-    }
-    const int half = rot >> 1;
-    const bool low = c < half;
-    const int other = (threadIdx.x & 63) + (c >= rot ? 0 : low ? half / E : -(half / E));
-    T y[E];
-#pragma unroll
-    for (int i = 0; i < E; ++i) y[i] = __shfl(x[i], other);
-    if (c >= rot) return;
-    const int at = low ? c : c - half;
-#pragma unroll
-    for (int i = 0; i < E; i += 4) {
-      const f32x4 co = *reinterpret_cast<const f32x4 *>(cs + at + i), si = *reinterpret_cast<const f32x4 *>(sn + at + i);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) x[i + e] = low ? x[i + e] * T(co[e]) - y[i + e] * T(si[e]) : x[i + e] * T(co[e]) + y[i + e] * T(si[e]);
-    }
+  for (int m = 1; m < lph; m <<= 1) v += __shfl_xor(v, m);
+  return v;
+}
+template <int CTRL>
+__device__ __forceinline__ double dpp_d(double v) {
+  const uint64_t u = __double_as_longlong(v);
+  return __longlong_as_double((long long)((uint64_t)(uint32_t)dpp_i<CTRL>((int)(u >> 32)) << 32 | (uint32_t)dpp_i<CTRL>((int)u)));
+}
+__device__ __forceinline__ double head_sum(double v, int lph) {
+  if (lph == 16) {
+    v += dpp_d<0xB1>(v);
+    v += dpp_d<0x4E>(v);
+    v += dpp_d<0x141>(v);
+    return v + dpp_d<0x140>(v);
   }
+  for (int m = 1; m < lph; m <<= 1) v += __shfl_xor(v, m);
+  return v;
+}
 
-  __device__ __forceinline__ void store(void *p) const {
-    if constexpr (BF16) {
-      uint32_t u[E / 2];
+// 1 / sqrt(x): the instruction's result (one unit off at most), in 64 bits improved
+// from half the digits by two steps of y (3 - x y^2) / 2.
+__device__ __forceinline__ float inv_sqrt(float x) { return __builtin_amdgcn_rsqf(x); }
+__device__ __forceinline__ double inv_sqrt(double x) {
+  double y = __builtin_amdgcn_rsq(x);
 #pragma unroll
-      for (int i = 0; i < E; i += 2) u[i / 2] = pack_bf16x2((float)x[i], (float)x[i + 1]);
-      *static_cast<uint4 *>(p) = uint4{u[0], u[1], u[2], u[3]};
-    } else {
-      *static_cast<f32x4 *>(p) = f32x4{(float)x[0], (float)x[1], (float)x[2], (float)x[3]};
-    }
-  }
+  for (int i = 0; i < 2; ++i) y = fma(0.5 * y, fma(-x * y, y, 1.0), y);
+  return y;
+}
 
-  // Columns c .. of a row in 4 bits; the lanes of a group (32 / E of them) find its scale together.
-  __device__ __forceinline__ void store4(uint8_t *codes, uint8_t *scales, int c, bool on) const {
-    float y[E], top = 0.f;
-    bool odd = false;
+// How a lane's E columns of a head turn: out = x fx + y fy with y the columns that x's
+// turn with, of another lane of the head or its own pairs; fx and fy are cos and sin,
+// times the columns' norm weights in fp32.
+template <int E>
+struct Lane {
+  static constexpr int ES = 16 / E;
+  int c, c2, from;          // first column of the lane's and of those they turn with; the lane that has them
+  bool pairs, turns, live;  // live: the token has a position, and the lane columns
+  int p, half;
+
+  __device__ __forceinline__ Lane(const AppendArgs &a, int lph, int tok, bool on) {
+    half = a.rot_dim >> 1;
+    c = (threadIdx.x & (lph - 1)) * E;
+    turns = c < a.rot_dim;
+    pairs = a.pairs;
+    const bool low = c < half, own = !turns || pairs;
+    from = (threadIdx.x & 63) + (own ? 0 : low ? half / E : -(half / E));
+    c2 = own ? c : low ? c + half : c - half;
+    p = a.pos ? a.pos[tok] : 0;
+    live = on && c < a.head_dim && (!a.pos || (uint32_t)p < (uint32_t)a.n_pos);   // no such position: the rows are left as they were
+    turns = turns && live;
+  }
+  __device__ __forceinline__ void angles(const AppendArgs &a, float (&co)[E], float (&si)[E]) const {
 #pragma unroll
     for (int i = 0; i < E; ++i) {
-      y[i] = sticky_f32(x[i]);
-      top = fmaxf(top, fabsf(y[i]));
-      odd |= !(fabsf(y[i]) < INFINITY);
+      co[i] = 1.f;
+      si[i] = 0.f;
     }
-    top = odd ? INFINITY : top;
+    if (!turns) return;
+    const float *cs = a.cos + (int64_t)p * half, *sn = a.sin + (int64_t)p * half;
+    if (pairs) {
 #pragma unroll
-    for (int m = 1; m < kKv4Group / E; m <<= 1) top = fmaxf(top, __shfl_xor(top, m));
-    if (!on) return;
-    const uint32_t byte = kv4_scale_byte(top);
-    const float unit = kv4_scale(byte);
-    uint32_t w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, y[0], y[1], unit, 0);
-    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, y[2], y[3], unit, 1);
-    if constexpr (E == 8) {
-      w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, y[4], y[5], unit, 2);
-      w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, y[6], y[7], unit, 3);
-      *reinterpret_cast<uint32_t *>(codes + c / 2) = w;
+      for (int i = 0; i < E; ++i) {
+        co[i] = cs[(c >> 1) + (i >> 1)];
+        si[i] = i & 1 ? sn[(c >> 1) + (i >> 1)] : -sn[(c >> 1) + (i >> 1)];
+      }
     } else {
-      *reinterpret_cast<uint16_t *>(codes + c / 2) = (uint16_t)w;
+      const bool low = c < half;
+      const int at = low ? c : c2;
+#pragma unroll
+      for (int i = 0; i < E; i += 4) {
+        const f32x4 x = *reinterpret_cast<const f32x4 *>(cs + at + i), y = *reinterpret_cast<const f32x4 *>(sn + at + i);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          co[i + e] = x[e];
+          si[i + e] = low ? -y[e] : y[e];
+        }
+      }
     }
-    if (c % kKv4Group == 0) scales[c / kKv4Group] = (uint8_t)byte;
+  }
+  // The columns that the lane's turn with, in its own columns' order.
+  __device__ __forceinline__ uint4 other(uint4 w, int lph) const {
+    if (pairs)
+      return E == 8 ? uint4{w.x >> 16 | w.x << 16, w.y >> 16 | w.y << 16, w.z >> 16 | w.z << 16, w.w >> 16 | w.w << 16} : uint4{w.y, w.x, w.w, w.z};
+    if (lph == 16 && half == 8 * E)       // the lane eight on in its row of 16
+      return uint4{(uint32_t)dpp_i<0x128>((int)w.x), (uint32_t)dpp_i<0x128>((int)w.y), (uint32_t)dpp_i<0x128>((int)w.z), (uint32_t)dpp_i<0x128>((int)w.w)};
+    return uint4{(uint32_t)__shfl((int)w.x, from), (uint32_t)__shfl((int)w.y, from), (uint32_t)__shfl((int)w.z, from), (uint32_t)__shfl((int)w.w, from)};
+  }
+  __device__ __forceinline__ void weights(float (&own)[E], float (&far)[E], const void *norm, int d) const {
+    const uint4 x = ld16_or_zero(c < d, static_cast<const char *>(norm) + c * ES), y = ld16_or_zero(c < d, static_cast<const char *>(norm) + c2 * ES);
+    unpack(own, x);
+    unpack(far, y);
+    if (pairs) {
+#pragma unroll
+      for (int i = 0; i < E; i += 2) {
+        const float z = far[i];
+        far[i] = far[i + 1];
+        far[i + 1] = z;
+      }
+    }
   }
 };
 
-// LPH lanes have a head's row; a wave's rows follow one another, token by token: the
-// token's query heads, then its key heads, then its value heads.
-template <bool BF16, bool FOUR>
-__global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a, int lph_log2) {
-  constexpr int E = BF16 ? 8 : 4, ES = BF16 ? 2 : 4;
-  using TK = typename std::conditional<FOUR, double, float>::type;
-  const int lph = 1 << lph_log2, heads = a.n_q + 2 * a.n_kv, d = a.head_dim;
-  const int64_t unit = ((int64_t)blockIdx.x * kThreads + threadIdx.x) >> lph_log2;
-  const int64_t units = (int64_t)(a.tok1 - a.tok0) * heads;
-  const int c = (threadIdx.x & (lph - 1)) * E;
-  const bool on = unit < units && c < d;
-  const int64_t u = unit < units ? unit : units - 1;
-  const int tok = a.tok0 + (int)(u / heads), head = (int)(u % heads);
-  const int kind = head < a.n_q ? 0 : head < a.n_q + a.n_kv ? 1 : 2;
-  const int hk = kind == 0 ? head : kind == 1 ? head - a.n_q : head - a.n_q - a.n_kv;
-  const char *src = static_cast<const char *>(kind == 0 ? a.q : kind == 1 ? a.k : a.v) +
-                    ((kind == 0 ? a.q_stride : kind == 1 ? a.k_stride : a.v_stride) * tok + (int64_t)hk * d + c) * ES;
-  float x[E];
+// The row's 1 / sqrt(mean of squares + eps).
+template <typename T, int E>
+__device__ __forceinline__ T row_norm(const T (&x)[E], float eps, int d, int lph) {
+  T s = 0;
 #pragma unroll
-  for (int i = 0; i < E; ++i) x[i] = 0.f;
-  if (on) load_cols(x, src, BF16);
-  const int p = a.pos ? a.pos[tok] : 0;
-  const bool live = on && (!a.pos || (uint32_t)p < (uint32_t)a.n_pos);   // no such position: the row is left as it was
-  const int64_t row = pool_row(a.seq, a.nseq, tok);
-  const int64_t at = (int64_t)hk * a.cap_total + row;
-  const int pc = a.pos ? min(max(p, 0), a.n_pos - 1) : 0;
-  const float *cs = a.cos + (int64_t)pc * (a.rot_dim >> 1), *sn = a.sin + (int64_t)pc * (a.rot_dim >> 1);
-  auto turn = [&](auto &y, const void *w) __attribute__((always_inline)) {
-    if (w) y.norm(static_cast<const char *>(w) + c * ES, d, lph, a.eps, on);
-    if (a.pos) y.rotate(cs, sn, c, a.rot_dim, a.pairs);
-  };
-  // A wave may hold rows of all three kinds; the lanes of one head agree.
-  if (kind == 0) {
-    Chunk<float, E, BF16> y;
+  for (int i = 0; i < E; ++i) s += x[i] * x[i];
+  return inv_sqrt(head_sum(s, lph) / T(d) + T(eps));
+}
+
+template <int E>
+__device__ __forceinline__ void store_row(void *p, const float (&x)[E]) {
+  if constexpr (E == 8)
+    *static_cast<uint4 *>(p) = uint4{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7])};
+  else
+    *static_cast<f32x4 *>(p) = f32x4{x[0], x[1], x[2], x[3]};
+}
+
+// Columns c .. of a row in 4 bits; the lanes of a group (32 / E of them) find its scale together.
+template <typename T, int E>
+__device__ __forceinline__ void store_row4(uint8_t *codes, uint8_t *scales, int c, const T (&x)[E], bool on) {
+  float y[E], top = 0.f;
+  bool odd = false;
 #pragma unroll
-    for (int i = 0; i < E; ++i) y.x[i] = x[i];
-    turn(y, a.q_norm);
-    if (live) y.store(static_cast<char *>(a.q_out) + (((int64_t)tok * a.n_q + hk) * d + c) * ES);
-  } else if (kind == 1) {
-    Chunk<TK, E, BF16> y;
+  for (int i = 0; i < E; ++i) {
+    y[i] = sticky_f32(x[i]);
+    top = fmaxf(top, fabsf(y[i]));
+    odd |= !(fabsf(y[i]) < INFINITY);
+  }
+  top = odd ? INFINITY : top;
 #pragma unroll
-    for (int i = 0; i < E; ++i) y.x[i] = x[i];
-    turn(y, a.k_norm);
-    if constexpr (FOUR) y.store4(static_cast<uint8_t *>(a.pool_k) + at * (d / 2), a.ks + at * (d / kKv4Group), c, live);
-    else if (live) y.store(static_cast<char *>(a.pool_k) + (at * d + c) * ES);
+  for (int m = 1; m < kKv4Group / E; m <<= 1) top = fmaxf(top, __shfl_xor(top, m));
+  if (!on) return;
+  const uint32_t byte = kv4_scale_byte(top);
+  const float unit = kv4_scale(byte);
+  uint32_t w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, y[0], y[1], unit, 0);
+  w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, y[2], y[3], unit, 1);
+  if constexpr (E == 8) {
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, y[4], y[5], unit, 2);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, y[6], y[7], unit, 3);
+    *reinterpret_cast<uint32_t *>(codes + c / 2) = w;
   } else {
-    Chunk<float, E, BF16> y;
+    *reinterpret_cast<uint16_t *>(codes + c / 2) = (uint16_t)w;
+  }
+  if (c % kKv4Group == 0) scales[c / kKv4Group] = (uint8_t)byte;
+}
+
+// lph lanes have a head's row, and a block 256 / lph of them (slots).  The first four_blocks
+// blocks take the key and value heads that go to 4 bits, one a slot: keys in fp64, so
+// that a value next to a border between two codes falls on its own side of it.  The
+// others take the heads that stay in the inputs' type, HB a slot with their loads
+// together.  The slots take the heads of one token, or of several where a token has few
+// (1 << *_log2 slots each), so a lane loads cos, sin and the norm's weights once.
+template <bool BF16, bool FOUR, int HB>
+__global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a) {
+  constexpr int E = BF16 ? 8 : 4, ES = BF16 ? 2 : 4;
+  const int lph = 1 << a.lph_log2, d = a.head_dim, all = kThreads >> a.lph_log2, slot = threadIdx.x >> a.lph_log2;
+  const int c = (threadIdx.x & (lph - 1)) * E;
+  if (!FOUR || blockIdx.x >= a.four_blocks) {
+    const uint32_t bid = blockIdx.x - a.four_blocks;
+    const int turn = (int)(bid % a.q_turns), slots = 1 << a.q_log2;
+    const int at = a.tok0 + (int)(bid / a.q_turns) * (all >> a.q_log2) + (slot >> a.q_log2), tok = min(at, a.tok1 - 1);
+    const int h0 = (slot & (slots - 1)) + turn * HB * slots, heads = FOUR ? a.n_q : a.n_q + 2 * a.n_kv;
+    const bool on = at < a.tok1;
+    uint4 row[HB];
 #pragma unroll
-    for (int i = 0; i < E; ++i) y.x[i] = x[i];
-    if constexpr (FOUR) y.store4(static_cast<uint8_t *>(a.pool_v) + at * (d / 2), a.vs + at * (d / kKv4Group), c, live);
-    else if (live) y.store(static_cast<char *>(a.pool_v) + (at * d + c) * ES);
+    for (int n = 0; n < HB; ++n) {
+      const int head = h0 + n * slots;
+      const bool q = FOUR || head < a.n_q, k = head < a.n_q + a.n_kv;
+      const char *base = static_cast<const char *>(q ? a.q : k ? a.k : a.v);
+      const int64_t off = (q ? a.q_stride : k ? a.k_stride : a.v_stride) * tok + (int64_t)(q ? head : k ? head - a.n_q : head - a.n_q - a.n_kv) * d + c;
+      row[n] = ld16_or_zero(on && c < d && head < heads, base + off * ES);
+    }
+    const Lane<E> l(a, lph, tok, on);
+    float co[E], si[E], qx[E], qy[E], kx[E], ky[E];
+    l.angles(a, co, si);
+    auto factors = [&](float (&fx)[E], float (&fy)[E], const void *norm) __attribute__((always_inline)) {
+      if (norm) l.weights(fx, fy, norm, d);
+#pragma unroll
+      for (int i = 0; i < E; ++i) {
+        fx[i] = norm ? fx[i] * co[i] : co[i];
+        fy[i] = norm ? fy[i] * si[i] : si[i];
+      }
+    };
+    factors(qx, qy, a.q_norm);
+    if (!FOUR) factors(kx, ky, a.k_norm);
+    const int64_t prow = FOUR ? 0 : pool_row(a.seq, a.nseq, tok);
+#pragma unroll
+    for (int n = 0; n < HB; ++n) {
+      const int head = h0 + n * slots;
+      const bool put = l.live && head < heads;
+      // The slots of a wave may hold heads of different kinds; the lanes of one head agree.
+      auto turn_row = [&](char *dst, const float (&fx)[E], const float (&fy)[E], bool norm) __attribute__((always_inline)) {
+        float x[E], y[E];
+        unpack(x, row[n]);
+        unpack(y, l.other(row[n], lph));
+        const float r = norm ? row_norm(x, a.eps, d, lph) : 1.f;
+#pragma unroll
+        for (int i = 0; i < E; ++i) {
+          x[i] *= fx[i];
+          if (l.turns) x[i] = fmaf(y[i], fy[i], x[i]);
+          if (norm) x[i] *= r;
+        }
+        if (put) store_row(dst, x);
+      };
+      if (FOUR || head < a.n_q) {
+        turn_row(static_cast<char *>(a.q_out) + (((int64_t)tok * a.n_q + head) * d + c) * ES, qx, qy, a.q_norm != nullptr);
+      } else if (head < a.n_q + a.n_kv) {
+        turn_row(static_cast<char *>(a.pool_k) + (((head - a.n_q) * a.cap_total + prow) * d + c) * ES, kx, ky, a.k_norm != nullptr);
+      } else if (put) {
+        *reinterpret_cast<uint4 *>(static_cast<char *>(a.pool_v) + (((head - a.n_q - a.n_kv) * a.cap_total + prow) * d + c) * ES) = row[n];
+      }
+    }
+    return;
+  }
+  const int turn = (int)(blockIdx.x % a.kv_turns), slots = 1 << a.kv_log2;
+  const int at = a.tok0 + (int)(blockIdx.x / a.kv_turns) * (all >> a.kv_log2) + (slot >> a.kv_log2), tok = min(at, a.tok1 - 1);
+  const int head = (slot & (slots - 1)) + turn * slots;
+  const bool on = at < a.tok1 && head < 2 * a.n_kv, k = head < a.n_kv;
+  const int hk = k ? head : head - a.n_kv;
+  const uint4 row = ld16_or_zero(on && c < d, static_cast<const char *>(k ? a.k : a.v) + ((k ? a.k_stride : a.v_stride) * tok + (int64_t)hk * d + c) * ES);
+  const Lane<E> l(a, lph, tok, on);
+  const int64_t r = (int64_t)hk * a.cap_total + pool_row(a.seq, a.nseq, tok);
+  // A wave may hold keys and values; the lanes of one head agree.
+  if (k) {
+    float co[E], si[E], wx[E], wy[E];
+    l.angles(a, co, si);
+    if (a.k_norm) l.weights(wx, wy, a.k_norm, d);
+    double x[E], y[E];
+    unpack(x, row);
+    unpack(y, l.other(row, lph));
+    if (a.k_norm) {
+      const double n = row_norm(x, a.eps, d, lph);
+#pragma unroll
+      for (int i = 0; i < E; ++i) {
+        x[i] *= n * wx[i];
+        y[i] *= n * wy[i];
+      }
+    }
+    if (l.turns) {
+#pragma unroll
+      for (int i = 0; i < E; ++i) x[i] = x[i] * co[i] + y[i] * si[i];
+    }
+    store_row4(static_cast<uint8_t *>(a.pool_k) + r * (d / 2), a.ks + r * (d / kKv4Group), c, x, l.live);
+  } else {
+    float x[E];
+    unpack(x, row);
+    store_row4(static_cast<uint8_t *>(a.pool_v) + r * (d / 2), a.vs + r * (d / kKv4Group), c, x, l.live);
   }
 }
 
-// Rows of a 4-bit pool as values: eight columns a lane.
-template <bool BF16>
-__global__ __launch_bounds__(kThreads) void kv4_read_kernel(ReadArgs a) {
+// Rows of a 4-bit pool as values: a thread has eight columns of one head of K or V and
+// takes them for TB tokens.
+template <bool BF16, int TB>
+__global__ __launch_bounds__(kThreads) void kv4_read_kernel(ReadArgs a, int blocks) {
   const int cw = a.head_dim >> 3, d = a.head_dim;           // chunks of a row
-  const int64_t per = (int64_t)2 * a.n_kv * cw;             // and of a token
-  const int64_t all = per * (a.tok1 - a.tok0), at = (int64_t)blockIdx.x * kThreads + threadIdx.x;
-  const int64_t i = at < all ? at : all - 1;
-  const int tok = a.tok0 + (int)(i / per), in = (int)(i % per);
-  const int c = in % cw, head = in / cw, hk = head % a.n_kv;
+  const int per = 2 * a.n_kv * cw;                          // and of a token
+  const int in = (int)(blockIdx.x % blocks) * kThreads + threadIdx.x;
+  const int tok0 = a.tok0 + (int)(blockIdx.x / blocks) * TB;
+  const int x = min(in, per - 1), c = x % cw, head = x / cw;
   const bool v = head >= a.n_kv;
-  const int64_t row = (int64_t)hk * a.cap_total + pool_row(a.seq, a.nseq, tok);
-  if (at >= all) return;
-  const uint32_t w = *reinterpret_cast<const uint32_t *>((v ? a.v : a.k) + row * (d >> 1) + 4 * c);
-  const uint32_t byte = (v ? a.vs : a.ks)[row * (d / kKv4Group) + (c >> 2)];
-  const float unit = byte == kKv4Nan ? __uint_as_float(0x7FC00000u) : kv4_scale(byte);
-  const int64_t o = ((int64_t)tok * a.n_kv + hk) * d + 8 * c;
-  if (BF16) {
-    *reinterpret_cast<uint4 *>(static_cast<uint16_t *>(v ? a.v_out : a.k_out) + o) =
-        byte == kKv4Nan ? uint4{0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u} : kv4_bf16x8(w, unit);
-  } else {
-    const f32x2_t p0 = kv4_f32x2<0>(w, unit), p1 = kv4_f32x2<1>(w, unit), p2 = kv4_f32x2<2>(w, unit), p3 = kv4_f32x2<3>(w, unit);
-    f32x4 *dst = reinterpret_cast<f32x4 *>(static_cast<float *>(v ? a.v_out : a.k_out) + o);
-    const bool nan = byte == kKv4Nan;
-    dst[0] = nan ? f32x4{unit, unit, unit, unit} : f32x4{p0[0], p0[1], p1[0], p1[1]};
-    dst[1] = nan ? f32x4{unit, unit, unit, unit} : f32x4{p2[0], p2[1], p3[0], p3[1]};
+  const int hk = v ? head - a.n_kv : head;
+  const uint8_t *const codes = (v ? a.v : a.k), *const scales = v ? a.vs : a.ks;
+  int s = find_seq(a.seq, a.nseq, tok0);
+  uint32_t w[TB], byte[TB];
+#pragma unroll
+  for (int n = 0; n < TB; ++n) {
+    const int tok = min(tok0 + n, a.tok1 - 1);
+    while (s + 1 < a.nseq && a.seq[s + 1].off <= tok) ++s;
+    const int64_t r = (int64_t)hk * a.cap_total + (int64_t)((uint64_t)(uint32_t)a.seq[s].row0_hi << 32 | (uint32_t)a.seq[s].row0_lo) + tok;
+    w[n] = *reinterpret_cast<const uint32_t *>(codes + r * (d >> 1) + 4 * c);
+    byte[n] = scales[r * (d / kKv4Group) + (c >> 2)];
+  }
+  if (in >= per) return;
+#pragma unroll
+  for (int n = 0; n < TB; ++n) {
+    if (tok0 + n >= a.tok1) return;
+    const bool nan = byte[n] == kKv4Nan;
+    const float unit = nan ? __uint_as_float(0x7FC00000u) : kv4_scale(byte[n]);
+    const int64_t o = ((int64_t)(tok0 + n) * a.n_kv + hk) * d + 8 * c;
+    if (BF16) {
+      *reinterpret_cast<uint4 *>(static_cast<uint16_t *>(v ? a.v_out : a.k_out) + o) =
+          nan ? uint4{0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u} : kv4_bf16x8(w[n], unit);
+    } else {
+      const f32x2_t p0 = kv4_f32x2<0>(w[n], unit), p1 = kv4_f32x2<1>(w[n], unit), p2 = kv4_f32x2<2>(w[n], unit), p3 = kv4_f32x2<3>(w[n], unit);
+      f32x4 *dst = reinterpret_cast<f32x4 *>(static_cast<float *>(v ? a.v_out : a.k_out) + o);
+      dst[0] = nan ? f32x4{unit, unit, unit, unit} : f32x4{p0[0], p0[1], p1[0], p1[1]};
+      dst[1] = nan ? f32x4{unit, unit, unit, unit} : f32x4{p2[0], p2[1], p3[0], p3[1]};
+    }
   }
 }
 
@@ -277,24 +407,49 @@ __global__ __launch_bounds__(64) void kv4_compact_kernel(Compact4Args a) {
 
 }  // namespace
 
-hipError_t launch_append(int dt, bool four, const AppendArgs &a, hipStream_t st) {
-  int lph_log2 = 0;
-  const int chunks = a.head_dim / (dt == 0 ? 4 : 8);
-  while (1 << lph_log2 < chunks) ++lph_log2;
-  const int64_t threads = ((int64_t)(a.tok1 - a.tok0) * (a.n_q + 2 * a.n_kv)) << lph_log2;
-  const dim3 grid((uint32_t)((threads + kThreads - 1) / kThreads)), block(kThreads);
-  if (dt == 0 && four) hipLaunchKernelGGL((append_kernel<false, true>), grid, block, 0, st, a, lph_log2);
-  else if (dt == 0) hipLaunchKernelGGL((append_kernel<false, false>), grid, block, 0, st, a, lph_log2);
-  else if (four) hipLaunchKernelGGL((append_kernel<true, true>), grid, block, 0, st, a, lph_log2);
-  else hipLaunchKernelGGL((append_kernel<true, false>), grid, block, 0, st, a, lph_log2);
+namespace {
+
+template <bool BF16, bool FOUR>
+void append(AppendArgs &a, int cus, hipStream_t st) {
+  a.lph_log2 = a.q_log2 = a.kv_log2 = 0;
+  while ((BF16 ? 8 : 4) << a.lph_log2 < a.head_dim) ++a.lph_log2;
+  const int all = kThreads >> a.lph_log2, toks = a.tok1 - a.tok0;
+  const int heads = FOUR ? a.n_q : a.n_q + 2 * a.n_kv;      // in the inputs' type
+  while (1 << a.q_log2 < std::min(heads, all)) ++a.q_log2;
+  while (1 << a.kv_log2 < std::min(2 * a.n_kv, all)) ++a.kv_log2;
+  auto groups = [&](int log2) { return (uint32_t)((toks + (all >> log2) - 1) / (all >> log2)); };
+  const int turns = (heads + (1 << a.q_log2) - 1) >> a.q_log2;
+  a.kv_turns = (2 * a.n_kv + (1 << a.kv_log2) - 1) >> a.kv_log2;
+  a.four_blocks = FOUR ? groups(a.kv_log2) * a.kv_turns : 0;
+  // heads a slot: as many as leave every compute unit four blocks
+  const int64_t work = (int64_t)groups(a.q_log2) * turns;
+  const int hb = turns >= 4 && work >= 4 * 4 * cus ? 4 : turns >= 2 && work >= 2 * 4 * cus ? 2 : 1;
+  a.q_turns = std::max(1, (turns + hb - 1) / hb);
+  const dim3 grid(a.four_blocks + (heads > 0 ? groups(a.q_log2) * a.q_turns : 0)), block(kThreads);
+  if (hb == 4) hipLaunchKernelGGL((append_kernel<BF16, FOUR, 4>), grid, block, 0, st, a);
+  else if (hb == 2) hipLaunchKernelGGL((append_kernel<BF16, FOUR, 2>), grid, block, 0, st, a);
+  else hipLaunchKernelGGL((append_kernel<BF16, FOUR, 1>), grid, block, 0, st, a);
+}
+
+}  // namespace
+
+hipError_t launch_append(int dt, bool four, AppendArgs &a, int cus, hipStream_t st) {
+  if (dt == 0) four ? append<false, true>(a, cus, st) : append<false, false>(a, cus, st);
+  else four ? append<true, true>(a, cus, st) : append<true, false>(a, cus, st);
   return hipGetLastError();
 }
 
-hipError_t launch_kv4_read(int dt, const ReadArgs &a, hipStream_t st) {
-  const int64_t threads = (int64_t)(a.tok1 - a.tok0) * 2 * a.n_kv * (a.head_dim / 8);
-  const dim3 grid((uint32_t)((threads + kThreads - 1) / kThreads)), block(kThreads);
-  if (dt == 0) hipLaunchKernelGGL((kv4_read_kernel<false>), grid, block, 0, st, a);
-  else hipLaunchKernelGGL((kv4_read_kernel<true>), grid, block, 0, st, a);
+hipError_t launch_kv4_read(int dt, const ReadArgs &a, int cus, hipStream_t st) {
+  const int per = 2 * a.n_kv * (a.head_dim / 8), blocks = (per + kThreads - 1) / kThreads, toks = a.tok1 - a.tok0;
+  const bool many = (int64_t)blocks * toks >= 4 * 8 * cus;
+  const dim3 grid((uint32_t)blocks * (many ? (toks + 3) / 4 : toks)), block(kThreads);
+  if (dt == 0) {
+    if (many) hipLaunchKernelGGL((kv4_read_kernel<false, 4>), grid, block, 0, st, a, blocks);
+    else hipLaunchKernelGGL((kv4_read_kernel<false, 1>), grid, block, 0, st, a, blocks);
+  } else {
+    if (many) hipLaunchKernelGGL((kv4_read_kernel<true, 4>), grid, block, 0, st, a, blocks);
+    else hipLaunchKernelGGL((kv4_read_kernel<true, 1>), grid, block, 0, st, a, blocks);
+  }
   return hipGetLastError();
 }
 
