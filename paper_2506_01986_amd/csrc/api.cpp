@@ -1365,25 +1365,16 @@ int append_impl(int dt, int B, const int32_t *off, const specmemo_rows *x, int n
   if ((rc = check_kv(dt, kv, ti, off))) return rc;
   if ((rc = check_rows(dt, x, ti, n_q, kv, kv4, q_out))) return rc;
   AppendArgs a{};
-  a.q = x->q;
-  a.k = x->k;
-  a.v = x->v;
-  a.q_stride = x->q_stride;
-  a.k_stride = x->k_stride;
-  a.v_stride = x->v_stride;
-  a.q_norm = x->q_norm;
-  a.k_norm = x->k_norm;
+  a.kind[0] = AppendKind{x->q, x->q_norm, q_out, x->q_stride, n_q};
+  a.kind[1] = AppendKind{x->k, x->k_norm, kv->k, x->k_stride, kv->n_kv};
+  a.kind[2] = AppendKind{x->v, nullptr, kv->v, x->v_stride, kv->n_kv};
   a.eps = x->eps;
-  a.q_out = q_out;
-  a.pool_k = kv->k;
-  a.pool_v = kv->v;
   if (kv4) {
     a.ks = static_cast<uint8_t *>(kv4->k_scale);
     a.vs = static_cast<uint8_t *>(kv4->v_scale);
   }
   a.cap_total = kv->cap_total;
   a.n_q = n_q;
-  a.n_kv = kv->n_kv;
   a.head_dim = kv->head_dim;
   if (x->rot_dim > 0) {
     a.cos = x->cos;

@@ -256,22 +256,26 @@ void plan_walk(int dt, bool causal, const std::vector<WalkSeq> &seqs, int n_kv, 
 struct RowsSeq {
   int32_t off, row0_lo, row0_hi;
 };
-constexpr int kMaxRowsSeq = 310;   // sequences of a launch
+constexpr int kMaxRowsSeq = 300;   // sequences of a launch
+struct AppendKind {               // query, key or value heads
+  const void *in;                 // token i's heads at i * stride elements
+  const void *norm;               // [head_dim] or null
+  void *out;                      // [tokens][n_q][head_dim], or the pool's rows or codes
+  int64_t stride;
+  int32_t heads;
+  int32_t log2, turns;            // the launch's own split (append_kernel)
+  uint32_t block0;
+};
 struct AppendArgs {
-  const void *q, *k, *v;          // token i's heads at i * stride elements
-  int64_t q_stride, k_stride, v_stride;
-  const void *q_norm, *k_norm;    // [head_dim] or null
+  AppendKind kind[3];
   const float *cos, *sin;         // [n_pos][rot_dim / 2]
   const int32_t *pos;             // null: no rotation
-  void *q_out;                    // [tokens][n_q][head_dim]
-  void *pool_k, *pool_v;          // [n_kv][cap_total][head_dim], or codes
   uint8_t *ks, *vs;               // scale bytes of a 4-bit pool
   int64_t cap_total;
-  int32_t n_q, n_kv, head_dim, n_pos, rot_dim, pairs;
-  float eps;
+  int32_t n_q, head_dim, n_pos, rot_dim, pairs;
+  float eps, inv_d;
   int32_t tok0, tok1;             // tokens of this launch
-  int32_t lph_log2, q_log2, kv_log2, q_turns, kv_turns;   // the launch's own split (append_kernel)
-  uint32_t four_blocks;
+  int32_t lph_log2;               // lanes of a head
   int32_t nseq;
   RowsSeq seq[kMaxRowsSeq];
 };

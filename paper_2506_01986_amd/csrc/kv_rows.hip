@@ -44,8 +44,8 @@ __device__ __forceinline__ int64_t pool_row(const RowsSeq *seq, int nseq, int to
 }
 
 // The 16 bytes of a row that a lane has, as E numbers.
-template <typename T, int E>
-__device__ __forceinline__ void unpack(T (&x)[E], uint4 w) {
+template <int E>
+__device__ __forceinline__ void unpack(float (&x)[E], uint4 w) {
   const uint32_t u[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
   for (int i = 0; i < E; ++i) x[i] = E == 8 ? bf16_to_f32((uint16_t)(u[i >> 1] >> (16 * (i & 1)))) : __uint_as_float(u[i & 3]);
@@ -58,7 +58,6 @@ __device__ __forceinline__ float sticky_f32(double d) {
   const uint64_t cut = u & ~0x1FFFFFFFull;
   return (float)__longlong_as_double((long long)(cut | (u != cut ? 0x20000000ull : 0ull)));
 }
-__device__ __forceinline__ float sticky_f32(float f) { return f; }
 
 // Sum over the lph lanes of a head, in each of them: a row of 16 lanes by DPP, as in
 // wave_max.
@@ -148,13 +147,18 @@ struct Lane {
       }
     }
   }
-  // The columns that the lane's turn with, in its own columns' order.
-  __device__ __forceinline__ uint4 other(uint4 w, int lph) const {
-    if (pairs)
-      return E == 8 ? uint4{w.x >> 16 | w.x << 16, w.y >> 16 | w.y << 16, w.z >> 16 | w.z << 16, w.w >> 16 | w.w << 16} : uint4{w.y, w.x, w.w, w.z};
-    if (lph == 16 && half == 8 * E)       // the lane eight on in its row of 16
-      return uint4{(uint32_t)dpp_i<0x128>((int)w.x), (uint32_t)dpp_i<0x128>((int)w.y), (uint32_t)dpp_i<0x128>((int)w.z), (uint32_t)dpp_i<0x128>((int)w.w)};
-    return uint4{(uint32_t)__shfl((int)w.x, from), (uint32_t)__shfl((int)w.y, from), (uint32_t)__shfl((int)w.z, from), (uint32_t)__shfl((int)w.w, from)};
+  // The columns that the lane's turn with, in its own columns' order; x: the lane's own, w: as loaded.
+  __device__ __forceinline__ void other(float (&y)[E], const float (&x)[E], uint4 w, int lph) const {
+    if (pairs) {
+#pragma unroll
+      for (int i = 0; i < E; ++i) y[i] = x[i ^ 1];
+    } else if (lph == 16 && half == 8 * E) {       // of the lane eight on in its row of 16
+#pragma unroll
+      for (int i = 0; i < E; ++i) y[i] = dpp_f<0x128>(x[i]);
+    } else {
+      unpack(y, uint4{(uint32_t)__shfl((int)w.x, from), (uint32_t)__shfl((int)w.y, from), (uint32_t)__shfl((int)w.z, from),
+                      (uint32_t)__shfl((int)w.w, from)});
+    }
   }
   __device__ __forceinline__ void weights(float (&own)[E], float (&far)[E], const void *norm, int d) const {
     const uint4 x = ld16_or_zero(c < d, static_cast<const char *>(norm) + c * ES), y = ld16_or_zero(c < d, static_cast<const char *>(norm) + c2 * ES);
@@ -171,13 +175,13 @@ struct Lane {
   }
 };
 
-// The row's 1 / sqrt(mean of squares + eps).
+// The row's 1 / sqrt(mean of squares + eps); inv_d = 1 / d.
 template <typename T, int E>
-__device__ __forceinline__ T row_norm(const T (&x)[E], float eps, int d, int lph) {
+__device__ __forceinline__ T row_norm(const float (&x)[E], float eps, T inv_d, int lph) {
   T s = 0;
 #pragma unroll
-  for (int i = 0; i < E; ++i) s += x[i] * x[i];
-  return inv_sqrt(head_sum(s, lph) / T(d) + T(eps));
+  for (int i = 0; i < E; ++i) s += T(x[i]) * T(x[i]);
+  return inv_sqrt(fma(head_sum(s, lph), inv_d, T(eps)));
 }
 
 template <int E>
@@ -189,19 +193,19 @@ __device__ __forceinline__ void store_row(void *p, const float (&x)[E]) {
 }
 
 // Columns c .. of a row in 4 bits; the lanes of a group (32 / E of them) find its scale together.
-template <typename T, int E>
-__device__ __forceinline__ void store_row4(uint8_t *codes, uint8_t *scales, int c, const T (&x)[E], bool on) {
-  float y[E], top = 0.f;
+template <int E>
+__device__ __forceinline__ void store_row4(uint8_t *codes, uint8_t *scales, int c, const float (&y)[E], bool on) {
+  float top = 0.f;
   bool odd = false;
 #pragma unroll
   for (int i = 0; i < E; ++i) {
-    y[i] = sticky_f32(x[i]);
     top = fmaxf(top, fabsf(y[i]));
     odd |= !(fabsf(y[i]) < INFINITY);
   }
   top = odd ? INFINITY : top;
-#pragma unroll
-  for (int m = 1; m < kKv4Group / E; m <<= 1) top = fmaxf(top, __shfl_xor(top, m));
+  top = fmaxf(top, dpp_f<0xB1>(top));
+  top = fmaxf(top, dpp_f<0x4E>(top));
+  if (E == 4) top = fmaxf(top, dpp_f<0x141>(top));
   if (!on) return;
   const uint32_t byte = kv4_scale_byte(top);
   const float unit = kv4_scale(byte);
@@ -217,108 +221,97 @@ __device__ __forceinline__ void store_row4(uint8_t *codes, uint8_t *scales, int 
   if (c % kKv4Group == 0) scales[c / kKv4Group] = (uint8_t)byte;
 }
 
-// lph lanes have a head's row, and a block 256 / lph of them (slots).  The first four_blocks
-// blocks take the key and value heads that go to 4 bits, one a slot: keys in fp64, so
-// that a value next to a border between two codes falls on its own side of it.  The
-// others take the heads that stay in the inputs' type, HB a slot with their loads
-// together.  The slots take the heads of one token, or of several where a token has few
-// (1 << *_log2 slots each), so a lane loads cos, sin and the norm's weights once.
+// lph lanes have a head's row, and a block 256 / lph of them (slots).  A block has heads
+// of one kind (query, key, value), and its slots those of one token, or of several where
+// a token has few: 1 << log2 slots each, HB heads a slot with their loads together, so
+// that a lane loads cos, sin and the norm's weights once.  Rows that go to 4 bits: one a
+// slot, keys in fp64, so that a value next to a border between two codes falls on its
+// own side of it.
 template <bool BF16, bool FOUR, int HB>
 __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a) {
   constexpr int E = BF16 ? 8 : 4, ES = BF16 ? 2 : 4;
+  const int kind = (blockIdx.x >= a.kind[1].block0) + (blockIdx.x >= a.kind[2].block0);
+  const AppendKind K = a.kind[kind];
   const int lph = 1 << a.lph_log2, d = a.head_dim, all = kThreads >> a.lph_log2, slot = threadIdx.x >> a.lph_log2;
-  const int c = (threadIdx.x & (lph - 1)) * E;
-  if (!FOUR || blockIdx.x >= a.four_blocks) {
-    const uint32_t bid = blockIdx.x - a.four_blocks;
-    const int turn = (int)(bid % a.q_turns), slots = 1 << a.q_log2;
-    const int at = a.tok0 + (int)(bid / a.q_turns) * (all >> a.q_log2) + (slot >> a.q_log2), tok = min(at, a.tok1 - 1);
-    const int h0 = (slot & (slots - 1)) + turn * HB * slots, heads = FOUR ? a.n_q : a.n_q + 2 * a.n_kv;
-    const bool on = at < a.tok1;
+  const int c = (threadIdx.x & (lph - 1)) * E, slots = 1 << K.log2;
+  const uint32_t bid = blockIdx.x - K.block0, group = bid / (uint32_t)K.turns;
+  const int at = a.tok0 + (int)group * (all >> K.log2) + (slot >> K.log2), tok = min(at, a.tok1 - 1);
+  const int hb = FOUR && kind != 0 ? 1 : HB;
+  const int h0 = (slot & (slots - 1)) + (int)(bid - group * K.turns) * hb * slots;
+  const bool on = at < a.tok1, has = on && c < d;
+  const char *const src = static_cast<const char *>(K.in) + (K.stride * tok + (int64_t)h0 * d + c) * ES;
+  const int step = slots * d * ES;
+  if (!FOUR || kind == 0) {
     uint4 row[HB];
 #pragma unroll
-    for (int n = 0; n < HB; ++n) {
-      const int head = h0 + n * slots;
-      const bool q = FOUR || head < a.n_q, k = head < a.n_q + a.n_kv;
-      const char *base = static_cast<const char *>(q ? a.q : k ? a.k : a.v);
-      const int64_t off = (q ? a.q_stride : k ? a.k_stride : a.v_stride) * tok + (int64_t)(q ? head : k ? head - a.n_q : head - a.n_q - a.n_kv) * d + c;
-      row[n] = ld16_or_zero(on && c < d && head < heads, base + off * ES);
-    }
+    for (int n = 0; n < HB; ++n) row[n] = ld16_or_zero(has && h0 + n * slots < K.heads, src + (int64_t)n * step);
     const Lane<E> l(a, lph, tok, on);
-    float co[E], si[E], qx[E], qy[E], kx[E], ky[E];
-    l.angles(a, co, si);
-    auto factors = [&](float (&fx)[E], float (&fy)[E], const void *norm) __attribute__((always_inline)) {
-      if (norm) l.weights(fx, fy, norm, d);
+    char *dst;
+    int64_t out_step;
+    if (kind == 0) {
+      dst = static_cast<char *>(K.out) + (((int64_t)tok * a.n_q + h0) * d + c) * ES;
+      out_step = step;
+    } else {
+      dst = static_cast<char *>(K.out) + ((h0 * a.cap_total + pool_row(a.seq, a.nseq, tok)) * d + c) * ES;
+      out_step = a.cap_total * step;
+    }
+    if (kind == 2) {
+#pragma unroll
+      for (int n = 0; n < HB; ++n)
+        if (l.live && h0 + n * slots < K.heads) *reinterpret_cast<uint4 *>(dst + n * out_step) = row[n];
+      return;
+    }
+    float fx[E], fy[E];
+    l.angles(a, fx, fy);
+    if (K.norm) {
+      float wx[E], wy[E];
+      l.weights(wx, wy, K.norm, d);
 #pragma unroll
       for (int i = 0; i < E; ++i) {
-        fx[i] = norm ? fx[i] * co[i] : co[i];
-        fy[i] = norm ? fy[i] * si[i] : si[i];
+        fx[i] *= wx[i];
+        fy[i] *= wy[i];
       }
-    };
-    factors(qx, qy, a.q_norm);
-    if (!FOUR) factors(kx, ky, a.k_norm);
-    const int64_t prow = FOUR ? 0 : pool_row(a.seq, a.nseq, tok);
+    }
 #pragma unroll
     for (int n = 0; n < HB; ++n) {
-      const int head = h0 + n * slots;
-      const bool put = l.live && head < heads;
-      // The slots of a wave may hold heads of different kinds; the lanes of one head agree.
-      auto turn_row = [&](char *dst, const float (&fx)[E], const float (&fy)[E], bool norm) __attribute__((always_inline)) {
-        float x[E], y[E];
-        unpack(x, row[n]);
-        unpack(y, l.other(row[n], lph));
-        const float r = norm ? row_norm(x, a.eps, d, lph) : 1.f;
+      float x[E], y[E];
+      unpack(x, row[n]);
+      l.other(y, x, row[n], lph);
+      const float r = K.norm ? row_norm(x, a.eps, a.inv_d, lph) : 1.f;
 #pragma unroll
-        for (int i = 0; i < E; ++i) {
-          x[i] *= fx[i];
-          if (l.turns) x[i] = fmaf(y[i], fy[i], x[i]);
-          if (norm) x[i] *= r;
-        }
-        if (put) store_row(dst, x);
-      };
-      if (FOUR || head < a.n_q) {
-        turn_row(static_cast<char *>(a.q_out) + (((int64_t)tok * a.n_q + head) * d + c) * ES, qx, qy, a.q_norm != nullptr);
-      } else if (head < a.n_q + a.n_kv) {
-        turn_row(static_cast<char *>(a.pool_k) + (((head - a.n_q) * a.cap_total + prow) * d + c) * ES, kx, ky, a.k_norm != nullptr);
-      } else if (put) {
-        *reinterpret_cast<uint4 *>(static_cast<char *>(a.pool_v) + (((head - a.n_q - a.n_kv) * a.cap_total + prow) * d + c) * ES) = row[n];
+      for (int i = 0; i < E; ++i) {
+        x[i] *= fx[i];
+        if (l.turns) x[i] = fmaf(y[i], fy[i], x[i]);
+        if (K.norm) x[i] *= r;
       }
+      if (l.live && h0 + n * slots < K.heads) store_row(dst + n * out_step, x);
     }
     return;
   }
-  const int turn = (int)(blockIdx.x % a.kv_turns), slots = 1 << a.kv_log2;
-  const int at = a.tok0 + (int)(blockIdx.x / a.kv_turns) * (all >> a.kv_log2) + (slot >> a.kv_log2), tok = min(at, a.tok1 - 1);
-  const int head = (slot & (slots - 1)) + turn * slots;
-  const bool on = at < a.tok1 && head < 2 * a.n_kv, k = head < a.n_kv;
-  const int hk = k ? head : head - a.n_kv;
-  const uint4 row = ld16_or_zero(on && c < d, static_cast<const char *>(k ? a.k : a.v) + ((k ? a.k_stride : a.v_stride) * tok + (int64_t)hk * d + c) * ES);
+  const uint4 row = ld16_or_zero(has && h0 < K.heads, src);
   const Lane<E> l(a, lph, tok, on);
-  const int64_t r = (int64_t)hk * a.cap_total + pool_row(a.seq, a.nseq, tok);
-  // A wave may hold keys and values; the lanes of one head agree.
-  if (k) {
-    float co[E], si[E], wx[E], wy[E];
-    l.angles(a, co, si);
-    if (a.k_norm) l.weights(wx, wy, a.k_norm, d);
-    double x[E], y[E];
-    unpack(x, row);
-    unpack(y, l.other(row, lph));
-    if (a.k_norm) {
-      const double n = row_norm(x, a.eps, d, lph);
-#pragma unroll
-      for (int i = 0; i < E; ++i) {
-        x[i] *= n * wx[i];
-        y[i] *= n * wy[i];
-      }
-    }
-    if (l.turns) {
-#pragma unroll
-      for (int i = 0; i < E; ++i) x[i] = x[i] * co[i] + y[i] * si[i];
-    }
-    store_row4(static_cast<uint8_t *>(a.pool_k) + r * (d / 2), a.ks + r * (d / kKv4Group), c, x, l.live);
-  } else {
-    float x[E];
-    unpack(x, row);
-    store_row4(static_cast<uint8_t *>(a.pool_v) + r * (d / 2), a.vs + r * (d / kKv4Group), c, x, l.live);
+  const bool put = l.live && h0 < K.heads;
+  const int64_t r = h0 * a.cap_total + pool_row(a.seq, a.nseq, tok);
+  float v[E];
+  unpack(v, row);
+  if (kind == 2) {
+    store_row4(static_cast<uint8_t *>(K.out) + r * (d / 2), a.vs + r * (d / kKv4Group), c, v, put);
+    return;
   }
+  float co[E], si[E], wx[E], wy[E];
+  l.angles(a, co, si);
+  if (K.norm) l.weights(wx, wy, K.norm, d);
+  float y[E];
+  l.other(y, v, row, lph);
+  const double n = K.norm ? row_norm(v, a.eps, 1.0 / d, lph) : 1.0;
+#pragma unroll
+  for (int i = 0; i < E; ++i) {
+    double x = v[i];
+    if (K.norm) x *= n * wx[i];
+    if (l.turns) x = x * co[i] + (K.norm ? y[i] * (n * wy[i]) : (double)y[i]) * si[i];
+    v[i] = sticky_f32(x);
+  }
+  store_row4(static_cast<uint8_t *>(K.out) + r * (d / 2), a.ks + r * (d / kKv4Group), c, v, put);
 }
 
 // Rows of a 4-bit pool as values: a thread has eight columns of one head of K or V and
@@ -411,24 +404,33 @@ namespace {
 
 template <bool BF16, bool FOUR>
 void append(AppendArgs &a, int cus, hipStream_t st) {
-  a.lph_log2 = a.q_log2 = a.kv_log2 = 0;
+  a.lph_log2 = 0;
   while ((BF16 ? 8 : 4) << a.lph_log2 < a.head_dim) ++a.lph_log2;
+  a.inv_d = 1.f / (float)a.head_dim;
   const int all = kThreads >> a.lph_log2, toks = a.tok1 - a.tok0;
-  const int heads = FOUR ? a.n_q : a.n_q + 2 * a.n_kv;      // in the inputs' type
-  while (1 << a.q_log2 < std::min(heads, all)) ++a.q_log2;
-  while (1 << a.kv_log2 < std::min(2 * a.n_kv, all)) ++a.kv_log2;
-  auto groups = [&](int log2) { return (uint32_t)((toks + (all >> log2) - 1) / (all >> log2)); };
-  const int turns = (heads + (1 << a.q_log2) - 1) >> a.q_log2;
-  a.kv_turns = (2 * a.n_kv + (1 << a.kv_log2) - 1) >> a.kv_log2;
-  a.four_blocks = FOUR ? groups(a.kv_log2) * a.kv_turns : 0;
-  // heads a slot: as many as leave every compute unit four blocks
-  const int64_t work = (int64_t)groups(a.q_log2) * turns;
-  const int hb = turns >= 4 && work >= 4 * 4 * cus ? 4 : turns >= 2 && work >= 2 * 4 * cus ? 2 : 1;
-  a.q_turns = std::max(1, (turns + hb - 1) / hb);
-  const dim3 grid(a.four_blocks + (heads > 0 ? groups(a.q_log2) * a.q_turns : 0)), block(kThreads);
-  if (hb == 4) hipLaunchKernelGGL((append_kernel<BF16, FOUR, 4>), grid, block, 0, st, a);
-  else if (hb == 2) hipLaunchKernelGGL((append_kernel<BF16, FOUR, 2>), grid, block, 0, st, a);
-  else hipLaunchKernelGGL((append_kernel<BF16, FOUR, 1>), grid, block, 0, st, a);
+  // heads a slot: as many as there are, and as leave every compute unit four blocks
+  int64_t slots = 0;
+  int most = 1;
+  for (AppendKind &k : a.kind) {
+    k.log2 = 0;
+    while (1 << k.log2 < std::min(k.heads, all)) ++k.log2;
+    most = std::max(most, (k.heads + (1 << k.log2) - 1) >> k.log2);
+    slots += (int64_t)toks * k.heads;
+  }
+  const int64_t blocks = slots / all;
+  const int hb = most >= 4 && blocks >= 4 * 4 * cus ? 4 : most >= 2 && blocks >= 2 * 4 * cus ? 2 : 1;
+  uint32_t block = 0;
+  for (int i = 0; i < 3; ++i) {
+    AppendKind &k = a.kind[i];
+    const int per = (FOUR && i != 0 ? 1 : hb) << k.log2;
+    k.turns = std::max(1, (k.heads + per - 1) / per);
+    k.block0 = block;
+    if (k.heads > 0) block += (uint32_t)((toks + (all >> k.log2) - 1) / (all >> k.log2)) * k.turns;
+  }
+  const dim3 grid(block), threads(kThreads);
+  if (hb == 4) hipLaunchKernelGGL((append_kernel<BF16, FOUR, 4>), grid, threads, 0, st, a);
+  else if (hb == 2) hipLaunchKernelGGL((append_kernel<BF16, FOUR, 2>), grid, threads, 0, st, a);
+  else hipLaunchKernelGGL((append_kernel<BF16, FOUR, 1>), grid, threads, 0, st, a);
 }
 
 }  // namespace
