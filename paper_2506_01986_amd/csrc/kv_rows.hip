@@ -184,12 +184,17 @@ __device__ __forceinline__ T row_norm(const float (&x)[E], float eps, T inv_d, i
   return inv_sqrt(fma(head_sum(s, lph), inv_d, T(eps)));
 }
 
+// 16 bytes past the caches' own rules: what reads them next runs on all XCDs, behind
+// other L2s, and the end of the kernel has nothing to write back (1024 rows of 32 + 32 +
+// 32 heads 12.0 us as ordinary stores, 9.3).
+__device__ __forceinline__ void store16(void *p, uint32_t x, uint32_t y, uint32_t z, uint32_t w) {
+  typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+  __builtin_nontemporal_store(u32x4{x, y, z, w}, static_cast<u32x4 *>(p));
+}
 template <int E>
 __device__ __forceinline__ void store_row(void *p, const float (&x)[E]) {
-  if constexpr (E == 8)
-    *static_cast<uint4 *>(p) = uint4{pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7])};
-  else
-    *static_cast<f32x4 *>(p) = f32x4{x[0], x[1], x[2], x[3]};
+  if constexpr (E == 8) store16(p, pack_bf16x2(x[0], x[1]), pack_bf16x2(x[2], x[3]), pack_bf16x2(x[4], x[5]), pack_bf16x2(x[6], x[7]));
+  else store16(p, __float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3]));
 }
 
 // Columns c .. of a row in 4 bits; the lanes of a group (32 / E of them) find its scale together.
@@ -258,7 +263,7 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a) {
     if (kind == 2) {
 #pragma unroll
       for (int n = 0; n < HB; ++n)
-        if (l.live && h0 + n * slots < K.heads) *reinterpret_cast<uint4 *>(dst + n * out_step) = row[n];
+        if (l.live && h0 + n * slots < K.heads) store16(dst + n * out_step, row[n].x, row[n].y, row[n].z, row[n].w);
       return;
     }
     float fx[E], fy[E];
@@ -341,16 +346,20 @@ __global__ __launch_bounds__(kThreads) void kv4_read_kernel(ReadArgs a, int bloc
   for (int n = 0; n < TB; ++n) {
     if (tok0 + n >= a.tok1) return;
     const bool nan = byte[n] == kKv4Nan;
-    const float unit = nan ? __uint_as_float(0x7FC00000u) : kv4_scale(byte[n]);
+    const float unit = kv4_scale(byte[n]);
     const int64_t o = ((int64_t)(tok0 + n) * a.n_kv + hk) * d + 8 * c;
-    if (BF16) {
-      *reinterpret_cast<uint4 *>(static_cast<uint16_t *>(v ? a.v_out : a.k_out) + o) =
-          nan ? uint4{0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u, 0x7FC07FC0u} : kv4_bf16x8(w[n], unit);
+    void *const out = v ? a.v_out : a.k_out;
+    if constexpr (BF16) {
+      const uint4 y = kv4_bf16x8(w[n], unit);
+      constexpr uint32_t q = 0x7FC07FC0u;
+      store16(static_cast<uint16_t *>(out) + o, nan ? q : y.x, nan ? q : y.y, nan ? q : y.z, nan ? q : y.w);
     } else {
-      const f32x2_t p0 = kv4_f32x2<0>(w[n], unit), p1 = kv4_f32x2<1>(w[n], unit), p2 = kv4_f32x2<2>(w[n], unit), p3 = kv4_f32x2<3>(w[n], unit);
-      f32x4 *dst = reinterpret_cast<f32x4 *>(static_cast<float *>(v ? a.v_out : a.k_out) + o);
-      dst[0] = nan ? f32x4{unit, unit, unit, unit} : f32x4{p0[0], p0[1], p1[0], p1[1]};
-      dst[1] = nan ? f32x4{unit, unit, unit, unit} : f32x4{p2[0], p2[1], p3[0], p3[1]};
+      const f32x2_t p[4] = {kv4_f32x2<0>(w[n], unit), kv4_f32x2<1>(w[n], unit), kv4_f32x2<2>(w[n], unit), kv4_f32x2<3>(w[n], unit)};
+      float y[2][4];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) y[i >> 2][i & 3] = nan ? __uint_as_float(0x7FC00000u) : p[i >> 1][i & 1];
+      store_row(static_cast<float *>(out) + o, y[0]);
+      store_row(static_cast<float *>(out) + o + 4, y[1]);
     }
   }
 }
