@@ -514,9 +514,16 @@ class KV4Pool:
         self.seq_len_h = _i32(seq_len)
 
     def struct(self) -> _KV4:
+        x, y, z = self.seq_base_h, self.seq_cap_h, self.seq_len_h
+        if type(x) is type(y) is type(z) is _ndarray:
+            try:       # as KVPool (1.6 us, 2.6 through the general form)
+                return _KV4(self.k.data_ptr(), self.v.data_ptr(), self.k_scale.data_ptr(), self.v_scale.data_ptr(),
+                            self.cap_total, self.n_kv, self.head_dim, self.seq_len.data_ptr(), _addressof(_from_buffer(x)),
+                            _addressof(_from_buffer(y)), _addressof(_from_buffer(z)))
+            except (AttributeError, TypeError, ValueError, BufferError):
+                pass
         return _KV4(_ptr(self.k), _ptr(self.v), _ptr(self.k_scale), _ptr(self.v_scale), self.cap_total, self.n_kv,
-                    self.head_dim, _ptr(self.seq_len), _host_addr(self.seq_base_h), _host_addr(self.seq_cap_h),
-                    _host_addr(self.seq_len_h))
+                    self.head_dim, _ptr(self.seq_len), _host_addr(x), _host_addr(y), _host_addr(z))
 
 
 _VALUES = ("torch.float32", "torch.bfloat16")
@@ -564,31 +571,52 @@ class QKVRows:
         self.q, self.k, self.v, self.pos, self.cos, self.sin = q, k, v, pos, cos, sin
         self.q_norm, self.k_norm, self.eps = q_norm, k_norm, eps
         self.tokens, self.n_q, self.n_kv, self.head_dim = int(k.shape[0]), 0 if q is None else int(q.shape[1]), int(k.shape[1]), d
-        self.rot_dim, self.rot_style, self.n_pos = rot_dim, rot_style, n_pos
-
-    def _stride(self, x) -> int:
-        return 0 if x is None else int(x.stride(0)) if self.tokens > 1 else int(x.shape[1]) * self.head_dim
+        self.rot_dim, self.rot_style, self.n_pos, self.dt = rot_dim, rot_style, n_pos, _VALUES.index(str(k.dtype))
+        stride = lambda x: 0 if x is None else int(x.stride(0)) if self.tokens > 1 else int(x.shape[1]) * d
+        self._layout = stride(q), stride(k), stride(v)
 
     def struct(self) -> _Rows:
-        return _Rows(_ptr(self.q), _ptr(self.k), _ptr(self.v), self._stride(self.q), self._stride(self.k), self._stride(self.v),
-                     _ptr(self.q_norm), _ptr(self.k_norm), self.eps, _ptr(self.cos), _ptr(self.sin), _ptr(self.pos), self.n_pos,
-                     self.rot_dim, self.rot_style)
+        at = lambda x: None if x is None else x.data_ptr()
+        return _Rows(at(self.q), self.k.data_ptr(), self.v.data_ptr(), *self._layout, at(self.q_norm), at(self.k_norm),
+                     self.eps, at(self.cos), at(self.sin), at(self.pos), self.n_pos, self.rot_dim, self.rot_style)
+
+
+def _offsets(new_off) -> np.ndarray:
+    """Host offsets as an int32 array (arrays of that kind as they are: 0.1 us, 0.5 through numpy's conversions)."""
+    if type(new_off) is _ndarray and new_off.dtype is _I32 and new_off.ndim == 1 and new_off.flags.c_contiguous:
+        return new_off
+    return _i32(new_off)
+
+
+_I32 = np.dtype(np.int32)
+
+
+def _out_tensor(name: str, x, dtype, values: int):
+    if x.dtype is not dtype or x.numel() != values or not x.is_contiguous():
+        raise ValueError(f"{name}: {values} values of {dtype} without gaps expected, got {tuple(x.shape)} of {x.dtype}")
 
 
 def _append(fn, dt: int, new_off, rows: QKVRows, kv, q_out, stream):
-    off, ks, rs = _new_off(new_off, kv), kv.struct(), rows.struct()
-    if int(off[-1]) != rows.tokens or rows.n_kv != kv.n_kv or rows.head_dim != kv.head_dim:
-        raise ValueError(f"{rows.tokens} tokens of {rows.n_kv} KV heads of {rows.head_dim} for {int(off[-1])} tokens and a pool "
-                         f"of {kv.n_kv} heads of {kv.head_dim}")
-    if str(rows.k.dtype) != _VALUES[dt]:
-        raise ValueError(f"rows of {rows.k.dtype} for type {dt}")
-    _check_tensor("q_out", q_out, (_VALUES[dt],))
-    if hasattr(q_out, "numel") and q_out.numel() != rows.tokens * rows.n_q * rows.head_dim:
-        raise ValueError(f"q_out of {q_out.numel()} values for {rows.tokens} tokens of {rows.n_q} heads")
-    _check(fn(dt, len(off) - 1, _host_addr(off), C.byref(rs), rows.n_q, C.byref(ks), _ptr(q_out), _stream(stream)))
+    off = _offsets(new_off)
+    B, tokens = len(off) - 1, rows.tokens
+    if B < 0 or len(kv.seq_len_h) < B or len(kv.seq_base_h) < B or len(kv.seq_cap_h) < B:
+        raise ValueError(f"new_off of {off.shape} for a pool of {len(kv.seq_base_h)} sequences")
+    if off[B] != tokens or rows.n_kv != kv.n_kv or rows.head_dim != kv.head_dim or rows.dt != dt:
+        raise ValueError(f"{tokens} tokens of {rows.n_kv} KV heads of {rows.head_dim}, type {rows.dt}, for {off[B]} tokens and a "
+                         f"pool of {kv.n_kv} heads of {kv.head_dim}, type {dt}")
+    if q_out is None:
+        if rows.n_q and tokens:
+            raise ValueError("q_out is missing")
+    else:
+        _out_tensor("q_out", q_out, rows.k.dtype, tokens * rows.n_q * rows.head_dim)
+    _check(fn(dt, B, _host_addr(off), C.byref(rows.struct()), rows.n_q, C.byref(kv.struct()),
+              None if q_out is None else q_out.data_ptr(), _stream(stream)))
 
 
 def kv_append(dt: int, new_off, rows: QKVRows, kv: KVPool, q_out, stream=None):
+    for x in (kv.k, kv.v):      # written in the rows' type, as they lie
+        if x.dtype is not rows.k.dtype or not x.is_contiguous():
+            raise ValueError(f"a pool of {rows.k.dtype} without gaps expected, got {x.dtype} of strides {x.stride()}")
     _append(load().specmemo_kv_append, dt, new_off, rows, kv, q_out, stream)
 
 
@@ -597,12 +625,17 @@ def kv4_append(dt: int, new_off, rows: QKVRows, kv: KV4Pool, q_out, stream=None)
 
 
 def kv4_read(dt: int, new_off, kv: KV4Pool, k_out, v_out, stream=None):
-    off, ks = _new_off(new_off, kv), kv.struct()
-    for name, x in (("k_out", k_out), ("v_out", v_out)):
-        _check_tensor(name, x, (_VALUES[dt],))
-        if hasattr(x, "numel") and x.numel() != int(off[-1]) * kv.n_kv * kv.head_dim:
-            raise ValueError(f"{name} of {x.numel()} values for {int(off[-1])} tokens")
-    _check(load().specmemo_kv4_read(dt, len(off) - 1, _host_addr(off), C.byref(ks), _ptr(k_out), _ptr(v_out), _stream(stream)))
+    off = _offsets(new_off)
+    B = len(off) - 1
+    if B < 0 or len(kv.seq_len_h) < B or len(kv.seq_base_h) < B or len(kv.seq_cap_h) < B:
+        raise ValueError(f"new_off of {off.shape} for a pool of {len(kv.seq_base_h)} sequences")
+    if str(k_out.dtype) != _VALUES[dt]:
+        raise ValueError(f"outputs of {k_out.dtype} for type {dt}")
+    values = int(off[B]) * kv.n_kv * kv.head_dim
+    _out_tensor("k_out", k_out, k_out.dtype, values)
+    _out_tensor("v_out", v_out, k_out.dtype, values)
+    _check(load().specmemo_kv4_read(dt, B, _host_addr(off), C.byref(kv.struct()), k_out.data_ptr(), v_out.data_ptr(),
+                                    _stream(stream)))
 
 
 def kv4_prompt_attn_bytes(dt: int, new_off, kv: KV4Pool, n_q: int, prefix: Optional[Prefix] = None) -> int:
