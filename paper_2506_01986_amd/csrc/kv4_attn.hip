@@ -203,11 +203,9 @@ __device__ __forceinline__ void walk4(const WalkArgs &a, const WalkItem &it, uin
   const int sb0 = ksb * NSB;
   WalkAcc A;
 
-  auto work = [&](const uint8_t *ks, const uint8_t *vs, const uint32_t (&ksc)[NSB], int j) __attribute__((always_inline)) {
-    const bool pre = j < np;
-    const int kt = (pre ? j : j - np) * TK;
-    if (!pre && !TREE && kt + 32 * sb0 > lim_hi) return;   // past every row of the wave
-    f32x16 Sc[NSB];
+  // Scores of tile j, and whether the wave has rows that see any of its keys.
+  auto sees = [&](int j) __attribute__((always_inline)) { return wave_rows && (TREE || j < np || (j - np) * TK + 32 * sb0 <= lim_hi); };
+  auto scores = [&](f32x16 (&Sc)[NSB], const uint8_t *ks, const uint32_t (&ksc)[NSB]) __attribute__((always_inline)) {
     uint4 kf[NSB][2];
 #pragma unroll
     for (int sb = 0; sb < NSB; ++sb)
@@ -225,27 +223,51 @@ __device__ __forceinline__ void walk4(const WalkArgs &a, const WalkItem &it, uin
       Sc[sb] = qk_part<0, 0>(kf[sb][0], Q, Sc[sb], sc);
       Sc[sb] = qk_part<1, 0>(kf[sb][1], Q, Sc[sb], sc);
     }
-    walk_mask<NSB, TREE>(Sc, M, pre, kt, pre ? P : kend, 32 * sb0);
-    walk_softmax_pv<NSB>(Sc, A, vs + 32 * sb0 * (D * 2), vro, a.scale_log2);
   };
 
-  // Iteration j waits for tile j's loads; after its barrier every wave is done with
-  // tile j - 1, whose slots take tile j + 1: K's codes by direct loads, V's from the
-  // registers that they were loaded to an iteration ago.
-  auto tile = [&](int j, auto slot_c) __attribute__((always_inline)) {
-    constexpr int slot = decltype(slot_c)::value;
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    ring_barrier();
-    uint32_t ksc[NSB];
+  // Iteration j waits for its loads; after its barrier every wave is done with V of tile
+  // j - 1, whose slot takes V of tile j + 1 from the registers that it was loaded to an
+  // iteration ago.
+  // AHEAD: tile j's scores were made an iteration ago, and tile j + 1's are made beside
+  // tile j's weights; K's codes are loaded two tiles ahead.
+  constexpr bool AHEAD = KSPLIT == 2;
+  f32x16 Sc[AHEAD ? 2 : 1][NSB];
+  uint32_t ksc[NSB];
+  auto next_k = [&](int slot, int j) __attribute__((always_inline)) {      // K of tile j, the next one; its scales become current
 #pragma unroll
     for (int sb = 0; sb < NSB; ++sb) ksc[sb] = ksn[sb];
-    if (j + 1 < j1) {
-      issue_k(kring[slot ^ 1], j + 1);
-      load_ks(ksn, j + 1);
-      store_v(raw, vring[slot ^ 1]);
-      if (j + 2 < j1) load_v(raw, j + 2);
+    if (j < j1) {
+      issue_k(kring[slot], j);
+      load_ks(ksn, j);
     }
-    if (wave_rows) work(kring[slot], vring[slot], ksc, j);
+  };
+  if constexpr (AHEAD) {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    ring_barrier();
+    next_k(1, j0 + 1);
+    scores(Sc[0], kring[0], ksc);
+  }
+  auto tile = [&](int j, auto slot_c) __attribute__((always_inline)) {
+    constexpr int slot = decltype(slot_c)::value, cur = AHEAD ? slot : 0;
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    ring_barrier();
+    const bool more = j + 1 < j1, pre = j < np, now = sees(j);     // (if not now, at no later tile)
+    next_k(AHEAD ? slot : slot ^ 1, AHEAD ? j + 2 : j + 1);
+    auto put_v = [&]() __attribute__((always_inline)) {
+      if (more) store_v(raw, vring[slot ^ 1]);
+      if (j + 2 < j1) load_v(raw, j + 2);
+    };
+    if (!AHEAD) put_v();
+    uint32_t pk[2 * NSB][4];
+    if (now) {
+      if (!AHEAD) scores(Sc[cur], kring[slot], ksc);
+      walk_mask<NSB, TREE>(Sc[cur], M, pre, (pre ? j : j - np) * TK, pre ? P : kend, 32 * sb0);
+      walk_max<NSB>(Sc[cur], A, a.scale_log2);
+      if constexpr (AHEAD) scores(Sc[cur ^ 1], kring[slot ^ 1], ksc);        // after the last tile: of what the slot held, unused
+      walk_weights<NSB>(Sc[cur], A, a.scale_log2, pk);
+    }
+    if (AHEAD) put_v();
+    if (now) walk_pv<NSB>(pk, A, vring[slot] + 32 * sb0 * (D * 2), vro);
   };
   for (int j = j0; j < j1; j += 2) {
     tile(j, std::integral_constant<int, 0>{});
@@ -489,7 +511,9 @@ __global__ __launch_bounds__(kWaves4 * 64, 2) void walk4_attn_bf16(WalkArgs a) {
 // fp32 queries: the arrangement of the fp32 attention over rows of 32 bits (32 query
 // rows a block on the 32x32x2 product, the waves taking 32-key tiles in turn, merged
 // through LDS), with the rows converted to fp32 as they are read.  DB: 32-column
-// groups of the head; lane half h contracts columns 16 DB h .. + 16 DB - 1.
+// groups of the head; lane half h contracts columns 16 DB h .. + 16 DB - 1.  A lane's
+// rows of O^T are columns DB r .. + DB - 1 (r = lane % 32, one of each block i), so that
+// a key's V takes one load of a lane and not DB.
 constexpr int kF32Waves = 4;
 
 template <int DB, bool TREE>
@@ -531,6 +555,9 @@ __global__ __launch_bounds__(64 * kF32Waves, 2) void walk4_attn_f32(WalkArgs a) 
     if (tree) M.root_path(par, node);
   }
 
+  // the lane's columns: their first byte and place in it, their groups, the last of the first group
+  const int col = DB * (lane & 31), vbyte = col >> 1, vshift = 4 * (col & 1), vgroup = col >> 5, vlast = (col + DB - 1) >> 5;
+  const int vsplit = 31 - (col & 31);
   float m = -INFINITY, l = 0.f;
   f32x16 O[DB];
 #pragma unroll
@@ -550,16 +577,15 @@ __global__ __launch_bounds__(64 * kF32Waves, 2) void walk4_attn_f32(WalkArgs a) 
       kc[i] = *reinterpret_cast<const uint2 *>(K0 + kr * (DD / 2) + 8 * (DB * h + i));
       ksc[i] = a.ks[kr * DB + ((DB * h + i) >> 1)];
     }
-    uint32_t vc[VR][DB], vsc[VR][DB];                // a column's byte of key rows, and its scale
+    uint32_t vc[VR], vs0[VR], vs1[VR];               // a lane's columns' codes of key rows, and the scales of the first and last
     auto load_v = [&](int r0) __attribute__((always_inline)) {
 #pragma unroll
       for (int r = 0; r < VR; ++r) {
         const int64_t vr = base + min(kt + 8 * ((r0 + r) >> 2) + 4 * h + ((r0 + r) & 3), end - 1);
-#pragma unroll
-        for (int i = 0; i < DB; ++i) {
-          vc[r][i] = V0[vr * (DD / 2) + 16 * i + ((lane & 31) >> 1)];
-          vsc[r][i] = a.vs[vr * DB + i];
-        }
+        const uint8_t *p = V0 + vr * (DD / 2) + vbyte, *ps = a.vs + vr * DB;
+        vc[r] = DB == 4 ? *reinterpret_cast<const uint16_t *>(p) : DB == 3 ? p[0] | (uint32_t)p[1] << 8 : p[0];
+        vs0[r] = ps[vgroup];
+        vs1[r] = DB == 3 ? ps[vlast] : vs0[r];
       }
     };
     if (VR == 16) load_v(0);
@@ -600,12 +626,14 @@ __global__ __launch_bounds__(64 * kF32Waves, 2) void walk4_attn_f32(WalkArgs a) 
       for (int r = 0; r < VR; ++r)
 #pragma unroll
         for (int i = 0; i < DB; ++i) {
-          const f32x2_t v = kv4_f32x2<0>(vc[r][i], kv4_scale(vsc[r][i]));
-          O[i] = __builtin_amdgcn_mfma_f32_32x32x2f32(lane & 1 ? v[1] : v[0], Sc[0][r0 + r], O[i], 0, 0, 0);
+          const uint32_t w = vc[r] >> vshift;
+          const float unit = kv4_scale(DB == 3 && i > vsplit ? vs1[r] : vs0[r]);
+          const f32x2_t v = i < 2 ? kv4_f32x2<0>(w, unit) : kv4_f32x2<1>(w, unit);
+          O[i] = __builtin_amdgcn_mfma_f32_32x32x2f32(v[i & 1], Sc[0][r0 + r], O[i], 0, 0, 0);
         }
     }
   }
-  walk_finish_f32<DB, W>(a, it, O, m, l, row_ok, node, hq, merge);
+  walk_finish_f32<DB, W, true>(a, it, O, m, l, row_ok, node, hq, merge);
 }
 
 template <int DB, bool TREE>

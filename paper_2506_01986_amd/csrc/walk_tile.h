@@ -75,12 +75,10 @@ __device__ __forceinline__ void walk_v_offsets(int (&vro)[kAttnHeadDim / 32]) {
   for (int i = 0; i < kAttnHeadDim / 32; ++i) vro[i] = (4 * h + tj) * (kAttnHeadDim * 2) + 64 * (i ^ tj) + 16 * te + 8 * (tq & 1);
 }
 
-// The softmax weights of NSB x 32 keys and their product with V; vs: V row of the first of them.
+// The running maximum after NSB x 32 scores of every row.
 template <int NSB>
-__device__ __forceinline__ void walk_softmax_pv(f32x16 (&Sc)[NSB], WalkAcc &A, const uint8_t *vs, const int (&vro)[kAttnHeadDim / 32],
-                                                float scale_log2) {
+__device__ __forceinline__ void walk_max(const f32x16 (&Sc)[NSB], WalkAcc &A, float scale_log2) {
   constexpr int D = kAttnHeadDim;
-  const bf16x2_t ones = __builtin_bit_cast(bf16x2_t, 0x3F803F80u);
   float tm;
   if constexpr (NSB == 2) {
     tm = tile_max32(Sc);
@@ -104,10 +102,15 @@ __device__ __forceinline__ void walk_softmax_pv(f32x16 (&Sc)[NSB], WalkAcc &A, c
 #pragma unroll
       for (int r2 = 0; r2 < 16; ++r2) A.O[i][r2] *= alpha;
   }
+}
+
+// The softmax weights of NSB x 32 keys in bf16, as the second operand of the product with V.
+template <int NSB>
+__device__ __forceinline__ void walk_weights(const f32x16 (&Sc)[NSB], WalkAcc &A, float scale_log2, uint32_t (&pk)[2 * NSB][4]) {
+  const bf16x2_t ones = __builtin_bit_cast(bf16x2_t, 0x3F803F80u);
   const float m_use = A.m == -INFINITY ? 0.f : A.m;
   // Weights are rounded to bf16, the matrix product's operand type (2^-8 of a
   // weight, as the inputs' own type); their sum is taken of the rounded ones.
-  uint32_t pk[2 * NSB][4];
 #pragma unroll
   for (int sb = 0; sb < NSB; ++sb)
 #pragma unroll
@@ -123,6 +126,12 @@ __device__ __forceinline__ void walk_softmax_pv(f32x16 (&Sc)[NSB], WalkAcc &A, c
 #pragma unroll
     for (int q = 0; q < 4; ++q)
       A.lsum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, pk[mh][q]), ones, A.lsum, false);
+}
+
+// Their product with V; vs: V row of the first of the keys.
+template <int NSB>
+__device__ __forceinline__ void walk_pv(const uint32_t (&pk)[2 * NSB][4], WalkAcc &A, const uint8_t *vs, const int (&vro)[kAttnHeadDim / 32]) {
+  constexpr int D = kAttnHeadDim;
 #pragma unroll
   for (int mh = 0; mh < 2 * NSB; ++mh) {
     const bf16x8 pf = __builtin_bit_cast(bf16x8, uint4{pk[mh][0], pk[mh][1], pk[mh][2], pk[mh][3]});
@@ -135,6 +144,15 @@ __device__ __forceinline__ void walk_softmax_pv(f32x16 (&Sc)[NSB], WalkAcc &A, c
       A.O[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf, A.O[i], 0, 0, 0);
     }
   }
+}
+
+template <int NSB>
+__device__ __forceinline__ void walk_softmax_pv(const f32x16 (&Sc)[NSB], WalkAcc &A, const uint8_t *vs, const int (&vro)[kAttnHeadDim / 32],
+                                                float scale_log2) {
+  uint32_t pk[2 * NSB][4];
+  walk_max<NSB>(Sc, A, scale_log2);
+  walk_weights<NSB>(Sc, A, scale_log2, pk);
+  walk_pv<NSB>(pk, A, vs, vro);
 }
 
 // The end of a row block's walk: KSPLIT = 2 merges the two wave groups through LDS (mo:
@@ -198,7 +216,8 @@ __device__ __forceinline__ void walk_finish(const WalkArgs &a, const WalkItem &i
 // The end of an fp32 row block: its W waves' parts of the same 32 rows are merged
 // through LDS, wave w taking entries 4 DB / W w ... of the accumulator order, then
 // written to `out` or to the parts.
-template <int DB, int W>
+// COLS: row r of block i of O^T is column DB r + i (else 32 i + r).
+template <int DB, int W, bool COLS = false>
 __device__ __forceinline__ void walk_finish_f32(const WalkArgs &a, const WalkItem &it, const f32x16 (&O)[DB], float m, float l,
                                                 bool row_ok, int node, int hq, float (&merge)[W][walk_unit_floats(DB)]) {
   constexpr int UF = walk_unit_floats(DB);
@@ -221,14 +240,23 @@ __device__ __forceinline__ void walk_finish_f32(const WalkArgs &a, const WalkIte
   float *const u = direct ? nullptr : a.part + (int64_t)walk_part(a, S, it.kvh, it.rb, it.ch) * UF;
   const float inv = direct ? 1.f / lt : 1.f;
   for (int iq = wave; iq < 4 * DB; iq += W) {        // d-block iq / 4, entries 4 (iq % 4) .. + 3
+    const int col = 32 * (iq >> 2) + 8 * (iq & 3) + 4 * h;
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int w = 0; w < W; ++w) {
-      const f32x4 v = *reinterpret_cast<const f32x4 *>(&merge[w][(iq * 64 + lane) * 4]);
+      f32x4 v;
+      if constexpr (COLS) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int r = (col + e) / DB, q = 4 * ((col + e) % DB) + (r >> 3);
+          v[e] = merge[w][(q * 64 + 32 * (r >> 2 & 1) + (lane & 31)) * 4 + (r & 3)];
+        }
+      } else {
+        v = *reinterpret_cast<const f32x4 *>(&merge[w][(iq * 64 + lane) * 4]);
+      }
 #pragma unroll
       for (int e = 0; e < 4; ++e) o[e] = fmaf(v[e], mw[w], o[e]);
     }
-    const int col = 32 * (iq >> 2) + 8 * (iq & 3) + 4 * h;
     if (!row_ok) continue;
     if (!direct) *reinterpret_cast<f32x4 *>(u + (iq * 64 + lane) * 4) = o;
     else if (col < d)
