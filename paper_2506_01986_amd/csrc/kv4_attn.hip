@@ -42,7 +42,7 @@ constexpr int kVTile4 = TK * D * 2;           // 16 KB in bf16
 
 typedef int i32x8_t __attribute__((ext_vector_type(8)));
 typedef uint32_t u32x6_t __attribute__((ext_vector_type(6)));
-typedef __bf16 bf16x32_t __attribute__((ext_vector_type(32)));
+typedef float f32x32_t __attribute__((ext_vector_type(32)));
 
 // A wave's queries as the scaled product's operands, in STEPS products over the
 // columns: step s takes group (4 / STEPS) s + h of a lane's row, scale byte i of sc[s]
@@ -62,11 +62,16 @@ struct Query6 {
       uint4 w[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) w[i] = ld16_or_zero(ok, row + (D / STEPS) * s + kKv4Group * h + 8 * i);
-      bf16x32_t x;
-      __builtin_memcpy(&x, w, sizeof(x));
+      // columns in two halves, even and odd, as the conversion takes and interleaves them
+      f32x16 even, odd;
       float top = 0.f;
 #pragma unroll
-      for (int i = 0; i < 32; ++i) top = fmaxf(top, fabsf((float)x[i]));
+      for (int i = 0; i < 16; ++i) {
+        const uint32_t u = reinterpret_cast<const uint32_t *>(w)[i];
+        even[i] = __uint_as_float(u << 16);
+        odd[i] = __uint_as_float(u & 0xFFFF0000u);
+        top = fmaxf(fmaxf(top, fabsf(even[i])), fabsf(odd[i]));
+      }
       // 7.5 = 1.875 x 4; magnitudes under 2^-113 are lost (scores of nothing)
       const uint32_t u = __float_as_uint(top);
       const uint32_t e = max((int)(u >> 23) - 2 + ((u & 0x7FFFFFu) > 0x700000u), 14);
@@ -74,11 +79,14 @@ struct Query6 {
 #pragma unroll
       for (int p = 0; p < 3; ++p) {
         const float unit = __uint_as_float((e - (p == 0 ? 0 : p == 1 ? 4 : 10)) << 23);
-        part[s][p] = __builtin_amdgcn_cvt_scalef32_pk32_fp6_bf16(x, unit);
+        part[s][p] = __builtin_amdgcn_cvt_scalef32_2xpk16_fp6_f32(even, odd, unit);
         if (p < 2) {
-          const bf16x32_t y = __builtin_amdgcn_cvt_scalef32_pk32_bf16_fp6(part[s][p], unit);
+          const f32x32_t y = __builtin_amdgcn_cvt_scalef32_pk32_f32_fp6(part[s][p], unit);
 #pragma unroll
-          for (int i = 0; i < 32; ++i) x[i] = (__bf16)((float)x[i] - (float)y[i]);   // exact
+          for (int i = 0; i < 16; ++i) {       // exact
+            even[i] -= y[2 * i];
+            odd[i] -= y[2 * i + 1];
+          }
         }
       }
     }
