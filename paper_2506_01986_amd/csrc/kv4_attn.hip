@@ -45,42 +45,72 @@ typedef uint32_t u32x6_t __attribute__((ext_vector_type(6)));
 typedef float f32x32_t __attribute__((ext_vector_type(32)));
 
 // A wave's queries as the scaled product's operands, in STEPS products over the
-// columns: step s takes group (4 / STEPS) s + h of a lane's row, scale byte i of sc[s]
-// is part i's.
-template <int STEPS>
+// columns: step s takes group (4 / STEPS) s + h of a lane's row.  A query is the sum of
+// its parts, each of six bits (sign, two of exponent, three of mantissa: steps of 1/8
+// under 2, 1/4 under 4, 1/2 up to 7.5) times 2^(e - shift), the rest of the one before:
+//   bf16  3 parts, shifts 0, 4, 10: every value down to 2^-8 of the 32 columns' largest
+//         (which lies in (3.75, 7.5] x 2^e), smaller ones within 2^-16 of it
+//   fp32  5 parts, shifts 0, 4, 9, 14, 19: a rest is at most 4 units of the next part and
+//         leaves 1/8 of one, 2^-22 in the end: within 2^-23.9 of the largest
+// Scale byte p % 4 of sc[s][p / 4] is part p's.
+template <int STEPS, bool F32>
 struct Query6 {
-  u32x6_t part[STEPS][3];
-  uint32_t sc[STEPS];
+  static constexpr int PARTS = F32 ? 5 : 3;
+  u32x6_t part[STEPS][PARTS];
+  uint32_t sc[STEPS][(PARTS + 3) / 4];
 
+  static constexpr int shift(int p) { return p == 0 ? 0 : F32 ? 5 * p - 1 : p == 1 ? 4 : 10; }
   __device__ __forceinline__ i32x8_t operand(int s, int p) const {
     const u32x6_t &w = part[s][p];
     return i32x8_t{(int)w[0], (int)w[1], (int)w[2], (int)w[3], (int)w[4], (int)w[5], 0, 0};
   }
-  __device__ __forceinline__ void load(bool ok, const uint16_t *row, int h) {
+  // row: the lane's row; groups of columns past `groups` are zero
+  __device__ __forceinline__ void load(bool ok, const void *row, int h, int groups = 4) {
 #pragma unroll
     for (int s = 0; s < STEPS; ++s) {
-      uint4 w[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) w[i] = ld16_or_zero(ok, row + (D / STEPS) * s + kKv4Group * h + 8 * i);
+      const int g = (4 / STEPS) * s + h;
+      const bool has = ok && g < groups;
       // columns in two halves, even and odd, as the conversion takes and interleaves them
       f32x16 even, odd;
+      if constexpr (F32) {
+        const float *p = static_cast<const float *>(row) + kKv4Group * g;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          f32x4 w = {0.f, 0.f, 0.f, 0.f};
+          if (has) w = *reinterpret_cast<const f32x4 *>(p + 4 * i);
+          even[2 * i] = w[0];
+          odd[2 * i] = w[1];
+          even[2 * i + 1] = w[2];
+          odd[2 * i + 1] = w[3];
+        }
+      } else {
+        const uint16_t *p = static_cast<const uint16_t *>(row) + kKv4Group * g;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint4 w = ld16_or_zero(has, p + 8 * i);
+          const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            even[4 * i + j] = __uint_as_float(u[j] << 16);
+            odd[4 * i + j] = __uint_as_float(u[j] & 0xFFFF0000u);
+          }
+        }
+      }
       float top = 0.f;
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        const uint32_t u = reinterpret_cast<const uint32_t *>(w)[i];
-        even[i] = __uint_as_float(u << 16);
-        odd[i] = __uint_as_float(u & 0xFFFF0000u);
-        top = fmaxf(fmaxf(top, fabsf(even[i])), fabsf(odd[i]));
-      }
-      // 7.5 = 1.875 x 4; magnitudes under 2^-113 are lost (scores of nothing)
+      for (int i = 0; i < 16; ++i) top = fmaxf(fmaxf(top, fabsf(even[i])), fabsf(odd[i]));
+      // 7.5 = 1.875 x 4; magnitudes under 2^-103 are lost (scores of nothing)
       const uint32_t u = __float_as_uint(top);
-      const uint32_t e = max((int)(u >> 23) - 2 + ((u & 0x7FFFFFu) > 0x700000u), 14);
-      sc[s] = e | (e - 4) << 8 | (e - 10) << 16;
+      const uint32_t e = max((int)(u >> 23) - 2 + ((u & 0x7FFFFFu) > 0x700000u), 24);
 #pragma unroll
-      for (int p = 0; p < 3; ++p) {
-        const float unit = __uint_as_float((e - (p == 0 ? 0 : p == 1 ? 4 : 10)) << 23);
+      for (int i = 0; i < (PARTS + 3) / 4; ++i) sc[s][i] = 0;
+#pragma unroll
+      for (int p = 0; p < PARTS; ++p) {
+        const uint32_t ep = e - shift(p);
+        const float unit = __uint_as_float(ep << 23);
+        sc[s][p / 4] |= ep << (8 * (p % 4));
         part[s][p] = __builtin_amdgcn_cvt_scalef32_2xpk16_fp6_f32(even, odd, unit);
-        if (p < 2) {
+        if (p + 1 < PARTS) {
           const f32x32_t y = __builtin_amdgcn_cvt_scalef32_pk32_f32_fp6(part[s][p], unit);
 #pragma unroll
           for (int i = 0; i < 16; ++i) {       // exact
@@ -94,11 +124,11 @@ struct Query6 {
 };
 
 template <int STEP, int PART>
-__device__ __forceinline__ f32x16 qk_part(uint4 k, const Query6<2> &q, f32x16 c, uint32_t kscale) {
+__device__ __forceinline__ f32x16 qk_part(uint4 k, const Query6<2, false> &q, f32x16 c, uint32_t kscale) {
   const i32x8_t a = {(int)k.x, (int)k.y, (int)k.z, (int)k.w, 0, 0, 0, 0};
   const i32x8_t b = q.operand(STEP, PART);
   // formats: 4 = four bits, 2 = six bits; the scale byte of each operand is chosen by number
-  return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, c, 4, 2, 2 * STEP, (int)kscale, PART, (int)q.sc[STEP]);
+  return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, c, 4, 2, 2 * STEP, (int)kscale, PART, (int)q.sc[STEP][0]);
 }
 
 // Four waves per block; K codes and V values each have a two-slot ring of 64-key
@@ -190,7 +220,7 @@ __device__ __forceinline__ void walk4(const WalkArgs &a, const WalkItem &it, uin
   const bool row_ok = my_row < rows;
   const int node = row_ok ? my_row / g : S.T - 1;
   const int hq = it.kvh * g + (row_ok ? my_row % g : 0);
-  Query6<2> Q;
+  Query6<2, false> Q;
   Q.load(row_ok, static_cast<const uint16_t *>(a.q) + ((int64_t)(S.row0 + node) * a.n_q + hq) * D, h);
   if (tree && tid < S.T) par[tid] = pn;
   WalkMask M{L, P, h, node};
@@ -296,6 +326,11 @@ __device__ __forceinline__ void walk4(const WalkArgs &a, const WalkItem &it, uin
 //   O^T: V is converted as it arrives, through the wave's own 16 KB of LDS.  A product
 //        contracts 32 keys, the four of each lane group from two blocks of 16, which is
 //        where the scores left the weights.
+// fp32 queries (DB groups of 32 columns) take the same way, up to 32 rows an item: past
+// 16, two waves have rows 0 to 15 and two the others.  A weight is the sum of three bf16
+// numbers, each the rest of the one before (24 bits), V is exact in bf16, and the sums
+// are fp32: the products cost a sixth of the fp32 matrix instructions' (2 x 32 rows x 64
+// keys x 128 columns: 6.9 us of those a wave).
 constexpr int kFewRows = 16;
 
 // Chunk of 16 bytes c of V row r: eight lanes that write (two rows, four groups) and 32
@@ -312,14 +347,17 @@ __device__ __forceinline__ float sum_of_groups(float x) {
   return sum_with_other_half(__uint_as_float(r[0]) + __uint_as_float(r[1]));
 }
 
-template <bool TREE>
+template <bool TREE, bool F32, int DB>
 __device__ __forceinline__ void walk4_few(const WalkArgs &a, const WalkItem &it, uint8_t (*lds)[kVTile4], int *par) {
+  constexpr int ROW = 16 * DB;            // bytes of a row's codes
   const WalkSet &S = it.S;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int q16 = lane & 15, G = lane >> 4, g = a.group, L = S.L, P = S.P;
   const int rows = S.T * g;
+  const int nr = F32 && rows - 32 * it.rb > kFewRows ? 2 : 1;     // groups of 16 rows, each with 4 / nr waves
+  const int my_row = 32 * it.rb + kFewRows * (wave & (nr - 1)) + q16;
   const int np = (P + TK - 1) / TK;
-  const int kend = walk_keys(S, 0, g);
+  const int kend = walk_keys(S, it.rb, g);
   const int j0 = it.ch * S.ct, j1 = min(np + (kend + TK - 1) / TK, j0 + S.ct);
   const int64_t head = (int64_t)it.kvh * a.cap_total;
   const int64_t prow = head + S.pbase, srow = head + S.base;
@@ -336,31 +374,31 @@ __device__ __forceinline__ void walk4_few(const WalkArgs &a, const WalkItem &it,
     const bool pre = j < np;
     const int kt = (pre ? j : j - np) * TK, end = pre ? P : kend;
     const int64_t row0 = pre ? prow : srow;
-    const uint8_t *const kb = K0 + row0 * kRow4, *const vb = V0 + row0 * kRow4;
-    const uint8_t *const ksb = a.ks + row0 * kScales, *const vsb = a.vs + row0 * kScales;
+    const uint8_t *const kb = K0 + row0 * ROW, *const vb = V0 + row0 * ROW;
+    const uint8_t *const ksb = a.ks + row0 * DB, *const vsb = a.vs + row0 * DB;
 #pragma unroll
     for (int n = 0; n < 4; ++n) {       // rows past the end repeat the last one (finite values, masked out)
       const uint32_t r = (uint32_t)min(kt + 16 * n + q16, end - 1);
-      w.k[n] = *reinterpret_cast<const uint4 *>(kb + r * kRow4 + 16 * G);
-      w.ks[n] = ksb[r * kScales + G];
+      w.k[n] = ld16_or_zero(DB == 4 || G < DB, kb + r * ROW + 16 * G);
+      w.ks[n] = DB == 4 || G < DB ? ksb[r * DB + G] : 127u;
     }
 #pragma unroll
     for (int n = 0; n < 4; ++n) {
       const uint32_t r = (uint32_t)min(kt + 16 * n + (lane >> 2), end - 1);
-      w.v[n] = *reinterpret_cast<const uint4 *>(vb + r * kRow4 + 16 * (lane & 3));
-      w.vs[n] = vsb[r * kScales + (lane & 3)];
+      w.v[n] = ld16_or_zero(DB == 4 || (lane & 3) < DB, vb + r * ROW + 16 * (lane & 3));
+      w.vs[n] = DB == 4 || (lane & 3) < DB ? vsb[r * DB + (lane & 3)] : 127u;
     }
   };
 
   Raw nxt;
-  const int jw = j0 + wave;
+  const int stride = kWaves4 / nr, jw = j0 + (nr == 2 ? wave >> 1 : wave);
   if (jw < j1) load(nxt, jw);
   const bool tree = TREE && S.slab;
-  const bool row_ok = q16 < rows;
-  const int node = row_ok ? q16 / g : S.T - 1;
-  const int hq = it.kvh * g + (row_ok ? q16 % g : 0);
-  Query6<1> Q;
-  Q.load(row_ok, static_cast<const uint16_t *>(a.q) + ((int64_t)(S.row0 + node) * a.n_q + hq) * D, G);
+  const bool row_ok = my_row < rows;
+  const int node = row_ok ? my_row / g : S.T - 1;
+  const int hq = it.kvh * g + (row_ok ? my_row % g : 0);
+  Query6<1, F32> Q;
+  Q.load(row_ok, static_cast<const uint8_t *>(a.q) + ((int64_t)(S.row0 + node) * a.n_q + hq) * (32 * DB * (F32 ? 4 : 2)), G, DB);
   WalkMask M{L, P, 0, node};
   if (TREE) {
     if (tree && tid < S.T) par[tid] = a.parent[S.row0 + tid];
@@ -369,32 +407,41 @@ __device__ __forceinline__ void walk4_few(const WalkArgs &a, const WalkItem &it,
   }
 
   float m = -INFINITY, lsum = 0.f;
-  f32x4 O[D / 16];
+  f32x4 O[2 * DB];
 #pragma unroll
-  for (int i = 0; i < D / 16; ++i) O[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int i = 0; i < 2 * DB; ++i) O[i] = f32x4{0.f, 0.f, 0.f, 0.f};
   const bf16x2_t ones = __builtin_bit_cast(bf16x2_t, 0x3F803F80u);
 
-  for (int j = jw; j < j1; j += kWaves4) {
+  for (int j = jw; j < j1; j += stride) {
     const Raw cur = nxt;
-    if (j + kWaves4 < j1) load(nxt, j + kWaves4);
+    if (j + stride < j1) load(nxt, j + stride);
     const bool pre = j < np;
     const int kt = (pre ? j : j - np) * TK;
     f32x4 Sc[4];
 #pragma unroll
     for (int n = 0; n < 4; ++n) {
       const i32x8_t ka = {(int)cur.k[n].x, (int)cur.k[n].y, (int)cur.k[n].z, (int)cur.k[n].w, 0, 0, 0, 0};
+      auto part = [&](auto p) __attribute__((always_inline)) {       // smallest parts first
+        Sc[n] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(ka, Q.operand(0, p), Sc[n], 4, 2, 0, (int)cur.ks[n], p % 4, (int)Q.sc[0][p / 4]);
+      };
       Sc[n] = f32x4{0.f, 0.f, 0.f, 0.f};
-      Sc[n] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(ka, Q.operand(0, 2), Sc[n], 4, 2, 0, (int)cur.ks[n], 2, (int)Q.sc[0]);
-      Sc[n] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(ka, Q.operand(0, 1), Sc[n], 4, 2, 0, (int)cur.ks[n], 1, (int)Q.sc[0]);
-      Sc[n] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(ka, Q.operand(0, 0), Sc[n], 4, 2, 0, (int)cur.ks[n], 0, (int)Q.sc[0]);
+      if constexpr (F32) {
+        part(std::integral_constant<int, 4>{});
+        part(std::integral_constant<int, 3>{});
+      }
+      part(std::integral_constant<int, 2>{});
+      part(std::integral_constant<int, 1>{});
+      part(std::integral_constant<int, 0>{});
     }
 #pragma unroll
     for (int n = 0; n < 4; ++n) {
       const int r = 16 * n + (lane >> 2), c = lane & 3;
       const float unit = kv4_scale(cur.vs[n]);
       const uint32_t w[4] = {cur.v[n].x, cur.v[n].y, cur.v[n].z, cur.v[n].w};
+      if (DB == 4 || c < DB) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) *reinterpret_cast<uint4 *>(mem + r * (D * 2) + 16 * few_swz(r, 4 * c + i)) = kv4_bf16x8(w[i], unit);
+        for (int i = 0; i < 4; ++i) *reinterpret_cast<uint4 *>(mem + r * (D * 2) + 16 * few_swz(r, 4 * c + i)) = kv4_bf16x8(w[i], unit);
+      }
     }
     // entry r of block n is key kt + 16 n + 4 G + r
     if (TREE && !pre) {
@@ -428,25 +475,35 @@ __device__ __forceinline__ void walk4_few(const WalkArgs &a, const WalkItem &it,
       m = m_new;
       lsum *= alpha;
 #pragma unroll
-      for (int i = 0; i < D / 16; ++i) O[i] *= alpha;
+      for (int i = 0; i < 2 * DB; ++i) O[i] *= alpha;
     }
     const float m_use = m == -INFINITY ? 0.f : m;
-    // weights in bf16, the product's operand type, and their sum of the rounded ones
-    uint32_t pk[2][4];
+    // bf16: weights are rounded to the product's operand type (2^-8 of a weight, as the
+    // inputs' own type), and their sum is taken of the rounded ones.
+    constexpr int WP = F32 ? 3 : 1;
+    uint32_t pk[WP][2][4];
 #pragma unroll
     for (int n = 0; n < 4; ++n)
 #pragma unroll
       for (int r = 0; r < 4; r += 2) {
-        const float p0 = fast_exp2(fmaf(Sc[n][r], a.scale_log2, -m_use)), p1 = fast_exp2(fmaf(Sc[n][r + 1], a.scale_log2, -m_use));
-        pk[n >> 1][2 * (n & 1) + (r >> 1)] = pack_bf16x2(p0, p1);
+        float p0 = fast_exp2(fmaf(Sc[n][r], a.scale_log2, -m_use)), p1 = fast_exp2(fmaf(Sc[n][r + 1], a.scale_log2, -m_use));
+        if (F32) lsum += p0 + p1;
+#pragma unroll
+        for (int w = 0; w < WP; ++w) {
+          const uint32_t u = pack_bf16x2(p0, p1);
+          pk[w][n >> 1][2 * (n & 1) + (r >> 1)] = u;
+          p0 -= __uint_as_float(u << 16);                // exact
+          p1 -= __uint_as_float(u & 0xFFFF0000u);
+        }
       }
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
+      if (!F32) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) lsum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, pk[b][e]), ones, lsum, false);
-      const bf16x8 pf = __builtin_bit_cast(bf16x8, uint4{pk[b][0], pk[b][1], pk[b][2], pk[b][3]});
+        for (int e = 0; e < 4; ++e) lsum = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2_t, pk[0][b][e]), ones, lsum, false);
+      }
 #pragma unroll
-      for (int i = 0; i < D / 16; ++i) {
+      for (int i = 0; i < 2 * DB; ++i) {
         // lane e of a group of 16 gives the place of piece e % 4 (8 bytes) of row e / 4 and gets column e of four rows
         const int r0 = 32 * b + 4 * G + (q16 >> 2), r1 = r0 + 16;
         const int at0 = r0 * (D * 2) + 16 * few_swz(r0, 2 * i + ((q16 & 3) >> 1)) + 8 * (q16 & 1);
@@ -454,52 +511,59 @@ __device__ __forceinline__ void walk4_few(const WalkArgs &a, const WalkItem &it,
         const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t *)(mem + at0));
         const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_t *)(mem + at1));
         const bf16x8 vf = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-        O[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf, O[i], 0, 0, 0);
+#pragma unroll
+        for (int w = WP - 1; w >= 0; --w)
+          O[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, __builtin_bit_cast(bf16x8, uint4{pk[w][b][0], pk[w][b][1], pk[w][b][2], pk[w][b][3]}), O[i], 0, 0, 0);
       }
     }
   }
 
   // The waves' parts: O[i] of a lane is columns 16 i + 4 G .. + 3 of row q16.
+  constexpr int ML = 32 * DB * kFewRows;
   float *const part = reinterpret_cast<float *>(mem);
 #pragma unroll
-  for (int i = 0; i < D / 16; ++i) *reinterpret_cast<f32x4 *>(part + ((4 * i + G) * kFewRows + q16) * 4) = O[i];
+  for (int i = 0; i < 2 * DB; ++i) *reinterpret_cast<f32x4 *>(part + ((4 * i + G) * kFewRows + q16) * 4) = O[i];
   const float ltot = sum_of_groups(lsum);
   if (G == 0) {
-    part[D * kFewRows + q16] = m;
-    part[D * kFewRows + kFewRows + q16] = ltot;
+    part[ML + q16] = m;
+    part[ML + kFewRows + q16] = ltot;
   }
   __syncthreads();
-  const bool direct = walk_direct(S, 0, g);
-  float *const u = direct ? nullptr : a.part + (int64_t)walk_part(a, S, it.kvh, 0, it.ch) * walk_unit_floats(D / 32);
-#pragma unroll
-  for (int e = 0; e < 2; ++e) {
-    const int row = tid & 15, quad = (tid >> 4) + 16 * e;     // columns 4 quad .. + 3
-    if (row >= rows) break;
+  const bool direct = walk_direct(S, it.rb, g);
+  float *const u = direct ? nullptr : a.part + (int64_t)walk_part(a, S, it.kvh, it.rb, it.ch) * walk_unit_floats(DB);
+  for (int e = tid; e < 8 * DB * kFewRows * nr; e += 64 * kWaves4) {
+    const int row = e & 15, grp = nr == 2 ? (e >> 4) & 1 : 0, quad = e >> (nr == 2 ? 5 : 4);     // columns 4 quad .. + 3
+    const int urow = kFewRows * grp + row, at_row = 32 * it.rb + urow;
+    if (at_row >= rows) continue;
     float w[kWaves4], mx = -INFINITY, lt = 0.f;
-#pragma unroll
-    for (int v = 0; v < kWaves4; ++v) {
-      w[v] = reinterpret_cast<const float *>(lds[v])[D * kFewRows + row];
-      mx = fmaxf(mx, w[v]);
-    }
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int v = 0; v < kWaves4; ++v) {
+      w[v] = nr == 1 || (v & 1) == grp ? reinterpret_cast<const float *>(lds[v])[ML + row] : -INFINITY;
+      mx = fmaxf(mx, w[v]);
+    }
+#pragma unroll
+    for (int v = 0; v < kWaves4; ++v) {
+      if (nr == 2 && (v & 1) != grp) continue;
       const float *pv = reinterpret_cast<const float *>(lds[v]);
       const float wt = w[v] == -INFINITY ? 0.f : fast_exp2(w[v] - mx);
-      lt = fmaf(pv[D * kFewRows + kFewRows + row], wt, lt);
+      lt = fmaf(pv[ML + kFewRows + row], wt, lt);
       const f32x4 x = *reinterpret_cast<const f32x4 *>(pv + (quad * kFewRows + row) * 4);
 #pragma unroll
       for (int c = 0; c < 4; ++c) o[c] = fmaf(x[c], wt, o[c]);
     }
     if (direct) {
       const float inv = 1.f / lt;
-      const int64_t at = ((int64_t)(S.row0 + row / g) * a.n_q + it.kvh * g + row % g) * D + 4 * quad;
-      *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(a.out) + at) = uint2{pack_bf16x2(o[0] * inv, o[1] * inv), pack_bf16x2(o[2] * inv, o[3] * inv)};
+      const int64_t at = ((int64_t)(S.row0 + at_row / g) * a.n_q + it.kvh * g + at_row % g) * (32 * DB) + 4 * quad;
+      if constexpr (F32)
+        *reinterpret_cast<f32x4 *>(static_cast<float *>(a.out) + at) = f32x4{o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
+      else
+        *reinterpret_cast<uint2 *>(static_cast<uint16_t *>(a.out) + at) = uint2{pack_bf16x2(o[0] * inv, o[1] * inv), pack_bf16x2(o[2] * inv, o[3] * inv)};
     } else {                              // in the order of write_part: row % 32 + 32 h, columns 32 i + 8 q + 4 h
-      *reinterpret_cast<f32x4 *>(u + ((quad >> 1) * 64 + row + 32 * (quad & 1)) * 4) = o;
+      *reinterpret_cast<f32x4 *>(u + ((quad >> 1) * 64 + urow + 32 * (quad & 1)) * 4) = o;
       if (quad == 0) {
-        u[(D / 32) * 1024 + row] = mx;
-        u[(D / 32) * 1024 + 32 + row] = lt;
+        u[DB * 1024 + urow] = mx;
+        u[DB * 1024 + 32 + urow] = lt;
       }
     }
   }
@@ -511,151 +575,28 @@ __global__ __launch_bounds__(kWaves4 * 64, 2) void walk4_attn_bf16(WalkArgs a) {
   __shared__ __attribute__((aligned(1024))) uint8_t vring[4][kVTile4];   // two slots, or a tile of each wave
   WalkItem it;
   decode_walk(a, blockIdx.x, it);
-  if (it.S.rb == 32) walk4_few<TREE>(a, it, vring, reinterpret_cast<int *>(kring[0]));
+  if (it.S.rb == 32) walk4_few<TREE, false, 4>(a, it, vring, reinterpret_cast<int *>(kring[0]));
   else if (it.S.rb == 64) walk4<2, TREE>(a, it, kring, vring);
   else walk4<1, TREE>(a, it, kring, vring);
 }
 
-// fp32 queries: the arrangement of the fp32 attention over rows of 32 bits (32 query
-// rows a block on the 32x32x2 product, the waves taking 32-key tiles in turn, merged
-// through LDS), with the rows converted to fp32 as they are read.  DB: 32-column
-// groups of the head; lane half h contracts columns 16 DB h .. + 16 DB - 1.  A lane's
-// rows of O^T are columns DB r .. + DB - 1 (r = lane % 32, one of each block i), so that
-// a key's V takes one load of a lane and not DB.
-constexpr int kF32Waves = 4;
-
 template <int DB, bool TREE>
-__global__ __launch_bounds__(64 * kF32Waves, 2) void walk4_attn_f32(WalkArgs a) {
-  constexpr int RB = 32, W = kF32Waves, UF = walk_unit_floats(DB), DD = 32 * DB;
-  constexpr int VR = DB <= 2 ? 16 : 4;   // key rows of V loaded together
-  __shared__ __attribute__((aligned(16))) float merge[W][UF];
+__global__ __launch_bounds__(kWaves4 * 64, 2) void walk4_attn_f32(WalkArgs a) {
+  __shared__ __attribute__((aligned(1024))) uint8_t lds[kWaves4][kVTile4];
   __shared__ int par[kMaxNodes];
   WalkItem it;
   decode_walk(a, blockIdx.x, it);
-  const WalkSet &S = it.S;
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int h = lane >> 5, g = a.group, L = S.L, P = S.P;
-  const int rows = S.T * g;
-  const int np = (P + TK - 1) / TK;
-  const int kend = walk_keys(S, it.rb, g);
-  const int j0 = it.ch * S.ct, j1 = min(np + (kend + TK - 1) / TK, j0 + S.ct);
-  const int64_t head = (int64_t)it.kvh * a.cap_total;
-  const uint8_t *const K0 = static_cast<const uint8_t *>(a.k), *const V0 = static_cast<const uint8_t *>(a.v);
-
-  const bool tree = TREE && S.slab;
-  const int my_row = it.rb * RB + (lane & 31);
-  const bool row_ok = my_row < rows;
-  const int node = row_ok ? my_row / g : S.T - 1;
-  const int hq = it.kvh * g + (row_ok ? my_row % g : 0);
-  f32x4 qf[4 * DB];
-  {
-    const float *qp = static_cast<const float *>(a.q) + ((int64_t)(S.row0 + node) * a.n_q + hq) * DD + 16 * DB * h;
-#pragma unroll
-    for (int t = 0; t < 4 * DB; ++t) {
-      qf[t] = f32x4{0.f, 0.f, 0.f, 0.f};
-      if (row_ok) qf[t] = *reinterpret_cast<const f32x4 *>(qp + 4 * t);
-    }
-  }
-  WalkMask M{L, P, h, node};
-  if (TREE) {
-    if (tree && tid < S.T) par[tid] = a.parent[S.row0 + tid];
-    ring_barrier();                                  // (does not wait for the queries)
-    if (tree) M.root_path(par, node);
-  }
-
-  // the lane's columns: their first byte and place in it, their groups, the last of the first group
-  const int col = DB * (lane & 31), vbyte = col >> 1, vshift = 4 * (col & 1), vgroup = col >> 5, vlast = (col + DB - 1) >> 5;
-  const int vsplit = 31 - (col & 31);
-  float m = -INFINITY, l = 0.f;
-  f32x16 O[DB];
-#pragma unroll
-  for (int i = 0; i < DB; ++i)
-#pragma unroll
-    for (int r = 0; r < 16; ++r) O[i][r] = 0.f;
-  for (int t2 = 2 * j0 + wave; t2 < 2 * j1; t2 += W) {
-    const bool pre = (t2 >> 1) < np;
-    const int kt = (pre ? t2 : t2 - 2 * np) * 32, end = pre ? P : kend;
-    if (kt >= end) continue;
-    const int64_t base = head + (pre ? S.pbase : S.base);
-    const int64_t kr = base + min(kt + (lane & 31), end - 1);
-    uint2 kc[DB];                                    // 16 columns each
-    uint32_t ksc[DB];                                // and their scale
-#pragma unroll
-    for (int i = 0; i < DB; ++i) {
-      kc[i] = *reinterpret_cast<const uint2 *>(K0 + kr * (DD / 2) + 8 * (DB * h + i));
-      ksc[i] = a.ks[kr * DB + ((DB * h + i) >> 1)];
-    }
-    uint32_t vc[VR], vs0[VR], vs1[VR];               // a lane's columns' codes of key rows, and the scales of the first and last
-    auto load_v = [&](int r0) __attribute__((always_inline)) {
-#pragma unroll
-      for (int r = 0; r < VR; ++r) {
-        const int64_t vr = base + min(kt + 8 * ((r0 + r) >> 2) + 4 * h + ((r0 + r) & 3), end - 1);
-        const uint8_t *p = V0 + vr * (DD / 2) + vbyte, *ps = a.vs + vr * DB;
-        vc[r] = DB == 4 ? *reinterpret_cast<const uint16_t *>(p) : DB == 3 ? p[0] | (uint32_t)p[1] << 8 : p[0];
-        vs0[r] = ps[vgroup];
-        vs1[r] = DB == 3 ? ps[vlast] : vs0[r];
-      }
-    };
-    if (VR == 16) load_v(0);
-    f32x16 Sc[1];
-#pragma unroll
-    for (int r = 0; r < 16; ++r) Sc[0][r] = 0.f;
-#pragma unroll
-    for (int i = 0; i < DB; ++i) {
-      const float s = kv4_scale(ksc[i]);
-      const f32x2_t kv[8] = {kv4_f32x2<0>(kc[i].x, s), kv4_f32x2<1>(kc[i].x, s), kv4_f32x2<2>(kc[i].x, s), kv4_f32x2<3>(kc[i].x, s),
-                             kv4_f32x2<0>(kc[i].y, s), kv4_f32x2<1>(kc[i].y, s), kv4_f32x2<2>(kc[i].y, s), kv4_f32x2<3>(kc[i].y, s)};
-#pragma unroll
-      for (int c = 0; c < 16; ++c)
-        Sc[0] = __builtin_amdgcn_mfma_f32_32x32x2f32(kv[c >> 1][c & 1], qf[4 * i + (c >> 2)][c & 3], Sc[0], 0, 0, 0);
-    }
-    walk_mask<1, TREE>(Sc, M, pre, kt, end, 0);
-    float tm = -INFINITY;
-#pragma unroll
-    for (int r = 0; r < 16; ++r) tm = fmaxf(tm, Sc[0][r]);
-    const float mn = fmaxf(m, max_with_other_half(tm) * a.scale_log2);
-    const float m_use = mn == -INFINITY ? 0.f : mn;
-    const float alpha = m == -INFINITY ? 0.f : fast_exp2(m - m_use);
-    m = mn;
-    l *= alpha;
-#pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      Sc[0][r] = fast_exp2(fmaf(Sc[0][r], a.scale_log2, -m_use));
-      l += Sc[0][r];
-    }
-#pragma unroll
-    for (int i = 0; i < DB; ++i)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) O[i][r] *= alpha;
-#pragma unroll
-    for (int r0 = 0; r0 < 16; r0 += VR) {
-      if (VR < 16) load_v(r0);
-#pragma unroll
-      for (int r = 0; r < VR; ++r)
-#pragma unroll
-        for (int i = 0; i < DB; ++i) {
-          const uint32_t w = vc[r] >> vshift;
-          const float unit = kv4_scale(DB == 3 && i > vsplit ? vs1[r] : vs0[r]);
-          const f32x2_t v = i < 2 ? kv4_f32x2<0>(w, unit) : kv4_f32x2<1>(w, unit);
-          O[i] = __builtin_amdgcn_mfma_f32_32x32x2f32(v[i & 1], Sc[0][r0 + r], O[i], 0, 0, 0);
-        }
-    }
-  }
-  walk_finish_f32<DB, W, true>(a, it, O, m, l, row_ok, node, hq, merge);
-}
-
-template <int DB, bool TREE>
-void launch4_f32(const WalkArgs &a, hipStream_t st) {
-  hipLaunchKernelGGL((walk4_attn_f32<DB, TREE>), dim3(a.blocks), dim3(64 * kF32Waves), 0, st, a);
+  walk4_few<TREE, true, DB>(a, it, lds, par);
 }
 
 template <bool TREE>
 void launch4_f32(const WalkArgs &a, hipStream_t st) {
+  const dim3 grid(a.blocks), block(kWaves4 * 64);
   switch (a.head_dim / 32) {
-    case 1: return launch4_f32<1, TREE>(a, st);
-    case 2: return launch4_f32<2, TREE>(a, st);
-    case 3: return launch4_f32<3, TREE>(a, st);
-    default: return launch4_f32<4, TREE>(a, st);
+    case 1: hipLaunchKernelGGL((walk4_attn_f32<1, TREE>), grid, block, 0, st, a); break;
+    case 2: hipLaunchKernelGGL((walk4_attn_f32<2, TREE>), grid, block, 0, st, a); break;
+    case 3: hipLaunchKernelGGL((walk4_attn_f32<3, TREE>), grid, block, 0, st, a); break;
+    default: hipLaunchKernelGGL((walk4_attn_f32<4, TREE>), grid, block, 0, st, a);
   }
 }
 

@@ -216,8 +216,7 @@ __device__ __forceinline__ void walk_finish(const WalkArgs &a, const WalkItem &i
 // The end of an fp32 row block: its W waves' parts of the same 32 rows are merged
 // through LDS, wave w taking entries 4 DB / W w ... of the accumulator order, then
 // written to `out` or to the parts.
-// COLS: row r of block i of O^T is column DB r + i (else 32 i + r).
-template <int DB, int W, bool COLS = false>
+template <int DB, int W>
 __device__ __forceinline__ void walk_finish_f32(const WalkArgs &a, const WalkItem &it, const f32x16 (&O)[DB], float m, float l,
                                                 bool row_ok, int node, int hq, float (&merge)[W][walk_unit_floats(DB)]) {
   constexpr int UF = walk_unit_floats(DB);
@@ -244,16 +243,7 @@ __device__ __forceinline__ void walk_finish_f32(const WalkArgs &a, const WalkIte
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int w = 0; w < W; ++w) {
-      f32x4 v;
-      if constexpr (COLS) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int r = (col + e) / DB, q = 4 * ((col + e) % DB) + (r >> 3);
-          v[e] = merge[w][(q * 64 + 32 * (r >> 2 & 1) + (lane & 31)) * 4 + (r & 3)];
-        }
-      } else {
-        v = *reinterpret_cast<const f32x4 *>(&merge[w][(iq * 64 + lane) * 4]);
-      }
+      const f32x4 v = *reinterpret_cast<const f32x4 *>(&merge[w][(iq * 64 + lane) * 4]);
 #pragma unroll
       for (int e = 0; e < 4; ++e) o[e] = fmaf(v[e], mw[w], o[e]);
     }
