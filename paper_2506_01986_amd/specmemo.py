@@ -538,12 +538,12 @@ class QKVRows:
 
     def __init__(self, q, k, v, pos=None, cos=None, sin=None, rot_dim: Optional[int] = None, rot_style: int = ROT_HALVES,
                  q_norm=None, k_norm=None, eps: float = 1e-5):
+        if k is None or v is None or k.dim() != 3:
+            raise ValueError("keys and values [tokens][heads][head_dim] are needed")
         d = int(k.shape[2])
         for name, x in (("q", q), ("k", k), ("v", v)):
             if x is None:
-                if name == "q":
-                    continue
-                raise ValueError(f"{name} is missing")
+                continue
             if x.dim() != 3 or int(x.shape[0]) != int(k.shape[0]) or int(x.shape[2]) != d or x.dtype != k.dtype or str(x.dtype) not in _VALUES:
                 raise ValueError(f"{name}: {tuple(x.shape)} of {x.dtype} beside keys {tuple(k.shape)} of {k.dtype}")
             if x.stride(2) != 1 or (x.shape[1] > 1 and x.stride(1) != d):
