@@ -767,7 +767,7 @@ auto guarded(decltype(std::declval<F>()()) on_throw, F f) noexcept -> decltype(f
 }
 
 // A prefix must lie in the pool, and where it reaches into a slab, in its committed rows.
-int check_prefix(const specmemo_prefix *px, const specmemo_kv *kv, int dt, int B) {
+int check_prefix(const specmemo_prefix *px, const specmemo_kv *kv, int64_t most, int B) {
   if (!px) return SPECMEMO_OK;
   if (!px->base_h || !px->len_h) return fail(SPECMEMO_E_ARG, "prefix host arrays must be non-NULL");
   std::vector<int> order(B);
@@ -780,7 +780,6 @@ int check_prefix(const specmemo_prefix *px, const specmemo_kv *kv, int dt, int B
     if (base < 0 || base > kv->cap_total - len)
       return fail(SPECMEMO_E_BUDGET, "sequence %d: prefix of %lld rows at %lld outside the pool of %lld rows", b,
                   (long long)len, (long long)base, (long long)kv->cap_total);
-    const int64_t most = dt == SPECMEMO_BF16 ? kMaxSlabRows : INT32_MAX / 2;   // tile numbers and row offsets in 32 bits
     if (len > most) return fail(SPECMEMO_E_BUDGET, "sequence %d: prefix of %lld rows exceeds %lld", b, (long long)len, (long long)most);
     if (b > 0 && base == px->base_h[b - 1] && len == px->len_h[b - 1]) continue;
     // the slabs that begin before the prefix ends, from the last one back to the prefix's start
@@ -798,19 +797,20 @@ int check_prefix(const specmemo_prefix *px, const specmemo_kv *kv, int dt, int B
   return SPECMEMO_OK;
 }
 
-// Shared checks of the two calls (lengths and trees are checked before).
-int check_walk(int dt, const TreeInfo &ti, const int32_t *off_h, const specmemo_kv *kv, const specmemo_prefix *px, int n_q) {
+// Shared checks of the calls (lengths and trees are checked before).  four: a 4-bit pool.
+int check_walk(int dt, const TreeInfo &ti, const int32_t *off_h, const specmemo_kv *kv, const specmemo_prefix *px, int n_q, bool four) {
   int rc;
+  const int64_t most = dt == SPECMEMO_BF16 || four ? kMaxSlabRows : INT32_MAX / 2;   // tile numbers and row offsets in 32 bits
   if ((rc = check_kv(dt, kv, ti, off_h))) return rc;
   if (n_q < 1 || n_q % kv->n_kv) return fail(SPECMEMO_E_ARG, "n_q=%d must be a positive multiple of n_kv=%d", n_q, kv->n_kv);
   if (kv->cap_total >= INT64_C(1) << 40) return fail(SPECMEMO_E_ARG, "cap_total=%lld, under 2^40 expected", (long long)kv->cap_total);
   for (int b = 0; b < ti.B; ++b) {
-    if (dt == SPECMEMO_BF16 && kv->seq_cap_h[b] > kMaxSlabRows)
+    if (kv->seq_cap_h[b] > most && most == kMaxSlabRows)
       return fail(SPECMEMO_E_BUDGET, "seq_cap[%d]=%d exceeds %d rows", b, kv->seq_cap_h[b], kMaxSlabRows);
     if ((int64_t)(off_h[b + 1] - off_h[b]) * (n_q / kv->n_kv) > INT32_MAX / 2)
       return fail(SPECMEMO_E_ARG, "sequence %d: too many query rows", b);
   }
-  return check_prefix(px, kv, dt, ti.B);
+  return check_prefix(px, kv, most, ti.B);
 }
 
 int check_offsets(int B, const int32_t *off, TreeInfo *ti) {
@@ -824,11 +824,12 @@ int check_offsets(int B, const int32_t *off, TreeInfo *ti) {
   return SPECMEMO_OK;
 }
 
-int check_prompt(int dt, int B, const int32_t *off, const specmemo_kv *kv, const specmemo_prefix *px, int n_q, TreeInfo *ti) {
+int check_prompt(int dt, int B, const int32_t *off, const specmemo_kv *kv, const specmemo_prefix *px, int n_q, TreeInfo *ti,
+                 bool four = false) {
   int rc;
   if ((rc = check_dtype(dt))) return rc;
   if ((rc = check_offsets(B, off, ti))) return rc;
-  return check_walk(dt, *ti, off, kv, px, n_q);
+  return check_walk(dt, *ti, off, kv, px, n_q, four);
 }
 
 WalkPlan make_walk(int dt, bool causal, const TreeInfo &ti, const int32_t *off_h, const specmemo_kv *kv,
@@ -910,11 +911,11 @@ int run_walk(int dt, bool tree, const TreeInfo &ti, const int32_t *off_h, const 
                     tree ? "tree attention launch" : "prompt attention launch");
 }
 
-int check_tree_walk(int dt, const specmemo_trees *t, const specmemo_kv *kv, const specmemo_prefix *px, int n_q, TreeInfo *ti) {
+int check_tree4(int dt, const specmemo_trees *t, const specmemo_kv *kv, const specmemo_prefix *px, int n_q, TreeInfo *ti) {
   int rc;
   if ((rc = check_dtype(dt))) return rc;
   if ((rc = check_trees(t, ti))) return rc;
-  return check_walk(dt, *ti, t->node_off_h, kv, px, n_q);
+  return check_walk(dt, *ti, t->node_off_h, kv, px, n_q, true);
 }
 
 int check_tree_prefix(int dt, const specmemo_trees *t, const specmemo_kv *kv, const specmemo_prefix *px, int n_q, TreeInfo *ti) {
@@ -922,7 +923,7 @@ int check_tree_prefix(int dt, const specmemo_trees *t, const specmemo_kv *kv, co
   if ((rc = check_dtype(dt))) return rc;
   if ((rc = check_trees(t, ti))) return rc;
   if (!px) return fail(SPECMEMO_E_ARG, "prefix is NULL");
-  return check_walk(dt, *ti, t->node_off_h, kv, px, n_q);
+  return check_walk(dt, *ti, t->node_off_h, kv, px, n_q, false);
 }
 
 }  // namespace
@@ -1461,7 +1462,7 @@ int specmemo_kv4_prompt_attn(specmemo_dtype dt, int32_t B, const int32_t *new_of
     int rc;
     if ((rc = check_kv4(kv))) return rc;
     const specmemo_kv view = as_kv(*kv);
-    if ((rc = check_prompt(dt, B, new_off_h, &view, prefix, n_q, &ti))) return rc;
+    if ((rc = check_prompt(dt, B, new_off_h, &view, prefix, n_q, &ti, true))) return rc;
     return run_walk(dt, false, ti, new_off_h, nullptr, &view, prefix, n_q, scale, q, out, ws, ws_bytes, stream, kv);
   });
 }
@@ -1472,7 +1473,7 @@ size_t specmemo_kv4_prompt_attn_bytes(specmemo_dtype dt, int32_t B, const int32_
     TreeInfo ti;
     if (check_kv4(kv)) return (size_t)0;
     const specmemo_kv view = as_kv(*kv);
-    if (check_prompt(dt, B, new_off_h, &view, prefix, n_q, &ti)) return (size_t)0;
+    if (check_prompt(dt, B, new_off_h, &view, prefix, n_q, &ti, true)) return (size_t)0;
     return walk_ws_bytes(make_walk(dt, true, ti, new_off_h, &view, prefix, n_q, true), kv->head_dim);
   });
 }
@@ -1485,7 +1486,7 @@ int specmemo_kv4_tree_attn(specmemo_dtype dt, const specmemo_trees *t, const spe
     int rc;
     if ((rc = check_kv4(kv))) return rc;
     const specmemo_kv view = as_kv(*kv);
-    if ((rc = check_tree_walk(dt, t, &view, prefix, n_q, &ti))) return rc;
+    if ((rc = check_tree4(dt, t, &view, prefix, n_q, &ti))) return rc;
     return run_walk(dt, true, ti, t->node_off_h, t->parent, &view, prefix, n_q, scale, q, out, ws, ws_bytes, stream, kv);
   });
 }
@@ -1496,7 +1497,7 @@ size_t specmemo_kv4_tree_attn_bytes(specmemo_dtype dt, const specmemo_trees *t, 
     TreeInfo ti;
     if (check_kv4(kv)) return (size_t)0;
     const specmemo_kv view = as_kv(*kv);
-    if (check_tree_walk(dt, t, &view, prefix, n_q, &ti)) return (size_t)0;
+    if (check_tree4(dt, t, &view, prefix, n_q, &ti)) return (size_t)0;
     return walk_ws_bytes(make_walk(dt, false, ti, t->node_off_h, &view, prefix, n_q, true), kv->head_dim);
   });
 }

@@ -9,17 +9,18 @@
 // bf16 queries:
 //   S^T = K Q^T   K's codes and scales are operands as they lie: the scaled product
 //                 of 32 x 32 x 64 takes 4-bit values with a scale for each lane's 32
-//                 columns.  Its other operand holds six bits, so a query is three of
-//                 them, q = q0 2^e + q1 2^(e-4) + q2 2^(e-10), each the rest of the one
-//                 before: with e from the 32 columns' largest magnitude (in (3.75,
-//                 7.5] x 2^e) that is every bf16 value down to 2^-8 of the largest, and
-//                 smaller ones within 2^-16 of the largest.  Three such products take
-//                 0.76 of the time of the bf16 products of the same columns (15.9 ns
-//                 against 2 x 15.6 for 32 columns x 2), and K is neither converted nor
-//                 read from LDS in 16 bits.
+//                 columns.  Its other operand holds six bits, so a query is the sum of
+//                 three (Query6).  Three such products of 64 columns take a matrix core
+//                 48 ns, the four of the same columns in bf16 62, and K is neither
+//                 converted nor read from LDS in 16 bits.  (Two parts of eight bits, the
+//                 other way to hold a bf16 value, take 59.)
 //   O^T = V^T P^T V is contracted over keys, whose scales differ, so a tile is
 //                 converted to bf16 once (by the block's four waves, on its way to LDS)
 //                 and read by the transposing loads.
+// 8192 tokens over 16384 keys, 64 query heads over 8 (3.3 TFLOP): 2.6 to 2.7 ms, 1.21 to
+// 1.27 PFLOP/s, where a large bf16 product of this card's library reaches 1.13 to 1.25:
+// matrix cores 0.50 busy at 2.05 GHz, vector units 0.58, loads and barriers 4% of a wave's
+// time.  Blocks of 128 rows (two a compute unit) take 1.7 us for a tile, of 64 1.2.
 #include <type_traits>
 
 #include "device.h"
@@ -134,7 +135,9 @@ __device__ __forceinline__ f32x16 qk_part(uint4 k, const Query6<2, false> &q, f3
 // Four waves per block; K codes and V values each have a two-slot ring of 64-key
 // tiles.  KSPLIT as in the attention over rows of 16 bits: 1: every wave takes whole
 // tiles for its 32 rows; 2: two groups of waves over the same rows, one for each half
-// of a tile's keys, merged at the end.
+// of a tile's keys, merged at the end.  (Tiles as loaded in a ring of four, three ahead
+// of the products, V converted from there: 8192 tokens over 16384 keys 2790 us against
+// 2682; no wave waits for memory as it is.)
 template <int KSPLIT, bool TREE>
 __device__ __forceinline__ void walk4(const WalkArgs &a, const WalkItem &it, uint8_t (*kring)[kKTile4], uint8_t (*vring)[kVTile4]) {
   constexpr int RW = kWaves4 / KSPLIT, RB = 32 * RW, NSB = 2 / KSPLIT;
@@ -267,7 +270,10 @@ __device__ __forceinline__ void walk4(const WalkArgs &a, const WalkItem &it, uin
   // j - 1, whose slot takes V of tile j + 1 from the registers that it was loaded to an
   // iteration ago.
   // AHEAD: tile j's scores were made an iteration ago, and tile j + 1's are made beside
-  // tile j's weights; K's codes are loaded two tiles ahead.
+  // tile j's weights; K's codes are loaded two tiles ahead.  Where a wave has half a tile's
+  // keys its chain is what a tile takes (43 prompts of up to 8 tokens over 800 to 6300 keys:
+  // 59.9 us, 52.7 ahead); with whole tiles two waves a SIMD fill each other's gaps and the
+  // registers of a second tile cost more (8192 over 16384: 2682, 2795 ahead).
   constexpr bool AHEAD = KSPLIT == 2;
   f32x16 Sc[AHEAD ? 2 : 1][NSB];
   uint32_t ksc[NSB];
@@ -320,7 +326,9 @@ __device__ __forceinline__ void walk4(const WalkArgs &a, const WalkItem &it, uin
 // bound by memory: the waves of a block share nothing but the merge at the end, and
 // each takes every fourth tile of the item with the next one's loads in flight
 // (8.7 KB a wave, 70 KB a compute unit).  Queries fill the 16-wide products: a tile's
-// scores are 16 to a lane, half of those of the 32-wide ones.
+// scores are 16 to a lane, half of those of the 32-wide ones.  32 single tokens over 256
+// to 16384 keys, 64 query heads over 8 (188 MB): 83.8 us as 64-row blocks, 41 so, 35 of
+// them the walk: 6.7 TB/s between the start (6 us) and the last blocks' end, then the merge.
 //   S^T: 16 keys x 128 columns a product.  A lane's operand is the codes of one group
 //        of its key, 16 bytes as they lie in memory, and that group's scale.
 //   O^T: V is converted as it arrives, through the wave's own 16 KB of LDS.  A product

@@ -320,18 +320,19 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a) {
 }
 
 // Rows of a 4-bit pool as values: a thread has eight columns of one head of K or V and
-// takes them for TB tokens.
+// takes them for TB tokens, one after another.  A token's chunks take `blocks` blocks, or
+// 1 << log2 threads of one that has several tokens' worth.
 template <bool BF16, int TB>
-__global__ __launch_bounds__(kThreads) void kv4_read_kernel(ReadArgs a, int blocks) {
+__global__ __launch_bounds__(kThreads) void kv4_read_kernel(ReadArgs a, int blocks, int log2) {
   const int cw = a.head_dim >> 3, d = a.head_dim;           // chunks of a row
   const int per = 2 * a.n_kv * cw;                          // and of a token
-  const int in = (int)(blockIdx.x % blocks) * kThreads + threadIdx.x;
-  const int tok0 = a.tok0 + (int)(blockIdx.x / blocks) * TB;
+  const int in = (int)(blockIdx.x % blocks) * kThreads + (threadIdx.x & ((1 << log2) - 1));
+  const int tok0 = a.tok0 + ((int)(blockIdx.x / blocks) * (kThreads >> log2) + (threadIdx.x >> log2)) * TB;
   const int x = min(in, per - 1), c = x % cw, head = x / cw;
   const bool v = head >= a.n_kv;
   const int hk = v ? head - a.n_kv : head;
   const uint8_t *const codes = (v ? a.v : a.k), *const scales = v ? a.vs : a.ks;
-  int s = find_seq(a.seq, a.nseq, tok0);
+  int s = find_seq(a.seq, a.nseq, min(tok0, a.tok1 - 1));
   uint32_t w[TB], byte[TB];
 #pragma unroll
   for (int n = 0; n < TB; ++n) {
@@ -452,14 +453,18 @@ hipError_t launch_append(int dt, bool four, AppendArgs &a, int cus, hipStream_t 
 
 hipError_t launch_kv4_read(int dt, const ReadArgs &a, int cus, hipStream_t st) {
   const int per = 2 * a.n_kv * (a.head_dim / 8), blocks = (per + kThreads - 1) / kThreads, toks = a.tok1 - a.tok0;
-  const bool many = (int64_t)blocks * toks >= 4 * 8 * cus;
-  const dim3 grid((uint32_t)blocks * (many ? (toks + 3) / 4 : toks)), block(kThreads);
+  int log2 = 8;
+  while (log2 > 0 && 1 << (log2 - 1) >= per) --log2;
+  const int tpb = kThreads >> log2;                         // tokens at once of a block
+  // four tokens a thread where that leaves every compute unit eight blocks
+  const int tb = (int64_t)blocks * toks >= (int64_t)4 * 8 * cus * tpb ? 4 : 1;
+  const dim3 grid((uint32_t)blocks * ((toks + tb * tpb - 1) / (tb * tpb))), block(kThreads);
   if (dt == 0) {
-    if (many) hipLaunchKernelGGL((kv4_read_kernel<false, 4>), grid, block, 0, st, a, blocks);
-    else hipLaunchKernelGGL((kv4_read_kernel<false, 1>), grid, block, 0, st, a, blocks);
+    if (tb == 4) hipLaunchKernelGGL((kv4_read_kernel<false, 4>), grid, block, 0, st, a, blocks, log2);
+    else hipLaunchKernelGGL((kv4_read_kernel<false, 1>), grid, block, 0, st, a, blocks, log2);
   } else {
-    if (many) hipLaunchKernelGGL((kv4_read_kernel<true, 4>), grid, block, 0, st, a, blocks);
-    else hipLaunchKernelGGL((kv4_read_kernel<true, 1>), grid, block, 0, st, a, blocks);
+    if (tb == 4) hipLaunchKernelGGL((kv4_read_kernel<true, 4>), grid, block, 0, st, a, blocks, log2);
+    else hipLaunchKernelGGL((kv4_read_kernel<true, 1>), grid, block, 0, st, a, blocks, log2);
   }
   return hipGetLastError();
 }

@@ -173,6 +173,10 @@ def test_attention():
     expect("E_ARG", prompt, scale=float("inf"))
     expect("E_BUDGET", prompt, off=(0, 1, 42))
     expect("E_BUDGET", prompt, prefix=sm.Prefix([0, 0], [5001, 0]))
+    for dt in (sm.BF16, sm.FP32):                                                      # 32-bit offsets within a slab and a prefix
+        expect("E_BUDGET", prompt, off=(0, 1), p=FakeKV4([10], [(1 << 23) + 1], [0]), dt=dt)
+        big = FakeKV4([10, 0], [40, 40], [1 << 24, (1 << 24) + 50])
+        expect("E_BUDGET", prompt, off=(0, 1, 2), p=big, dt=dt, prefix=sm.Prefix([0, 0], [(1 << 23) + 1] * 2))
     x = FakeKV4([5000, 0], [6000, 40], [0, 6000])
     x.k_scale = None
     expect("E_ARG", prompt, p=x)
