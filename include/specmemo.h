@@ -446,7 +446,8 @@ typedef struct {
  *   (y_a, y_b) <- (y_a cos - y_b sin, y_b cos + y_a sin), angle j < rot_dim / 2 of row
  *       pos[t]; HALVES: a = j, b = j + rot_dim / 2; PAIRS: a = 2 j, b = 2 j + 1
  *   q_out[t][head] = y;  slab row L_b + i of K = y, of V = v    (L_b = kv->seq_len_h[b])
- * in fp32, rounded once to `dt`.  A token whose position is outside [0, n_pos) writes
+ * in fp32 (sums of squares and their mean + eps within its normal range), rounded once
+ * to `dt`.  A token whose position is outside [0, n_pos) writes
  * nothing: its rows of q_out, K and V stay as they were.  All other rows of the pool
  * stay as they were.  The lengths are the caller's to advance; kv->seq_len is not read.
  * new_off_h: host [B+1], new_off_h[0] = 0, non-decreasing, 1 <= B <=

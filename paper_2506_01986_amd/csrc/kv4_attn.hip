@@ -273,7 +273,7 @@ __device__ __forceinline__ void walk4(const WalkArgs &a, const WalkItem &it, uin
   // tile j's weights; K's codes are loaded two tiles ahead.  Where a wave has half a tile's
   // keys its chain is what a tile takes (43 prompts of up to 8 tokens over 800 to 6300 keys:
   // 59.9 us, 52.7 ahead); with whole tiles two waves a SIMD fill each other's gaps and the
-  // registers of a second tile cost more (8192 over 16384: 2682, 2795 ahead).
+  // registers of a second tile cost more (8192 over 16384: 2708, 2795 ahead).
   constexpr bool AHEAD = KSPLIT == 2;
   f32x16 Sc[AHEAD ? 2 : 1][NSB];
   uint32_t ksc[NSB];

@@ -192,6 +192,35 @@ def test_codes(dtype):
         assert np.array_equal(out.cpu().double().numpy(), values(code, scale), equal_nan=True)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_keys_of_an_infinite_norm(dtype):
+    """A normed key with an infinity: its column and the one it turns with are NaN, all others x / inf = 0;
+    a NaN takes the whole row.  No tolerance: zeros and NaN are exact in both forms."""
+    x = Rows(dtype, 2, 1, 128, [4], [0], norm=True, rot=64, seed=4)
+    x.k[1, 0, 5], x.k[2, 0, 100], x.k[3, 0, 64] = np.inf, -np.inf, np.nan
+    rows, kv = x.upload(), x.pool4()
+    sm.kv4_append(x.dt, x.off, rows, kv, x.q_out)
+    torch.cuda.synchronize()
+    with np.errstate(invalid="ignore"):
+        want, _ = x.turned(x.k, x.k_norm)
+    code, scale = quantise(want.numpy())
+    assert (scale[1, 0] == 255).tolist() == [True, True, False, False]         # columns 5 and 37
+    assert (scale[2, 0] == 255).tolist() == [False, False, False, True] and (scale[3, 0] == 255).all()
+    got = kv.k_scale[:, x.dest.cuda()].transpose(0, 1).cpu().numpy()
+    assert np.array_equal(got, scale)
+    bits = unpack(kv.k[:, x.dest.cuda()].transpose(0, 1).cpu().numpy())
+    held = np.repeat(scale != 255, 32, -1)
+    held[0] = False                                                            # token 0 is as in test_append4
+    assert np.array_equal(bits[held] & 7, code[held] & 7) and not (bits[held] & 7).any()
+    # the same into a pool of the inputs' type
+    rows, kv = x.upload(), x.pool()
+    sm.kv_append(x.dt, x.off, rows, kv, x.q_out)
+    torch.cuda.synchronize()
+    got = kv.k[:, x.dest.cuda()].transpose(0, 1).cpu().double()
+    assert torch.equal(got[1:].isnan(), want[1:].isnan())
+    assert (got[1:][~want[1:].isnan()] == 0).all()
+
+
 def test_keys_next_to_borders():
     """Rotated keys within 2^-40 of a border fall on its right side: y_a = a cos - b sin with a cos on a border and b sin of
     either sign and next to nothing."""
