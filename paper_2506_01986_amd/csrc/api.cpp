@@ -1366,9 +1366,9 @@ int append_impl(int dt, int B, const int32_t *off, const specmemo_rows *x, int n
   if ((rc = check_kv(dt, kv, ti, off))) return rc;
   if ((rc = check_rows(dt, x, ti, n_q, kv, kv4, q_out))) return rc;
   AppendArgs a{};
-  a.kind[0] = AppendKind{x->q, x->q_norm, q_out, x->q_stride, n_q};
-  a.kind[1] = AppendKind{x->k, x->k_norm, kv->k, x->k_stride, kv->n_kv};
-  a.kind[2] = AppendKind{x->v, nullptr, kv->v, x->v_stride, kv->n_kv};
+  a.kind[kQueries] = AppendKind{x->q, x->q_norm, q_out, x->q_stride, n_q};
+  a.kind[kKeys] = AppendKind{x->k, x->k_norm, kv->k, x->k_stride, kv->n_kv};
+  a.kind[kValues] = AppendKind{x->v, nullptr, kv->v, x->v_stride, kv->n_kv};
   a.eps = x->eps;
   if (kv4) {
     a.ks = static_cast<uint8_t *>(kv4->k_scale);

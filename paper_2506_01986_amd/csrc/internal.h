@@ -257,7 +257,8 @@ struct RowsSeq {
   int32_t off, row0_lo, row0_hi;
 };
 constexpr int kMaxRowsSeq = 300;   // sequences of a launch
-struct AppendKind {               // query, key or value heads
+enum { kKeys, kQueries, kValues };   // kinds of heads, in the order of their blocks: the longest first
+struct AppendKind {
   const void *in;                 // token i's heads at i * stride elements
   const void *norm;               // [head_dim] or null
   void *out;                      // [tokens][n_q][head_dim], or the pool's rows or codes

@@ -9,7 +9,7 @@
 // for q and k; v is stored as it is.  Everything is one read of the inputs and one
 // write of the outputs: the kernels are bound by memory, or where there are few rows
 // by one launch's latency.  1024 tokens of 32 + 32 + 32 heads (50 MB) 8.2 us; 19k of 64 + 8 + 8
-// (722 MB, into 4 bits) 179 us: 4.0 TB/s; one tree 3.4 to 4.2 us.  Reading the
+// (722 MB, into 4 bits) 144 us: 5.0 TB/s; one tree 3.4 to 4.2 us.  Reading the
 // 4-bit rows of those 19k back (99 MB): 21 us.  Compaction, three dependent loads and a
 // store: 4.8 to 5.2 us whatever the batch.
 #include <algorithm>
@@ -54,12 +54,12 @@ __device__ __forceinline__ void unpack(float (&x)[E], uint4 w) {
   for (int i = 0; i < E; ++i) x[i] = E == 8 ? bf16_to_f32((uint16_t)(u[i >> 1] >> (16 * (i & 1)))) : __uint_as_float(u[i & 3]);
 }
 
-// fp64 -> fp32 with the last bit set where bits are lost: comparisons with numbers of
-// fewer bits (the borders between codes) come out as they would in 64 bits.
+// fp64 -> fp32, cut to 20 bits of fraction and the last of them set where any are lost:
+// comparisons with numbers of fewer bits (the borders between codes) come out as they
+// would in 64 bits.
 __device__ __forceinline__ float sticky_f32(double d) {
   const uint64_t u = __double_as_longlong(d);
-  const uint64_t cut = u & ~0x1FFFFFFFull;
-  return (float)__longlong_as_double((long long)(cut | (u != cut ? 0x20000000ull : 0ull)));
+  return (float)__longlong_as_double((long long)((uint64_t)((uint32_t)(u >> 32) | min((uint32_t)u, 1u)) << 32));
 }
 
 // Sum over the lph lanes of a head, in each of them: a row of 16 lanes by DPP, as in
@@ -231,11 +231,15 @@ __device__ __forceinline__ void store_row4(uint8_t *codes, uint8_t *scales, int 
 }
 
 // lph lanes have a head's row, and a block 256 / lph of them (slots).  A block has heads
-// of one kind (query, key, value), and its slots those of one token, or of several where
-// a token has few: 1 << log2 slots each, HB heads a slot with their loads together, so
-// that a lane loads cos, sin and the norm's weights once.  Rows that go to 4 bits: one a
-// slot, keys in fp64, so that a value next to a border between two codes falls on its
-// own side of it.
+// of one kind (keys, queries, values), and its slots those of one token, or of several
+// where a token has few: 1 << log2 slots each, HB heads a slot with their loads together,
+// so that a lane loads cos, sin and the norm's weights, and brings them to fp64, once.
+// Keys that go to 4 bits are normed and turned in fp64, so that a value next to a border
+// between two codes falls on its own side of it; they take longest and begin first.
+// 19k tokens of 64 + 8 + 8 heads into 4 bits: 179 us with one key or value head a slot,
+// 144 so; 8k of 32 + 32 + 32: 137, 84.  (fp32 with a bound on its error, and fp64 for the
+// rows of which a column's interval holds a border: 174 and 117, and 1024 tokens 17 us
+// against 11: the second way's registers and latency.)
 template <bool BF16, bool FOUR, int HB>
 __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a) {
   constexpr int E = BF16 ? 8 : 4, ES = BF16 ? 2 : 4;
@@ -245,26 +249,20 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a) {
   const int c = (threadIdx.x & (lph - 1)) * E, slots = 1 << K.log2;
   const uint32_t bid = blockIdx.x - K.block0, group = bid / (uint32_t)K.turns;
   const int at = a.tok0 + (int)group * (all >> K.log2) + (slot >> K.log2), tok = min(at, a.tok1 - 1);
-  const int hb = FOUR && kind != 0 ? 1 : HB;
-  const int h0 = (slot & (slots - 1)) + (int)(bid - group * K.turns) * hb * slots;
+  const int h0 = (slot & (slots - 1)) + (int)(bid - group * K.turns) * HB * slots;
   const bool on = at < a.tok1, has = on && c < d;
   const char *const src = static_cast<const char *>(K.in) + (K.stride * tok + (int64_t)h0 * d + c) * ES;
   const int step = slots * d * ES;
-  if (!FOUR || kind == 0) {
-    uint4 row[HB];
+  uint4 row[HB];
 #pragma unroll
-    for (int n = 0; n < HB; ++n) row[n] = ld16_or_zero(has && h0 + n * slots < K.heads, src + (int64_t)n * step);
-    const Lane<E> l(a, lph, tok, on);
-    char *dst;
-    int64_t out_step;
-    if (kind == 0) {
-      dst = static_cast<char *>(K.out) + (((int64_t)tok * a.n_q + h0) * d + c) * ES;
-      out_step = step;
-    } else {
-      dst = static_cast<char *>(K.out) + ((h0 * a.cap_total + pool_row(a.seq, a.nseq, tok)) * d + c) * ES;
-      out_step = a.cap_total * step;
-    }
-    if (kind == 2) {
+  for (int n = 0; n < HB; ++n) row[n] = ld16_or_zero(has && h0 + n * slots < K.heads, src + (int64_t)n * step);
+  const Lane<E> l(a, lph, tok, on);
+  const int64_t row0 = kind == kQueries ? (int64_t)tok * a.n_q + h0 : h0 * a.cap_total + pool_row(a.seq, a.nseq, tok);
+  const int64_t row_step = kind == kQueries ? slots : a.cap_total * slots;
+  if (!FOUR || kind == kQueries) {
+    char *const dst = static_cast<char *>(K.out) + (row0 * d + c) * ES;
+    const int64_t out_step = row_step * d * ES;
+    if (kind == kValues) {
 #pragma unroll
       for (int n = 0; n < HB; ++n)
         if (l.live && h0 + n * slots < K.heads) store16(dst + n * out_step, row[n].x, row[n].y, row[n].z, row[n].w);
@@ -283,6 +281,7 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a) {
     }
 #pragma unroll
     for (int n = 0; n < HB; ++n) {
+      if (h0 + n * slots >= K.heads) break;
       float x[E], y[E];
       unpack(x, row[n]);
       l.other(y, x, row[n], lph);
@@ -293,34 +292,54 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a) {
         if (l.turns) x[i] = fmaf(y[i], fy[i], x[i]);
         if (K.norm) x[i] *= r;
       }
-      if (l.live && h0 + n * slots < K.heads) store_row(dst + n * out_step, x);
+      if (l.live) store_row(dst + n * out_step, x);
     }
     return;
   }
-  const uint4 row = ld16_or_zero(has && h0 < K.heads, src);
-  const Lane<E> l(a, lph, tok, on);
-  const bool put = l.live && h0 < K.heads;
-  const int64_t r = h0 * a.cap_total + pool_row(a.seq, a.nseq, tok);
-  float v[E];
-  unpack(v, row);
-  if (kind == 2) {
-    store_row4(static_cast<uint8_t *>(K.out) + r * (d / 2), a.vs + r * (d / kKv4Group), c, v, put);
+  uint8_t *const codes = static_cast<uint8_t *>(K.out) + row0 * (d / 2);
+  uint8_t *const scales = (kind == kKeys ? a.ks : a.vs) + row0 * (d / kKv4Group);
+  const int64_t code_step = row_step * (d / 2), scale_step = row_step * (d / kKv4Group);
+  if (kind == kValues) {
+#pragma unroll
+    for (int n = 0; n < HB; ++n) {
+      if (h0 + n * slots >= K.heads) break;
+      float x[E];
+      unpack(x, row[n]);
+      store_row4(codes + n * code_step, scales + n * scale_step, c, x, l.live);
+    }
     return;
   }
-  float co[E], si[E], wx[E], wy[E];
-  l.angles(a, co, si);
-  if (K.norm) l.weights(wx, wy, K.norm, d);
-  float y[E];
-  l.other(y, v, row, lph);
-  const double n = K.norm ? row_norm(v, a.eps, 1.0 / d, lph) : 1.0;
+  double fx[E], fy[E];                // products of two fp32 numbers: exact
+  {
+    float co[E], si[E], wx[E], wy[E];
+    l.angles(a, co, si);
+    if (K.norm) l.weights(wx, wy, K.norm, d);
 #pragma unroll
-  for (int i = 0; i < E; ++i) {
-    double x = v[i];
-    if (K.norm) x *= n * wx[i];
-    if (l.turns) x = x * co[i] + (K.norm ? y[i] * (n * wy[i]) : (double)y[i]) * si[i];
-    v[i] = sticky_f32(x);
+    for (int i = 0; i < E; ++i) {
+      fx[i] = co[i];
+      fy[i] = si[i];
+      if (K.norm) {
+        fx[i] *= wx[i];
+        fy[i] *= wy[i];
+      }
+    }
   }
-  store_row4(static_cast<uint8_t *>(K.out) + r * (d / 2), a.ks + r * (d / kKv4Group), c, v, put);
+#pragma unroll
+  for (int n = 0; n < HB; ++n) {
+    if (h0 + n * slots >= K.heads) break;
+    float x[E], y[E];
+    unpack(x, row[n]);
+    l.other(y, x, row[n], lph);
+    const double r = K.norm ? row_norm(x, a.eps, 1.0 / d, lph) : 1.0;
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+      double v = x[i] * fx[i];
+      if (l.turns) v = fma((double)y[i], fy[i], v);
+      if (K.norm) v *= r;
+      x[i] = sticky_f32(v);
+    }
+    store_row4(codes + n * code_step, scales + n * scale_step, c, x, l.live);
+  }
 }
 
 // Rows of a 4-bit pool as values: a thread has eight columns of one head of K or V and
@@ -422,21 +441,18 @@ void append(AppendArgs &a, int cus, hipStream_t st) {
   while ((BF16 ? 8 : 4) << a.lph_log2 < a.head_dim) ++a.lph_log2;
   a.inv_d = 1.f / (float)a.head_dim;
   const int all = kThreads >> a.lph_log2, toks = a.tok1 - a.tok0;
-  // heads a slot: as many as there are, and as leave every compute unit four blocks
-  int64_t slots = 0;
-  int most = 1;
-  for (AppendKind &k : a.kind) {
-    k.log2 = 0;
-    while (1 << k.log2 < std::min(k.heads, all)) ++k.log2;
-    most = std::max(most, (k.heads + (1 << k.log2) - 1) >> k.log2);
-    slots += (int64_t)toks * k.heads;
-  }
-  const int64_t blocks = slots / all;
-  const int hb = most >= 4 && blocks >= 4 * 4 * cus ? 4 : most >= 2 && blocks >= 2 * 4 * cus ? 2 : 1;
+  // heads a slot: as many as there are, and as leave every compute unit two blocks (256
+  // tokens of 32 + 32 + 32 heads into 4 bits: 5.4 us with two a slot, 6.6 with one or
+  // four; 1024 of 64 + 8 + 8: 11.2 with four, 12.8 with two)
+  const int64_t blocks = (int64_t)toks * (a.kind[kQueries].heads + a.kind[kKeys].heads + a.kind[kValues].heads) / all;
+  const int most = std::max(a.kind[kQueries].heads, a.kind[kKeys].heads);
+  const int hb = most >= 4 && blocks >= 4 * 2 * cus ? 4 : most >= 2 && blocks >= 2 * 2 * cus ? 2 : 1;
   uint32_t block = 0;
   for (int i = 0; i < 3; ++i) {
     AppendKind &k = a.kind[i];
-    const int per = (FOUR && i != 0 ? 1 : hb) << k.log2;
+    k.log2 = 0;
+    while (hb << k.log2 < k.heads && 1 << k.log2 < all) ++k.log2;
+    const int per = hb << k.log2;
     k.turns = std::max(1, (k.heads + per - 1) / per);
     k.block0 = block;
     if (k.heads > 0) block += (uint32_t)((toks + (all >> k.log2) - 1) / (all >> k.log2)) * k.turns;

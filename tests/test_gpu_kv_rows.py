@@ -155,6 +155,44 @@ def test_append4(name):
         assert torch.equal(out.cpu().double(), torch.from_numpy(values(code, scale)))
 
 
+# as many rows as let a slot have two heads or four, some slots with fewer (a block's 8 or 16 slots times twice or four
+# times 512 blocks of rows)
+LARGE = {
+    "two_heads_7_of_3": ("bf16", 7, 3, 128, [800, 0, 1, 699], [3, 1, 0, 2], dict(norm=True)),
+    "four_heads_7_of_3": ("bf16", 7, 3, 128, [1500, 0, 1, 1100], [3, 1, 0, 2], dict(norm=True, fused=True)),
+    "four_heads_5_of_1": ("bf16", 5, 1, 128, [4999, 1], [0, 700], dict(rot=80, style="pairs")),
+    "keys_alone": ("bf16", 0, 9, 128, [1900], [1], dict(norm=True)),
+    "fp32_6_of_2": ("fp32", 6, 2, 96, [1000, 3, 700], [0, 5, 1], dict(norm=True, style="pairs", fused=True)),
+    "fp32_9_of_9": ("fp32", 9, 9, 64, [1300], [7], dict(rot=40, norm=True)),
+}
+
+
+@pytest.mark.parametrize("name", list(LARGE))
+def test_append_large(name):
+    *a, opts = LARGE[name]
+    x = Rows(*a, seed=len(name), **opts)
+    rows, kv = x.upload(), x.pool()
+    sm.kv_append(x.dt, x.off, rows, kv, x.q_out)
+    torch.cuda.synchronize()
+    check(x.q_out, *x.turned(x.q, x.q_norm))
+    x.check_pool(kv.k, *x.turned(x.k, x.k_norm))
+    x.check_pool(kv.v, x.v)
+
+
+@pytest.mark.parametrize("name", list(LARGE))
+def test_append4_large(name):
+    *a, opts = LARGE[name]
+    x = Rows(*a, seed=len(name), **opts)
+    rows, kv = x.upload(), x.pool4()
+    sm.kv4_append(x.dt, x.off, rows, kv, x.q_out)
+    torch.cuda.synchronize()
+    check(x.q_out, *x.turned(x.q, x.q_norm))
+    for y, codes, scales in ((x.turned(x.k, x.k_norm)[0], kv.k, kv.k_scale), (x.v.double(), kv.v, kv.v_scale)):
+        code, scale = quantise(y.numpy())
+        x.check_pool(scales, torch.from_numpy(scale))
+        x.check_pool(codes, torch.from_numpy(pack(code)))
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 def test_codes(dtype):
     """Values on and beside every border between codes, at every scale; groups of zeros, of the smallest and largest numbers,
