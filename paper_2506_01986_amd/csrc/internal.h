@@ -257,6 +257,17 @@ struct RowsSeq {
   int32_t off, row0_lo, row0_hi;
 };
 constexpr int kMaxRowsSeq = 300;   // sequences of a launch
+// The i-th token of a launch over tokens [tok0, tok1), and whether there is one; past the
+// end the last stands in.  A block's spare threads lie up to 255 tokens past tok1, which
+// may be 2^31 - 1: i counts from tok0, so that nothing passes 32 bits.
+struct RowsToken {
+  int tok;
+  bool on;
+};
+__host__ __device__ inline RowsToken rows_token(int tok0, int tok1, int i) {
+  const int n = tok1 - tok0;
+  return RowsToken{tok0 + (i < n ? i : n - 1), i < n};
+}
 enum { kKeys, kQueries, kValues };   // kinds of heads, in the order of their blocks: the longest first
 struct AppendKind {
   const void *in;                 // token i's heads at i * stride elements

@@ -248,9 +248,10 @@ __global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a) {
   const int lph = 1 << a.lph_log2, d = a.head_dim, all = kThreads >> a.lph_log2, slot = threadIdx.x >> a.lph_log2;
   const int c = (threadIdx.x & (lph - 1)) * E, slots = 1 << K.log2;
   const uint32_t bid = blockIdx.x - K.block0, group = bid / (uint32_t)K.turns;
-  const int at = a.tok0 + (int)group * (all >> K.log2) + (slot >> K.log2), tok = min(at, a.tok1 - 1);
+  const RowsToken at = rows_token(a.tok0, a.tok1, (int)group * (all >> K.log2) + (slot >> K.log2));
+  const int tok = at.tok;
   const int h0 = (slot & (slots - 1)) + (int)(bid - group * K.turns) * HB * slots;
-  const bool on = at < a.tok1, has = on && c < d;
+  const bool on = at.on, has = on && c < d;
   const char *const src = static_cast<const char *>(K.in) + (K.stride * tok + (int64_t)h0 * d + c) * ES;
   const int step = slots * d * ES;
   uint4 row[HB];
@@ -350,16 +351,16 @@ __global__ __launch_bounds__(kThreads) void kv4_read_kernel(ReadArgs a, int bloc
   const int cw = a.head_dim >> 3, d = a.head_dim;           // chunks of a row
   const int per = 2 * a.n_kv * cw;                          // and of a token
   const int in = (int)(blockIdx.x % blocks) * kThreads + (threadIdx.x & ((1 << log2) - 1));
-  const int tok0 = a.tok0 + ((int)(blockIdx.x / blocks) * (kThreads >> log2) + (threadIdx.x >> log2)) * TB;
+  const int tok0 = ((int)(blockIdx.x / blocks) * (kThreads >> log2) + (threadIdx.x >> log2)) * TB;   // of the launch's
   const int x = min(in, per - 1), c = x % cw, head = x / cw;
   const bool v = head >= a.n_kv;
   const int hk = v ? head - a.n_kv : head;
   const uint8_t *const codes = (v ? a.v : a.k), *const scales = v ? a.vs : a.ks;
-  int s = find_seq(a.seq, a.nseq, min(tok0, a.tok1 - 1));
+  int s = find_seq(a.seq, a.nseq, rows_token(a.tok0, a.tok1, tok0).tok);
   uint32_t w[TB], byte[TB];
 #pragma unroll
   for (int n = 0; n < TB; ++n) {
-    const int tok = min(tok0 + n, a.tok1 - 1);
+    const int tok = rows_token(a.tok0, a.tok1, tok0 + n).tok;
     while (s + 1 < a.nseq && a.seq[s + 1].off <= tok) ++s;
     const int64_t r = (int64_t)hk * a.cap_total + (int64_t)((uint64_t)(uint32_t)a.seq[s].row0_hi << 32 | (uint32_t)a.seq[s].row0_lo) + tok;
     w[n] = *reinterpret_cast<const uint32_t *>(codes + r * (d >> 1) + 4 * c);
@@ -368,10 +369,11 @@ __global__ __launch_bounds__(kThreads) void kv4_read_kernel(ReadArgs a, int bloc
   if (in >= per) return;
 #pragma unroll
   for (int n = 0; n < TB; ++n) {
-    if (tok0 + n >= a.tok1) return;
+    const RowsToken t = rows_token(a.tok0, a.tok1, tok0 + n);
+    if (!t.on) return;
     const bool nan = byte[n] == kKv4Nan;
     const float unit = kv4_scale(byte[n]);
-    const int64_t o = ((int64_t)(tok0 + n) * a.n_kv + hk) * d + 8 * c;
+    const int64_t o = ((int64_t)t.tok * a.n_kv + hk) * d + 8 * c;
     void *const out = v ? a.v_out : a.k_out;
     if constexpr (BF16) {
       const uint4 y = kv4_bf16x8(w[n], unit);
