@@ -614,9 +614,11 @@ def _append(fn, dt: int, new_off, rows: QKVRows, kv, q_out, stream):
 
 
 def kv_append(dt: int, new_off, rows: QKVRows, kv: KVPool, q_out, stream=None):
-    for x in (kv.k, kv.v):      # written in the rows' type, as they lie
-        if x.dtype is not rows.k.dtype or not x.is_contiguous():
-            raise ValueError(f"a pool of {rows.k.dtype} without gaps expected, got {x.dtype} of strides {x.stride()}")
+    values = kv.n_kv * kv.cap_total * kv.head_dim
+    for x in (kv.k, kv.v):      # written in the rows' type, as they lie, up to the last row
+        if x.dtype is not rows.k.dtype or not x.is_contiguous() or x.numel() != values:
+            raise ValueError(f"a pool of {values} values of {rows.k.dtype} without gaps expected, got {tuple(x.shape)} of {x.dtype}, "
+                             f"strides {x.stride()}")
     _append(load().specmemo_kv_append, dt, new_off, rows, kv, q_out, stream)
 
 
