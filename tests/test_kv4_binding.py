@@ -20,3 +20,25 @@ def test_values_beside_keys(v):
     kv.k = kv.v = bf(2, 29, 128)                  # cap_total says 30
     with pytest.raises(ValueError):
         sm.kv_append(sm.BF16, [0, 5], x, kv, None)
+
+
+def pool4(n=1):
+    u8 = lambda *s: torch.zeros(*s, dtype=torch.uint8)
+    return sm.KV4Pool(u8(2, 30, 64), u8(2, 30, 64), u8(2, 30, 4), u8(2, 30, 4), i32(n), [0] * n, [20] * n, [3] * n)
+
+
+FUSED = bf(5, 4 + 2 + 2, 128)
+BAD = [torch.zeros(5, 4, 128), bf(4, 4, 128), FUSED[:, :4], bf(4, 5, 128).transpose(0, 1), bf(5, 128, 4).transpose(1, 2)]
+TREES = sm.Trees([0, 5], [-1, 0, 0, 1, 1], [0, 1, 1, 2, 2], [0, 0, 1, 0, 1], dev_arrays=[i32(5)] * 4)
+CALLS = {"prompt": lambda q, out: sm.kv4_prompt_attn(sm.BF16, [0, 5], pool4(), 4, q, out),
+         "tree": lambda q, out: sm.kv4_tree_attn(sm.BF16, TREES, pool4(), 4, q, out)}
+
+
+@pytest.mark.parametrize("bad", range(len(BAD)))
+@pytest.mark.parametrize("call", list(CALLS))
+def test_attention_tensors(call, bad):
+    """Queries and outputs of another type, too few, or with gaps (queries as a slice of a fused row)."""
+    with pytest.raises(ValueError):
+        CALLS[call](BAD[bad], bf(5, 4, 128))
+    with pytest.raises(ValueError):
+        CALLS[call](bf(5, 4, 128), BAD[bad])
