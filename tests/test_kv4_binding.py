@@ -42,3 +42,26 @@ def test_attention_tensors(call, bad):
         CALLS[call](BAD[bad], bf(5, 4, 128))
     with pytest.raises(ValueError):
         CALLS[call](bf(5, 4, 128), BAD[bad])
+
+
+@pytest.mark.parametrize("name,bad", [("accept_len", i32(1)), ("accept_len", torch.zeros(2, dtype=torch.int64)), ("accept_len", i32(4)[::2]),
+                                      ("path", i32(11)), ("path", torch.zeros(2, 6, dtype=torch.int64)), ("path", i32(6, 2).t()),
+                                      ("path", i32(2, 8)[:, :6]), ("seq_len", i32(1))])
+def test_compaction_tensors(name, bad):
+    """Accepted lengths, paths and the pool's lengths: 32-bit integers, as many as the call reads or writes."""
+    trees = sm.Trees([0, 2, 4], [-1, 0] * 2, [0, 1] * 2, [0, 0] * 2, dev_arrays=[i32(4)] * 4)
+    kv = pool4(2)
+    kv.seq_base_h[1] = 10
+    kv.seq_cap_h[:] = 10
+    f = dict(accept_len=i32(2), path=i32(2, 6), seq_len=i32(2))
+    f[name] = bad
+    kv.seq_len = f["seq_len"]
+    with pytest.raises(ValueError):
+        sm.kv4_compact(trees, kv, f["accept_len"], f["path"], 6)
+
+
+def test_type_of_a_pool_s_lengths():
+    u8 = lambda *s: torch.zeros(*s, dtype=torch.uint8)
+    for bad in (torch.zeros(1), torch.zeros(1, dtype=torch.int64), i32(4)[::2]):
+        with pytest.raises(ValueError):
+            sm.KV4Pool(u8(2, 30, 64), u8(2, 30, 64), u8(2, 30, 4), u8(2, 30, 4), bad, [0], [20], [3])
