@@ -675,13 +675,20 @@ def kv4_prompt_attn(dt: int, new_off, kv: KV4Pool, n_q: int, q, out, prefix: Opt
                                            n_q, scale, q_at, out_at, _ptr(ws), ws_bytes, _stream(stream)))
 
 
+def _check_sequences(trees: Trees, kv: KV4Pool):
+    if trees.B > len(kv.seq_base_h) or trees.B > len(kv.seq_cap_h) or trees.B > len(kv.seq_len_h):
+        raise ValueError(f"{trees.B} trees for a pool of {min(len(kv.seq_base_h), len(kv.seq_cap_h), len(kv.seq_len_h))} sequences")
+
+
 def kv4_tree_attn_bytes(dt: int, trees: Trees, kv: KV4Pool, n_q: int, prefix: Optional[Prefix] = None) -> int:
+    _check_sequences(trees, kv)
     ts, ks = trees.struct(), kv.struct()
     return int(load().specmemo_kv4_tree_attn_bytes(dt, C.byref(ts), C.byref(ks), _prefix_ref(prefix, trees.B), n_q))
 
 
 def kv4_tree_attn(dt: int, trees: Trees, kv: KV4Pool, n_q: int, q, out, prefix: Optional[Prefix] = None, scale: float = 0.0,
                   ws=None, ws_bytes: int = 0, stream=None):
+    _check_sequences(trees, kv)
     ts, ks = trees.struct(), kv.struct()
     q_at, out_at = _q_and_out(dt, q, out, trees.node_off_h.item(-1) * n_q * kv.head_dim)
     _check(load().specmemo_kv4_tree_attn(dt, C.byref(ts), C.byref(ks), _prefix_ref(prefix, trees.B), n_q, scale, q_at, out_at,
@@ -707,6 +714,7 @@ def _compact_integers(B: int, seq_len, accept_len, path, path_stride: int):
 
 
 def kv4_compact(trees: Trees, kv: KV4Pool, accept_len, path, path_stride: int, stream=None):
+    _check_sequences(trees, kv)
     ts, ks = trees.struct(), kv.struct()
     _compact_integers(trees.B, kv.seq_len, accept_len, path, path_stride)
     _check(load().specmemo_kv4_compact(C.byref(ts), C.byref(ks), _ptr(accept_len), _ptr(path), path_stride, _stream(stream)))

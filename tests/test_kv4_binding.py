@@ -65,3 +65,17 @@ def test_type_of_a_pool_s_lengths():
     for bad in (torch.zeros(1), torch.zeros(1, dtype=torch.int64), i32(4)[::2]):
         with pytest.raises(ValueError):
             sm.KV4Pool(u8(2, 30, 64), u8(2, 30, 64), u8(2, 30, 4), u8(2, 30, 4), bad, [0], [20], [3])
+
+
+@pytest.mark.parametrize("short", ["seq_base_h", "seq_cap_h", "seq_len_h"])
+def test_more_trees_than_sequences(short):
+    """The pool's host arrays have an entry for every tree."""
+    trees = sm.Trees([0, 2, 4], [-1, 0] * 2, [0, 1] * 2, [0, 0] * 2, dev_arrays=[i32(4)] * 4)
+    kv = pool4(2)
+    setattr(kv, short, getattr(kv, short)[:1])
+    with pytest.raises(ValueError):
+        sm.kv4_tree_attn_bytes(sm.BF16, trees, kv, 4)
+    with pytest.raises(ValueError):
+        sm.kv4_tree_attn(sm.BF16, trees, kv, 4, bf(4, 4, 128), bf(4, 4, 128))
+    with pytest.raises(ValueError):
+        sm.kv4_compact(trees, kv, i32(2), i32(2, 6), 6)
