@@ -157,4 +157,13 @@ __device__ __forceinline__ void lds_load16(const void *src, uint32_t off, uint32
 // outstanding vector memory operation) and so shorten the prefetch distance.
 __device__ __forceinline__ void ring_barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
 
+// Between a wave's stores to LDS and its other lanes' loads of them (or the other way
+// round).  The LDS takes a wave's operations in order, so no instruction comes of it; it
+// tells the compiler, which sees one lane's accesses alone, to keep that order.
+__device__ __forceinline__ void wave_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
 }  // namespace specmemo

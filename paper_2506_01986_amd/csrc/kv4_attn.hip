@@ -504,6 +504,7 @@ __device__ __forceinline__ void walk4_few(const WalkArgs &a, const WalkItem &it,
           p1 -= __uint_as_float(u & 0xFFFF0000u);
         }
       }
+    wave_fence();                         // V: from the lanes that converted it to those that multiply
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
       if (!F32) {
@@ -524,6 +525,7 @@ __device__ __forceinline__ void walk4_few(const WalkArgs &a, const WalkItem &it,
           O[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, __builtin_bit_cast(bf16x8, uint4{pk[w][b][0], pk[w][b][1], pk[w][b][2], pk[w][b][3]}), O[i], 0, 0, 0);
       }
     }
+    wave_fence();                         // the next tile, or the parts, take V's place
   }
 
   // The waves' parts: O[i] of a lane is columns 16 i + 4 G .. + 3 of row q16.
