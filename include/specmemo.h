@@ -500,9 +500,9 @@ int specmemo_kv4_read(specmemo_dtype dt, int32_t B, const int32_t *new_off_h, co
  * bytes stand for.  Same arguments and workspace rules; head_dim is a multiple of 32, and
  * slabs and prefixes have at most 2^23 rows in either type.  q must be finite, and the
  * groups that a call walks too (scale bytes 2 .. 252).  Scores are sums in fp32 of the
- * query's products with the 4-bit keys.  bf16: columns of magnitude below 2^-8 of the
- * largest of their 32 are taken within 2^-16 of it, and the weights' rounding is that of
- * specmemo_prompt_attn.  fp32: columns are taken within 2^-23.9 of the largest of their
+ * query's products with the 4-bit keys.  bf16: columns of magnitude below 2^-7 of the
+ * largest of their 32 are taken within 2^-14.9 of it, and the weights' rounding is that
+ * of specmemo_prompt_attn.  fp32: columns are taken within 2^-23.9 of the largest of their
  * 32, weights in 24 bits. */
 int specmemo_kv4_prompt_attn(specmemo_dtype dt, int32_t B, const int32_t *new_off_h, const specmemo_kv4 *kv,
                              const specmemo_prefix *prefix, int32_t n_q, float scale, const void *q, void *out,

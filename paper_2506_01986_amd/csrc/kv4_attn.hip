@@ -49,8 +49,11 @@ typedef float f32x32_t __attribute__((ext_vector_type(32)));
 // columns: step s takes group (4 / STEPS) s + h of a lane's row.  A query is the sum of
 // its parts, each of six bits (sign, two of exponent, three of mantissa: steps of 1/8
 // under 2, 1/4 under 4, 1/2 up to 7.5) times 2^(e - shift), the rest of the one before:
-//   bf16  3 parts, shifts 0, 4, 10: every value down to 2^-8 of the 32 columns' largest
-//         (which lies in (3.75, 7.5] x 2^e), smaller ones within 2^-16 of it
+//   bf16  3 parts, shifts 0, 4, 10: values of at least 2^-5 x 2^e are exact, smaller ones
+//         leave up to 4 units of the last part and 1/8 of one at most in the end; the 32
+//         columns' largest lies in (3.75, 7.5] x 2^e, so those are 2^-7 and 2^-14.9 of it
+//         (shifts 0, 5, 10 with a largest under 4.25 would give 2^-15.1; a fourth part
+//         2^-20.9, for a third more of the scores' products)
 //   fp32  5 parts, shifts 0, 4, 9, 14, 19: a rest is at most 4 units of the next part and
 //         leaves 1/8 of one, 2^-22 in the end: within 2^-23.9 of the largest
 // Scale byte p % 4 of sc[s][p / 4] is part p's.
