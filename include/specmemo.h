@@ -503,7 +503,8 @@ int specmemo_kv4_read(specmemo_dtype dt, int32_t B, const int32_t *new_off_h, co
  * query's products with the 4-bit keys.  bf16: columns of magnitude below 2^-7 of the
  * largest of their 32 are taken within 2^-14.9 of it, and the weights' rounding is that
  * of specmemo_prompt_attn.  fp32: columns are taken within 2^-23.9 of the largest of their
- * 32, weights in 24 bits. */
+ * 32, weights in 24 bits.  A largest under 2^-101 counts as 2^-101 in this: columns far
+ * below that are taken as 0, whatever the keys and the scale. */
 int specmemo_kv4_prompt_attn(specmemo_dtype dt, int32_t B, const int32_t *new_off_h, const specmemo_kv4 *kv,
                              const specmemo_prefix *prefix, int32_t n_q, float scale, const void *q, void *out,
                              void *ws, size_t ws_bytes, void *stream);

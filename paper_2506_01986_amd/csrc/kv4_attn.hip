@@ -103,7 +103,8 @@ struct Query6 {
       float top = 0.f;
 #pragma unroll
       for (int i = 0; i < 16; ++i) top = fmaxf(fmaxf(top, fabsf(even[i])), fabsf(odd[i]));
-      // 7.5 = 1.875 x 4; magnitudes under 2^-103 are lost (scores of nothing)
+      // 7.5 = 1.875 x 4; a largest of 3.75 x 2^-103 or less is taken as that (scale bytes of all
+      // parts stay normal numbers), so that columns far below it come out as 0
       const uint32_t u = __float_as_uint(top);
       const uint32_t e = max((int)(u >> 23) - 2 + ((u & 0x7FFFFFu) > 0x700000u), 24);
 #pragma unroll

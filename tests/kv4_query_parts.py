@@ -15,11 +15,13 @@ SIX_BITS = np.concatenate([np.arange(16) / 8, 2 + np.arange(8) / 4, 4 + np.arang
 
 
 def stated():
-    """bf16: (columns from 2^-a of the largest up are exact, others within 2^-b of it), fp32: within 2^-b of it."""
+    """(columns from this much of the largest up are exact, others within this much of it, the least that it counts as)"""
     text = re.sub(r"\s+\*?\s*", " ", open(sm.HEADER).read())
     a, b = re.search(r"columns of magnitude below 2\^-([\d.]+) of the largest of their 32 are taken within 2\^-([\d.]+) of it", text).groups()
     c = re.search(r"fp32: columns are taken within 2\^-([\d.]+) of the largest of their 32", text).group(1)
-    return {"bf16": (2.0 ** -float(a), 2.0 ** -float(b)), "fp32": (np.inf, 2.0 ** -float(c))}
+    least = re.search(r"A largest under 2\^-([\d.]+) counts as 2\^-\1 in this", text)
+    least = 2.0 ** -float(least.group(1)) if least else 0.0
+    return {"bf16": (2.0 ** -float(a), 2.0 ** -float(b), least), "fp32": (np.inf, 2.0 ** -float(c), least)}
 
 
 def rest(x, shifts):

@@ -10,8 +10,8 @@ pytestmark = pytest.mark.gpu
 
 
 def parity(dtype, x):
-    exact, within = stated()[dtype]
-    top = x.top
+    exact, within, least = stated()[dtype]
+    top = np.maximum(x.top, least)
     s, tol = x.scores()
     bound = np.where(np.abs(x.x) >= exact * top, 0, within * top) * x.scale + tol
     off = np.abs(s - x.x * x.scale)
@@ -31,3 +31,11 @@ def test_bf16(T, far):
 @pytest.mark.parametrize("T", [4, 50])
 def test_fp32(T, d, far):
     parity("fp32", Columns("fp32", T, 3, 4, d, far, seed=far))
+
+
+@pytest.mark.parametrize("dtype,d", [("bf16", 128), ("fp32", 96)])
+@pytest.mark.parametrize("top", [120, 60, -60, -101, -104, -108, -112, -118])
+@pytest.mark.parametrize("T", [4, 50])
+def test_far_columns(dtype, d, top, T):
+    """Columns of every magnitude, the scale to match."""
+    parity(dtype, Columns(dtype, T, 4, 4, d, 6, top_exp=top, seed=T))

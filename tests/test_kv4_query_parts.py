@@ -22,7 +22,7 @@ def test_shifts_are_the_kernel_s():
 
 
 def test_bf16():
-    exact, within = stated()["bf16"]
+    exact, within, _ = stated()["bf16"]
     x = bf16_magnitudes(-30, 3)
     x = x[x <= 7.5]
     left = rest(x, SHIFTS["bf16"])
@@ -36,7 +36,7 @@ def test_bf16():
 
 
 def test_fp32():
-    _, within = stated()["fp32"]
+    _, within, _ = stated()["fp32"]
     r = np.random.default_rng(0)
     x = (r.uniform(1, 2, 1 << 20) * 2.0 ** r.integers(-30, 3, 1 << 20)).astype(np.float32)
     x = x[x <= 7.5]
@@ -44,3 +44,11 @@ def test_fp32():
     small = np.concatenate([x[x <= 3.75], np.float32([3.75])])
     assert (rest(small, SHIFTS["fp32"]) <= within * 3.75).all()          # any largest is above 3.75 units
     assert (left <= within * np.maximum(x, 3.75)).all()
+
+
+def test_the_least_largest():
+    """The kernel's least unit of the first part, 2^-103, is that of a largest just above 3.75 x 2^-103."""
+    text = open(os.path.join(CSRC, "kv4_attn.hip")).read()
+    assert "(u & 0x7FFFFFu) > 0x700000u), 24);" in text and 24 - 127 == -103
+    for _, _, least in stated().values():
+        assert 3.75 * 2.0 ** -103 <= least <= 4 * 2.0 ** -103
