@@ -484,10 +484,12 @@ typedef struct {
 int64_t specmemo_mem_kv4_bytes(int32_t layers, int32_t batch, int32_t n_kv, int32_t head_dim, int64_t tokens);
 
 /* specmemo_kv_append into a 4-bit pool.  A group's E is the least in [-125, 125] for
- * which no magnitude passes 7 x 2^E, and every value becomes the nearest of the group's,
- * ties to the even code.  Keys are normed and rotated in fp64, so that the code is that
- * of the exact value; q_out is as in specmemo_kv_append.  A group with an infinity, a
- * NaN or a magnitude past fp32's range gets the scale byte 255 (all its values are NaN). */
+ * which no magnitude passes 7 x 2^E (125 also where one does that is under 2^128: it
+ * becomes 6 x 2^125), and every value becomes the nearest of the group's, ties to the
+ * even code.  Keys are normed and rotated in fp64, and the code is that of the result: of
+ * an exact value nearer to a border between two codes than 2^-48 of its terms it may be
+ * either side's.  q_out is as in specmemo_kv_append.  A group with an infinity, a NaN or a
+ * magnitude of 2^128 or more gets the scale byte 255 (all its values are NaN). */
 int specmemo_kv4_append(specmemo_dtype dt, int32_t B, const int32_t *new_off_h, const specmemo_rows *x, int32_t n_q,
                         const specmemo_kv4 *kv, void *q_out, void *stream);
 
