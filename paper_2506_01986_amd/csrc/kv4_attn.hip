@@ -17,8 +17,8 @@
 //   O^T = V^T P^T V is contracted over keys, whose scales differ, so a tile is
 //                 converted to bf16 once (by the block's four waves, on its way to LDS)
 //                 and read by the transposing loads.
-// 8192 tokens over 16384 keys, 64 query heads over 8 (3.3 TFLOP): 2.6 to 2.7 ms, 1.21 to
-// 1.27 PFLOP/s, where a large bf16 product of this card's library reaches 1.13 to 1.25:
+// 8192 tokens over 16384 keys, 64 query heads over 8 (3.3 TFLOP): 2.64 to 2.75 ms, 1.20 to
+// 1.25 PFLOP/s, where a large bf16 product of this card's library reaches 1.13 to 1.25:
 // matrix cores 0.50 busy at 2.05 GHz, vector units 0.58, loads and barriers 4% of a wave's
 // time.  Blocks of 128 rows (two a compute unit) take 1.7 us for a tile, of 64 1.2.
 #include <type_traits>

@@ -8,10 +8,11 @@
 //   y = x / sqrt(mean(x^2) + eps) w,   y_a cos t - y_b sin t,   y_b cos t + y_a sin t
 // for q and k; v is stored as it is.  Everything is one read of the inputs and one
 // write of the outputs: the kernels are bound by memory, or where there are few rows
-// by one launch's latency.  1024 tokens of 32 + 32 + 32 heads (50 MB) 8.2 us; 19k of 64 + 8 + 8
-// (722 MB, into 4 bits) 144 us: 5.0 TB/s; one tree 3.4 to 4.2 us.  Reading the
-// 4-bit rows of those 19k back (99 MB): 21 us.  Compaction, three dependent loads and a
-// store: 4.8 to 5.2 us whatever the batch.
+// by one launch's latency.  1024 tokens of 32 + 32 + 32 heads (50 MB) 8.2 us on one set of
+// buffers, 10.0 on sets that change; 19k of 64 + 8 + 8 (722 MB, into 4 bits) 143 us: 5.0
+// TB/s; one tree 3.1 to 4.2 us.  Reading the 4-bit rows of those 19k back (99 MB): 19 us,
+// 29 right behind the append that wrote them.  Compaction, three dependent loads and a
+// store: 4.6 to 5.2 us whatever the batch.
 #include <algorithm>
 #include <type_traits>
 
