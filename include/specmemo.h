@@ -464,8 +464,9 @@ int specmemo_kv_append(specmemo_dtype dt, int32_t B, const int32_t *new_off_h, c
  * 128 columns takes 68 bytes instead of 256.  A row of a head is groups of 32
  * columns.  A column is a sign (bit 3) and one of the magnitudes 0, 1/2, 1, 3/2, 2, 3,
  * 4, 6 (codes 0 .. 7), times its group's 2^E; column 2 i is the low half of byte i.
- * The scale byte is E + 127.  Rows move and are dropped as those of specmemo_kv are:
- * every row has its own scales, so nothing is ever rounded twice. */
+ * The scale byte is E + 127 (2 .. 252), or 255: all values of the group are NaN.  Rows
+ * move and are dropped as those of specmemo_kv are: every row has its own scales, so
+ * nothing is ever rounded twice. */
 typedef struct {
   void *k, *v;                /* device uint8 [n_kv][cap_total][head_dim / 2]: codes */
   void *k_scale, *v_scale;    /* device uint8 [n_kv][cap_total][head_dim / 32] */
